@@ -108,7 +108,7 @@ typedef enum {
   T2V_ERR_OOM = 4,         /* the work-list cache could not allocate */
   T2V_ERR_BOUNDS = 5,      /* checked library only: a work item, or a row a kernel copies,
                               lies outside its clip (see "Checked library" below) */
-  T2V_ERR_WORKSPACE = 6    /* t2v_attn_bwd_qk_ws only: the workspace is too small */
+  T2V_ERR_WORKSPACE = 6    /* the workspace is too small (calls that take one) */
 } t2v_status;
 
 /* Tile orders for the scheduler (see t2v_build_worklist). */
@@ -210,6 +210,65 @@ int t2v_attn_bwd_qk_ws(const void* q, const void* k, const void* v,
                        int heads, int head_dim, float scale,
                        const void* dout, void* dq, void* dk, void* dv, float* delta_ws,
                        void* ws, uint64_t ws_bytes, uint64_t* need, void* stream);
+
+/* Causal attention with grouped heads, for prompts, for chunks and single tokens over cached keys, and for
+ * training. Sequences are packed as in t2v_attn_fwd_qk; of a sequence with Lq queries and Lk keys, query i
+ * sees keys 0 .. i + Lk - Lq (its last query sees every key). `heads` query heads share `kv_heads` key
+ * and value heads: query head h uses key head h / (heads / kv_heads). Any Lq and Lk >= 0 are allowed; a
+ * query that sees no key has out = 0, lse = -inf and dq = 0, a key that no query sees dk = dv = 0. What a
+ * query does not see does not reach its results, infinities and NaN included (those of dk and dv are the sums over
+ * the queries that see the key).
+ *   q            device bf16 [Tq, H, D], read only; q_stride elements between tokens, so that q may be a
+ *                slice of a fused projection: a multiple of 8, H * D <= q_stride <= 2^22
+ *   k, v         device bf16 [Tk, Hk, D] likewise, with k_stride and v_stride
+ *   out, dout, dq    device bf16 [Tq, H, D], contiguous;   lse device fp32 [H, Tq]
+ *   dk, dv       device bf16 [Tk, Hk, D], contiguous (sums over the heads of a group)
+ *   cu_seqlens_q, cu_seqlens_k   HOST int32 [nseq + 1] each (the same array twice for Lk = Lq); Lq times the
+ *                group's heads must stay below 2^31
+ *   heads, kv_heads   heads a multiple of kv_heads;   head_dim, scale as in t2v_attn_fwd
+ *   delta_ws     as in t2v_attn_bwd
+ *   ws, ws_bytes device scratch during the call, 16-byte aligned, for the partial results of long loops that
+ *                are cut so that all CUs take part; NULL and 0 if there is none
+ *   need         host uint64_t or NULL; receives the bytes that the call needs (at most 1 GiB, usually 0)
+ * With fewer than *need bytes nothing is launched and T2V_ERR_WORKSPACE is returned, so a first call with ws
+ * NULL asks for the size. Tensors without elements may be NULL. Outputs must not overlap each other or any
+ * input (q, k and v may overlap each other). Deterministic: no atomics; which loops are cut follows from
+ * the offsets and sizes alone. Work lists, streams, capture and errors as above. */
+int t2v_causal_fwd(const void* q, const void* k, const void* v,
+                   int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                   const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k, int nseq,
+                   int heads, int kv_heads, int head_dim, float scale, void* out, float* lse,
+                   void* ws, uint64_t ws_bytes, uint64_t* need, void* stream);
+
+int t2v_causal_bwd(const void* q, const void* k, const void* v,
+                   int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                   const void* out, const float* lse,
+                   const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k, int nseq,
+                   int heads, int kv_heads, int head_dim, float scale,
+                   const void* dout, void* dq, void* dk, void* dv, float* delta_ws,
+                   void* ws, uint64_t ws_bytes, uint64_t* need, void* stream);
+
+/* Rotary positions on the heads of q and k, before the attention calls: the first 2 n dimensions of each head, n the
+ * sum of the sections, are turned in pairs by angle position * freqs[j] and multiplied by mscale; the others are
+ * copied.
+ *   (y_a, y_b) = mscale * (x_a cos - x_b sin, x_a sin + x_b cos),  a, b = j, j + n (T2V_ROTARY_HALF) or
+ *   2 j, 2 j + 1 (T2V_ROTARY_INTERLEAVED)
+ * With inverse nonzero the angles' sign is turned, which is the gradient (of q from q_out's) too.
+ *   q, k         device bf16 [tokens, heads, D] and [tokens, kv_heads, D], read only, with q_stride and k_stride
+ *                elements between tokens as in t2v_causal_fwd; heads or kv_heads 0: that tensor is left out
+ *                (its pointers may be NULL, its stride is not read)
+ *   positions    device int32 [n_sections, tokens], any value
+ *   freqs        HOST double [n], radians a position, finite: angles are taken modulo a turn without rounding
+ *                at any position
+ *   sections     HOST int32 [n_sections], 1 to 3 counts of pairs (>= 0): the first sections[0] pairs turn by
+ *                row 0 of positions, and so on; 1 <= n <= D / 2
+ *   head_dim     D in {64, 128}
+ *   q_out, k_out device bf16, contiguous, written; must not overlap each other or any input
+ * Reads freqs and sections before it returns; needs no other memory. Errors as above. */
+typedef enum { T2V_ROTARY_HALF = 0, T2V_ROTARY_INTERLEAVED = 1 } t2v_rotary_layout;
+int t2v_rotary(const void* q, const void* k, int64_t q_stride, int64_t k_stride, const int32_t* positions,
+               int64_t tokens, int heads, int kv_heads, int head_dim, const double* freqs, const int32_t* sections,
+               int n_sections, int layout, float mscale, int inverse, void* q_out, void* k_out, void* stream);
 
 /* Thread-local message describing the last non-OK status of this thread. */
 const char* t2v_last_error(void);

@@ -36,7 +36,8 @@ ORDER_LONGEST_FIRST = 1
 EXPORTS = ("t2v_attn_fwd", "t2v_attn_bwd", "t2v_attn_fwd_qk", "t2v_attn_bwd_qk", "t2v_last_error",
            "t2v_release_cache", "t2v_build_worklist", "t2v_plan_makespan", "t2v_timing_enable", "t2v_kernel_times",
            "t2v_version", "t2v_list_schedule", "t2v_plan_cascades", "t2v_probe_mfma_peak", "t2v_trace_set",
-           "t2v_trace_count", "t2v_attn_bwd_noalloc", "t2v_attn_bwd_qk_ws")
+           "t2v_trace_count", "t2v_attn_bwd_noalloc", "t2v_attn_bwd_qk_ws", "t2v_causal_fwd", "t2v_causal_bwd",
+           "t2v_rotary")
 KERNEL_SLOTS = ("fwd", "bwd_pre", "bwd_dkdv", "bwd_dq")
 HOST_EXPORTS = ("t2v_last_error", "t2v_build_worklist", "t2v_plan_makespan", "t2v_version", "t2v_list_schedule",
                 "t2v_plan_cascades")
@@ -89,6 +90,18 @@ def _declare(lib, full: bool):
                                         ctypes.c_int, ctypes.c_float, _vp, _vp, _vp, _vp, _f32p, _vp]
         lib.t2v_attn_bwd_qk_ws.restype = ctypes.c_int
         lib.t2v_attn_bwd_qk_ws.argtypes = [*lib.t2v_attn_bwd_qk.argtypes[:-1], _vp, ctypes.c_uint64, _u64p, _vp]
+        lib.t2v_causal_fwd.restype = ctypes.c_int
+        lib.t2v_causal_fwd.argtypes = [_vp, _vp, _vp, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, _i32p, _i32p,
+                                       ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_float, _vp,
+                                       _f32p, _vp, ctypes.c_uint64, _u64p, _vp]
+        lib.t2v_causal_bwd.restype = ctypes.c_int
+        lib.t2v_causal_bwd.argtypes = [_vp, _vp, _vp, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, _vp, _f32p, _i32p,
+                                       _i32p, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_float,
+                                       _vp, _vp, _vp, _vp, _f32p, _vp, ctypes.c_uint64, _u64p, _vp]
+        lib.t2v_rotary.restype = ctypes.c_int
+        lib.t2v_rotary.argtypes = [_vp, _vp, ctypes.c_int64, ctypes.c_int64, _vp, ctypes.c_int64, ctypes.c_int,
+                                   ctypes.c_int, ctypes.c_int, _vp, _i32p, ctypes.c_int, ctypes.c_int, ctypes.c_float,
+                                   ctypes.c_int, _vp, _vp, _vp]
         lib.t2v_release_cache.restype = None
         lib.t2v_release_cache.argtypes = []
         lib.t2v_timing_enable.restype = ctypes.c_int
@@ -434,4 +447,112 @@ def attn_bwd(q, k, v, out, lse, dout, cu_seqlens, scale: float, dq=None, dk=None
                                       delta_ws.data_ptr(), None if ws is None else ws.data_ptr(),
                                       0 if ws is None else ws.numel(), need, _stream_handle(stream))
     _check(L, st)
+    return dq, dk, dv
+
+
+# ------------------------------------------------------- causal attention with grouped heads
+
+def _check_rows(t, name, shape):
+    """As _check_tensor, for a tensor whose tokens may be any distance apart (a slice of a fused
+    projection); returns that distance in elements."""
+    import torch
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.dtype != torch.bfloat16:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected {torch.bfloat16}")
+    T, H, D = shape
+    if t.numel() == 0 or t.is_contiguous():
+        return H * D
+    step = t.stride(0) if T > 1 else H * D
+    if t.stride(2) != 1 or (H > 1 and t.stride(1) != D) or step < H * D:
+        raise ValueError(f"{name} must hold each token's heads contiguously, got strides {t.stride()}")
+    return step
+
+
+def _causal_arguments(q, k, v, cu_seqlens, cu_seqlens_k):
+    """Checks what forward and backward share; returns (Tq, H, D, Tk, Hk, strides, query and key offsets)."""
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q and k must be [tokens, heads, head_dim]")
+    T, H, D = q.shape
+    Tk, Hk = k.shape[:2]
+    strides = (_check_rows(q, "q", (T, H, D)), _check_rows(k, "k", (Tk, Hk, D)), _check_rows(v, "v", (Tk, Hk, D)))
+    cq = _cu_array(cu_seqlens)
+    _check_offsets(cq, T, "cu_seqlens")
+    ck = cq if cu_seqlens_k is None else _cu_array(cu_seqlens_k)
+    _check_offsets(ck, Tk, "cu_seqlens" if cu_seqlens_k is None else "cu_seqlens_k")
+    if ck.shape != cq.shape:
+        raise ValueError(f"cu_seqlens has {cq.shape[0]} entries, cu_seqlens_k {ck.shape[0]}")
+    return T, H, D, Tk, Hk, strides, cq, ck
+
+
+def _on_device(t):
+    """The library works on the current device: make it the tensors' own."""
+    import torch
+    return contextlib.nullcontext() if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
+
+
+def _with_workspace(call, device, stream):
+    """call(ws address, ws bytes, need) until it has the workspace it asks for: twice at most."""
+    import torch
+    need = ctypes.c_uint64(0)
+    st = call(None, 0, ctypes.byref(need))
+    if st == T2V_ERR_WORKSPACE:
+        with _on(stream):
+            ws = torch.empty(need.value, dtype=torch.uint8, device=device)
+        st = call(ws.data_ptr(), ws.numel(), ctypes.byref(need))
+    return st
+
+
+def causal_attn_fwd(q, k, v, cu_seqlens, scale: float, out=None, lse=None, stream=None, cu_seqlens_k=None):
+    """Causal attention with grouped heads: q [Tq, H, D], k, v [Tk, Hk, D] (bf16, on the GPU; H a multiple of
+    Hk; tokens may be apart, as in slices of a fused projection). Query i of a sequence with Lq queries and Lk
+    keys sees keys 0 .. i + Lk - Lq; cu_seqlens_k None: Lk = Lq. Returns (out [Tq, H, D] bf16, lse [H, Tq] fp32).
+    """
+    import torch
+    T, H, D, Tk, Hk, strides, cq, ck = _causal_arguments(q, k, v, cu_seqlens, cu_seqlens_k)
+    if out is None or lse is None:
+        with _on(stream):
+            out = torch.empty((T, H, D), dtype=q.dtype, device=q.device) if out is None else out
+            lse = torch.empty((H, T), dtype=torch.float32, device=q.device) if lse is None else lse
+    _check_tensor(out, "out", (T, H, D))
+    _check_tensor(lse, "lse", (H, T), torch.float32)
+    _check_on_device((("q", q), ("k", k), ("v", v), ("out", out), ("lse", lse)))
+    L = lib()
+    with _on_device(q):
+        _check(L, _with_workspace(
+            lambda ws, n, need: L.t2v_causal_fwd(
+                q.data_ptr(), k.data_ptr(), v.data_ptr(), *strides, _offsets_ptr(cq), _offsets_ptr(ck),
+                cq.shape[0] - 1, H, Hk, D, float(scale), out.data_ptr(), lse.data_ptr(), ws, n, need,
+                _stream_handle(stream)), q.device, stream))
+    return out, lse
+
+
+def causal_attn_bwd(q, k, v, out, lse, dout, cu_seqlens, scale: float, dq=None, dk=None, dv=None, delta_ws=None,
+                    stream=None, cu_seqlens_k=None):
+    """Backward of causal_attn_fwd; returns (dq [Tq, H, D], dk, dv [Tk, Hk, D]) in bf16."""
+    import torch
+    T, H, D, Tk, Hk, strides, cq, ck = _causal_arguments(q, k, v, cu_seqlens, cu_seqlens_k)
+    for name, t in (("out", out), ("dout", dout)):
+        _check_tensor(t, name, (T, H, D))
+    _check_tensor(lse, "lse", (H, T), torch.float32)
+    with _on(stream):
+        dq = torch.empty((T, H, D), dtype=q.dtype, device=q.device) if dq is None else dq
+        dk = torch.empty((Tk, Hk, D), dtype=q.dtype, device=q.device) if dk is None else dk
+        dv = torch.empty((Tk, Hk, D), dtype=q.dtype, device=q.device) if dv is None else dv
+        if delta_ws is None:
+            delta_ws = torch.empty((2, H, T), dtype=torch.float32, device=q.device)
+    _check_tensor(dq, "dq", (T, H, D))
+    _check_tensor(dk, "dk", (Tk, Hk, D))
+    _check_tensor(dv, "dv", (Tk, Hk, D))
+    _check_tensor(delta_ws, "delta_ws", (2, H, T), torch.float32)
+    _check_on_device((("q", q), ("k", k), ("v", v), ("out", out), ("lse", lse), ("dout", dout), ("dq", dq),
+                      ("dk", dk), ("dv", dv), ("delta_ws", delta_ws)))
+    L = lib()
+    with _on_device(q):
+        _check(L, _with_workspace(
+            lambda ws, n, need: L.t2v_causal_bwd(
+                q.data_ptr(), k.data_ptr(), v.data_ptr(), *strides, out.data_ptr(), lse.data_ptr(), _offsets_ptr(cq),
+                _offsets_ptr(ck), cq.shape[0] - 1, H, Hk, D, float(scale), dout.data_ptr(), dq.data_ptr(),
+                dk.data_ptr(), dv.data_ptr(), delta_ws.data_ptr(), ws, n, need, _stream_handle(stream)),
+            q.device, stream))
     return dq, dk, dv

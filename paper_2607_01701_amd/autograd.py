@@ -6,10 +6,10 @@ from __future__ import annotations
 
 import numpy as np
 
-from ._lib import _cu_array, attn_bwd, attn_fwd
+from ._lib import _cu_array, attn_bwd, attn_fwd, causal_attn_bwd, causal_attn_fwd
 
 
-def _function():
+def _function(attn_fwd, attn_bwd):
     import torch
 
     class _VarlenAttention(torch.autograd.Function):
@@ -36,7 +36,8 @@ def _function():
     return _VarlenAttention
 
 
-_FN = None
+_FN = None  # varlen_attention's Function, made at its first call (torch is imported late)
+_CAUSAL_FN = None
 
 
 def varlen_attention(q, k, v, cu_seqlens, scale: float, cu_seqlens_k=None):
@@ -45,7 +46,18 @@ def varlen_attention(q, k, v, cu_seqlens, scale: float, cu_seqlens_k=None):
     gradients flow to q, k and v (lse is not differentiated)."""
     global _FN
     if _FN is None:
-        _FN = _function()
+        _FN = _function(attn_fwd, attn_bwd)
     cu = _cu_array(cu_seqlens)
     ck = None if cu_seqlens_k is None else _cu_array(cu_seqlens_k)
     return _FN.apply(q, k, v, np.array(cu, copy=True), float(scale), None if ck is None else np.array(ck, copy=True))
+
+
+def varlen_causal_attention(q, k, v, cu_seqlens, scale: float, cu_seqlens_k=None):
+    """Causal attention with grouped heads and autograd: q [Tq, H, D], k, v [Tk, Hk, D] as in causal_attn_fwd.
+    Returns (out, lse); gradients flow to q, k and v (lse is not differentiated)."""
+    global _CAUSAL_FN
+    if _CAUSAL_FN is None:
+        _CAUSAL_FN = _function(causal_attn_fwd, causal_attn_bwd)
+    cu = np.array(_cu_array(cu_seqlens), copy=True)
+    ck = None if cu_seqlens_k is None else np.array(_cu_array(cu_seqlens_k), copy=True)
+    return _CAUSAL_FN.apply(q, k, v, cu, float(scale), ck)

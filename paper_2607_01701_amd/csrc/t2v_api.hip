@@ -14,6 +14,7 @@
 #include <vector>
 
 #include "../../include/t2vattn.h"
+#include "t2v_causal_kernels.h"
 #include "t2v_host.h"
 #include "t2v_kernels.h"
 
@@ -48,7 +49,7 @@ int order_from_env() {
 // sharding) loses more to a part-empty last round of wide tiles. T2V_QTILE=wide or narrow
 // forces one (ablations and tests).
 struct TileRule {
-  int kind = 0;  // 0: dK/dV, 1: forward, 2: dQ, 3: one-pass backward of short key segments
+  int kind = 0;  // 0: dK/dV, 1: forward, 2: dQ, 3: one-pass backward of short key segments, then CausalKernel
   int wide = 0, narrow = 0;
   bool narrow_always = false;
   double max_loop = 0.0, penalty = 1.0;
@@ -181,7 +182,7 @@ TileRule short_rule() {
   return r;
 }
 
-// T2V_SPLIT=off disables the dK/dV loop split (for ablations).
+// T2V_SPLIT=off disables the loop splits (for ablations).
 bool split_enabled() {
   const char* s = std::getenv("T2V_SPLIT");
   return s == nullptr || std::strcmp(s, "off") != 0;
@@ -195,6 +196,66 @@ int cu_count() {
     return 0;
   }
   return n;
+}
+
+// ------------------------------------------------------- plans of the causal attention kernels
+
+// Rule of a causal work list. The narrow forms of forward and dQ keep two workgroups on a CU at
+// head_dim 128 and three at 64, the wide ones one.
+TileRule causal_rule(CausalKernel kind, int head_dim) {
+  TileRule r;
+  r.kind = kind;
+  if (kind == kCausalDkdv) {
+    r.wide = r.narrow = causal_dkdv_keys(head_dim);
+    return r;
+  }
+  r.narrow = kind == kCausalFwd ? causal_fwd_rows(true) : causal_dq_rows(true);
+  r.wide = kind == kCausalFwd ? causal_fwd_rows(false) : causal_dq_rows(false);
+  r.narrow_always = head_dim == 64;
+  r.forced = forced_tiles();
+  return r;
+}
+
+int64_t causal_slot_bytes(CausalKernel kind, int rows, int head_dim) {
+  if (kind == kCausalFwd) return causal_fwd_slot_bytes(rows, head_dim);
+  return kind == kCausalDq ? causal_dq_slot_bytes(rows, head_dim) : causal_dkdv_slot_bytes(head_dim);
+}
+
+constexpr int64_t kCausalMaxWorkspace = int64_t(1) << 30;
+
+// An item's fixed part (loads of its rows, stores, filling the pipeline) in keys or stages, and the
+// least length of a piece.
+double causal_fixed(CausalKernel kind) { return kind == kCausalDkdv ? 4.0 : 128.0; }
+int causal_least(CausalKernel kind) { return kind == kCausalDkdv ? 16 : 512; }
+
+CausalList causal_plan(const TileRule& r, const CausalShape& a, int head_dim, int order, bool split, int ncu,
+                       int* block) {
+  const auto kind = static_cast<CausalKernel>(r.kind);
+  const int stage = causal_dkdv_stage(head_dim);
+  const double fixed = causal_fixed(kind);
+  auto workers = [&](int rows) {
+    if (kind == kCausalDkdv || rows == r.wide) return ncu;
+    return ncu * (head_dim == 64 ? 3 : 2);
+  };
+  auto list = [&](int rows) {
+    int chunk = 0;
+    if (split && ncu > 0)
+      chunk = causal_chunk(kind, a, rows, stage, fixed, workers(rows), causal_least(kind),
+                           std::min<int64_t>(kCausalMaxWorkspace / causal_slot_bytes(kind, rows, head_dim), INT32_MAX));
+    return build_causal_list(kind, a, rows, stage, order, chunk, fixed);
+  };
+  *block = r.narrow;
+  if (r.forced == 2 || r.wide == r.narrow || (r.forced == 0 && r.narrow_always)) return list(*block);
+  CausalList wide = list(r.wide);
+  if (r.forced == 1) {
+    *block = r.wide;
+    return wide;
+  }
+  CausalList narrow = list(r.narrow);
+  if (causal_makespan(narrow, fixed, workers(r.narrow)) * 1.04 < causal_makespan(wide, fixed, workers(r.wide)))
+    return narrow;
+  *block = r.wide;
+  return wide;
 }
 
 // T2V_LOG=1: one line on stderr per new work list (items, predicted makespan, bound).
@@ -453,7 +514,9 @@ struct Plan {
   std::vector<int32_t> cu, cu_loop;  // offsets of the owned and the looped-over segments
   TileRule rule;                     // how block was chosen (part of the key)
   int heads = 0, block = 0, order = 0, device = 0, chunk = 0;
-  Item* d_items = nullptr;  // n_items work items, then n_reduce split tiles (loop split)
+  int group = 0, head_dim = 0;  // causal lists: query heads of a key head (`heads` counts key heads)
+  int64_t slots = 0;            // causal lists: partial slots that the items write
+  void* d_items = nullptr;  // n_items work items, then n_reduce split tiles (loop split)
   int n_items = 0, n_reduce = 0;
   ListPool::Block mem;             // d_items' block in the device pool
   hipEvent_t ready = nullptr;      // upload finished (from the device pool's event pool)
@@ -461,7 +524,10 @@ struct Plan {
   bool captured = false;  // a captured graph's launches read d_items
 #if T2V_CHECKED
   std::vector<Item> host_items;  // checked builds: the list as uploaded, validated at every call
+  std::vector<CausalItem> host_causal;
 #endif
+  const Item* items() const { return static_cast<const Item*>(d_items); }
+  const CausalItem* causal() const { return static_cast<const CausalItem*>(d_items); }
   ~Plan() {
     DevicePools& p = pools(device);
     std::lock_guard<std::mutex> lock(p.mu);
@@ -516,9 +582,10 @@ class PlanCache {
   // Returns the plan (creating and uploading it on `stream` if new) with the
   // upload ordered before any later work on `stream`.
   // The tile rows follow `rule` (chosen once, when the plan is built; plan->block). chunk > 0:
-  // the loop split of build_worklist, with the reduce list after the items.
+  // the loop split of build_worklist, with the reduce list after the items. Causal lists (group > 0): cu
+  // are the queries' offsets, cu_loop the keys', heads the key heads; chunk is -1 for no split.
   int get(const int32_t* cu, const int32_t* cu_loop, int nseq, int heads, const TileRule& rule, int order, int chunk,
-          hipStream_t stream, PlanRef* out) {
+          hipStream_t stream, PlanRef* out, int group = 0, int head_dim = 0) {
     int device = 0;
     hipError_t e = hipGetDevice(&device);
     if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
@@ -527,6 +594,7 @@ class PlanCache {
     for (auto itr = plans_.begin(); itr != plans_.end(); ++itr) {
       Plan& p = **itr;
       if (p.heads == heads && p.rule.same(rule) && p.order == order && p.device == device && p.chunk == chunk &&
+          p.group == group && p.head_dim == head_dim &&
           p.cu.size() == static_cast<size_t>(nseq + 1) &&
           std::memcmp(p.cu.data(), cu, sizeof(int32_t) * (nseq + 1)) == 0 &&
           std::memcmp(p.cu_loop.data(), cu_loop, sizeof(int32_t) * (nseq + 1)) == 0) {
@@ -554,26 +622,52 @@ class PlanCache {
       ncu = 0;
     }
     std::vector<Item> items;
-    const int block = rows_of(rule, cu, cu_loop, nseq, heads, order, ncu, &items);
+    CausalList causal;
+    int block = 0;
+    if (group > 0)
+      causal = causal_plan(rule, {cu, cu_loop, nseq, heads, group}, head_dim, order, chunk == 0, ncu, &block);
+    else
+      block = rows_of(rule, cu, cu_loop, nseq, heads, order, ncu, &items);
     p->rule = rule;
     p->heads = heads;
     p->block = block;
     p->order = order;
     p->device = device;
     p->chunk = chunk;
-    if (items.empty() || chunk > 0)
-      items = build_worklist(cu, cu_loop, nseq, heads, block, order, chunk, rule.kind == 3 ? short_weight : nullptr);
-    p->n_items = static_cast<int>(items.size());
-    if (chunk > 0) {
-      const std::vector<Item> red = build_reduce_list(cu, cu_loop, nseq, heads, block, chunk);
-      p->n_reduce = static_cast<int>(red.size());
-      items.insert(items.end(), red.begin(), red.end());
-    }
-    const size_t bytes = items.size() * sizeof(Item);
+    p->group = group;
+    p->head_dim = head_dim;
+    const void* list = nullptr;
+    size_t bytes = 0;
+    if (group > 0) {
+      p->slots = causal.slots;
+      p->n_items = static_cast<int>(causal.items.size());
+      p->n_reduce = static_cast<int>(causal.reduce.size());
+      if (log_enabled())
+        std::fprintf(stderr, "t2v: causal work list: %d sequences, %d x %d heads, %d-row tiles: %d items, %d split tiles, "
+                     "%lld slots on %d CUs\n", nseq, heads, group, block, p->n_items, p->n_reduce,
+                     static_cast<long long>(p->slots), ncu);
+      causal.items.insert(causal.items.end(), causal.reduce.begin(), causal.reduce.end());
+      list = causal.items.data();
+      bytes = causal.items.size() * sizeof(CausalItem);
 #if T2V_CHECKED
-    p->host_items = items;
+      p->host_causal = causal.items;
 #endif
-    if (log_enabled()) {
+    } else {
+      if (items.empty() || chunk > 0)
+        items = build_worklist(cu, cu_loop, nseq, heads, block, order, chunk, rule.kind == 3 ? short_weight : nullptr);
+      p->n_items = static_cast<int>(items.size());
+      if (chunk > 0) {
+        const std::vector<Item> red = build_reduce_list(cu, cu_loop, nseq, heads, block, chunk);
+        p->n_reduce = static_cast<int>(red.size());
+        items.insert(items.end(), red.begin(), red.end());
+      }
+      list = items.data();
+      bytes = items.size() * sizeof(Item);
+#if T2V_CHECKED
+      p->host_items = items;
+#endif
+    }
+    if (log_enabled() && group == 0) {
       double ms = 0.0, lb = 0.0;
       plan_makespan(items.data(), p->n_items, block, ncu > 0 ? ncu : 1, &ms, &lb);
       std::fprintf(stderr,
@@ -596,8 +690,8 @@ class PlanCache {
         p->mem = ListPool::Block{};
         return st;
       }
-      p->d_items = static_cast<Item*>(p->mem.ptr);
-      std::memcpy(staging.ptr, items.data(), bytes);
+      p->d_items = p->mem.ptr;
+      std::memcpy(staging.ptr, list, bytes);
       if (capturing) {
         // Now, outside the graph: an eager call that finds the plan before the graph has run would
         // otherwise read a list that is not there yet.
@@ -688,6 +782,17 @@ int check_plan(const PlanRef& p, const int32_t* cu_own, const int32_t* cu_loop, 
                     kernel);
 }
 
+int check_causal_plan(const PlanRef& p, const int32_t* cu_q, const int32_t* cu_k, int nseq, const char* kernel) {
+  const CausalShape a{cu_q, cu_k, nseq, p->heads, p->group};
+  const auto kind = static_cast<CausalKernel>(p->rule.kind);
+  const CausalItem* items = p->host_causal.data();
+  const int stage = causal_dkdv_stage(p->head_dim);
+  std::string why = check_causal_items(kind, items, p->n_items, a, p->block, stage, p->slots, false);
+  if (why.empty()) why = check_causal_items(kind, items + p->n_items, p->n_reduce, a, p->block, stage, p->slots, true);
+  if (!why.empty()) return set_error(T2V_ERR_BOUNDS, std::string("checked library: ") + kernel + " work list, " + why);
+  return T2V_OK;
+}
+
 // Set by check_arm once a call is about to launch kernels: only such calls wait for the device
 // afterwards (a call refused by validation, or with nothing to do, makes no device call).
 thread_local bool t_check_armed = false;
@@ -696,7 +801,8 @@ thread_local bool t_check_armed = false;
 int check_arm() {
   const unsigned int canary = check_canary();
   unsigned int rec[4];
-  for (auto take : {fwd_check_take, dkdv_check_take, dkdv_wide_check_take, dq_check_take, short_check_take}) {
+  for (auto take : {fwd_check_take, dkdv_check_take, dkdv_wide_check_take, dq_check_take, short_check_take,
+                    causal_fwd_check_take, causal_dkdv_check_take, causal_dq_check_take}) {
     const hipError_t e = take(rec, canary);
     if (e != hipSuccess) return hip_fail(e, "clearing the DMA row checks");
   }
@@ -708,11 +814,14 @@ int check_arm() {
 int check_collect(hipStream_t s) {
   hipError_t e = hipStreamSynchronize(s);
   if (e != hipSuccess) return hip_fail(e, "waiting for the checked kernels");
-  const char* names[5] = {"forward", "dK/dV", "dK/dV", "dQ", "one-pass backward"};
-  hipError_t (*takes[5])(unsigned int*, unsigned int) = {fwd_check_take, dkdv_check_take, dkdv_wide_check_take,
-                                                         dq_check_take, short_check_take};
+  constexpr int kSources = 8;
+  const char* names[kSources] = {"forward",        "dK/dV",        "dK/dV",    "dQ", "one-pass backward",
+                                 "causal forward", "causal dK/dV", "causal dQ"};
+  hipError_t (*takes[kSources])(unsigned int*, unsigned int) = {
+      fwd_check_take,   dkdv_check_take,       dkdv_wide_check_take,   dq_check_take,
+      short_check_take, causal_fwd_check_take, causal_dkdv_check_take, causal_dq_check_take};
   int status = T2V_OK;
-  for (int i = 0; i < 5; ++i) {
+  for (int i = 0; i < kSources; ++i) {
     unsigned int rec[4];
     e = takes[i](rec, 0u);
     if (e != hipSuccess) return hip_fail(e, "reading the DMA row checks");
@@ -886,7 +995,7 @@ int attn_fwd_impl(const void* q, const void* k, const void* v, const int32_t* cu
   a.scale = scale;
   a.trace = tracer().reserve(plan->n_items);
   a.persistent = persistent_enabled();
-  hipError_t e = timer().run(kSlotFwd, s, [&] { return launch_fwd(a, out, lse, plan->d_items, plan->n_items, s); });
+  hipError_t e = timer().run(kSlotFwd, s, [&] { return launch_fwd(a, out, lse, plan->items(), plan->n_items, s); });
   const int used = note_use(plan, s);
   if (e != hipSuccess) return hip_fail(e, "forward kernel launch");
   return used;
@@ -949,7 +1058,7 @@ int attn_bwd_short(const AttnArgs& args, const int32_t* cu_q, const int32_t* cu_
     a.partial = static_cast<float*>(ws->ptr);
     a.trace = tracer().reserve(plan->n_items);
     const hipError_t e = timer().run(kSlotDkdv, s, [&] {
-      return launch_bwd_short(a, plan->d_items, plan->n_items, plan->d_items + plan->n_items, plan->n_reduce, s);
+      return launch_bwd_short(a, plan->items(), plan->n_items, plan->items() + plan->n_items, plan->n_reduce, s);
     });
     const int used = note_use(plan, s);
     if (e != hipSuccess) return hip_fail(e, "one-pass backward launch");
@@ -1027,8 +1136,8 @@ int attn_bwd_impl(const void* q, const void* k, const void* v, const void* out, 
   if (pk->n_items > 0) {
     a.trace = tracer().reserve(pk->n_items);
     e = timer().run(kSlotDkdv, s, [&] {
-      hipError_t r = launch_bwd_dkdv(a, pk->d_items, pk->n_items, s);
-      if (r == hipSuccess && pk->n_reduce > 0) r = launch_bwd_dkdv_reduce(a, pk->d_items + pk->n_items, pk->n_reduce, s);
+      hipError_t r = launch_bwd_dkdv(a, pk->items(), pk->n_items, s);
+      if (r == hipSuccess && pk->n_reduce > 0) r = launch_bwd_dkdv_reduce(a, pk->items() + pk->n_items, pk->n_reduce, s);
       return r;
     });
     const int used = note_use(pk, s);
@@ -1037,7 +1146,7 @@ int attn_bwd_impl(const void* q, const void* k, const void* v, const void* out, 
   }
   if (pq->n_items > 0) {
     a.trace = tracer().reserve(pq->n_items);
-    e = timer().run(kSlotDq, s, [&] { return launch_bwd_dq(a, pq->d_items, pq->n_items, s); });
+    e = timer().run(kSlotDq, s, [&] { return launch_bwd_dq(a, pq->items(), pq->n_items, s); });
     const int used = note_use(pq, s);
     if (e != hipSuccess) return hip_fail(e, "dQ kernel launch");
     if (used != T2V_OK) return used;
@@ -1209,6 +1318,205 @@ int attn_bwd_noalloc_impl(const void* q, const void* k, const void* v, const voi
   return T2V_OK;
 }
 
+// ------------------------------------------------------- causal attention with grouped heads
+
+// The arguments that forward and backward share.
+struct CausalCall {
+  const void *q, *k, *v;
+  int64_t q_stride, k_stride, v_stride;
+  const int32_t *cu_q, *cu_k;
+  int nseq, heads, kv_heads, head_dim;
+  float scale;
+  int64_t tq = 0, tk = 0;
+};
+
+int64_t strided_bytes(int64_t tokens, int64_t stride, int heads, int head_dim) {
+  return tokens == 0 ? 0 : 2 * ((tokens - 1) * stride + static_cast<int64_t>(heads) * head_dim);
+}
+
+// Offsets, shapes and strides; fills tq and tk.
+int validate_causal(CausalCall& c) {
+  if (int st = check_offsets_on_host(c.cu_q, c.cu_k)) return st;
+  if (c.kv_heads < 1 || c.heads < 1 || c.heads % c.kv_heads != 0)
+    return set_error(T2V_ERR_INVALID_ARG, "heads (" + std::to_string(c.heads) + ") must be a multiple of kv_heads (" +
+                                              std::to_string(c.kv_heads) + ")");
+  if (int st = validate_shape(c.cu_q, c.nseq, c.heads, c.head_dim, c.scale, &c.tq)) return st;
+  if (c.cu_k != c.cu_q) {
+    if (int st = validate_shape(c.cu_k, c.nseq, c.kv_heads, c.head_dim, c.scale, &c.tk))
+      return set_error(st, std::string("cu_seqlens_k: ") + last_error());
+  } else {
+    c.tk = c.tq;
+  }
+  const int64_t group = c.heads / c.kv_heads;
+  for (int s = 0; s < c.nseq; ++s)
+    if ((c.cu_q[s + 1] - c.cu_q[s]) * group > INT32_MAX - 512)
+      return set_error(T2V_ERR_INVALID_ARG, "sequence " + std::to_string(s) + " has too many queries for its group of heads");
+  const struct {
+    int64_t stride;
+    int heads;
+    const char* name;
+  } strides[3] = {{c.q_stride, c.heads, "q_stride"}, {c.k_stride, c.kv_heads, "k_stride"}, {c.v_stride, c.kv_heads, "v_stride"}};
+  for (const auto& t : strides)
+    if (t.stride < static_cast<int64_t>(t.heads) * c.head_dim || t.stride % 8 != 0 || t.stride > (int64_t(1) << 22))
+      return set_error(T2V_ERR_INVALID_ARG, std::string(t.name) + " must be a multiple of 8 between heads * head_dim and 2^22, got " +
+                                                std::to_string(t.stride));
+  return T2V_OK;
+}
+
+// Pointer checks as validate_pointers; tensors without elements may be NULL.
+int validate_nonempty(std::vector<Range> inputs, std::vector<Range> outputs) {
+  auto empty = [](const Range& r) { return r.bytes == 0; };
+  inputs.erase(std::remove_if(inputs.begin(), inputs.end(), empty), inputs.end());
+  outputs.erase(std::remove_if(outputs.begin(), outputs.end(), empty), outputs.end());
+  return validate_pointers(inputs, outputs);
+}
+
+int causal_get(CausalKernel kind, const CausalCall& c, hipStream_t s, PlanRef* plan) {
+  return cache().get(c.cu_q, c.cu_k, c.nseq, c.kv_heads, causal_rule(kind, c.head_dim), order_from_env(),
+                     split_enabled() ? 0 : -1, s, plan, c.heads / c.kv_heads, c.head_dim);
+}
+
+uint64_t causal_workspace(const PlanRef& p) {
+  return static_cast<uint64_t>(p->slots * causal_slot_bytes(static_cast<CausalKernel>(p->rule.kind), p->block, p->head_dim));
+}
+
+int check_workspace(uint64_t have, uint64_t need) {
+  if (have >= need) return T2V_OK;
+  return set_error(T2V_ERR_WORKSPACE, "the call needs " + std::to_string(need) + " bytes of workspace, got " +
+                                          std::to_string(have));
+}
+
+CausalArgs causal_args(const CausalCall& c, void* ws) {
+  CausalArgs a{};
+  a.q = c.q;
+  a.k = c.k;
+  a.v = c.v;
+  a.q_stride = c.q_stride;
+  a.k_stride = c.k_stride;
+  a.v_stride = c.v_stride;
+  a.heads = c.heads;
+  a.kv_heads = c.kv_heads;
+  a.head_dim = c.head_dim;
+  a.tq = c.tq;
+  a.scale = c.scale;
+  a.partial = static_cast<float*>(ws);
+  return a;
+}
+
+int causal_fwd_impl(CausalCall& c, void* out, float* lse, void* ws, uint64_t ws_bytes, uint64_t* need, void* stream) {
+  if (need != nullptr) *need = 0;
+  if (int st = validate_causal(c)) return st;
+  if (c.tq == 0) return T2V_OK;
+  if (int st = validate_nonempty({{c.q, strided_bytes(c.tq, c.q_stride, c.heads, c.head_dim), "q"},
+                                  {c.k, strided_bytes(c.tk, c.k_stride, c.kv_heads, c.head_dim), "k"},
+                                  {c.v, strided_bytes(c.tk, c.v_stride, c.kv_heads, c.head_dim), "v"}},
+                                 {{out, tensor_bytes(c.tq, c.heads, c.head_dim), "out"},
+                                  {lse, c.tq * c.heads * 4, "lse"},
+                                  {ws, static_cast<int64_t>(ws_bytes), "ws"}}))
+    return st;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  PlanRef plan;
+  if (int st = causal_get(kCausalFwd, c, s, &plan)) return st;
+  const uint64_t bytes = causal_workspace(plan);
+  if (need != nullptr) *need = bytes;
+  if (int st = check_workspace(ws_bytes, bytes)) return st;
+#if T2V_CHECKED
+  if (int st = check_causal_plan(plan, c.cu_q, c.cu_k, c.nseq, "causal forward")) return st;
+  if (int st = check_arm()) return st;
+#endif
+  CausalArgs a = causal_args(c, ws);
+  a.out = out;
+  a.lse = lse;
+  a.trace = tracer().reserve(plan->n_items);
+  const hipError_t e = timer().run(kSlotFwd, s, [&] {
+    hipError_t r = launch_causal_fwd(a, plan->block, plan->causal(), plan->n_items, s);
+    if (r == hipSuccess && plan->n_reduce > 0)
+      r = launch_causal_fwd_join(a, plan->block, plan->causal() + plan->n_items, plan->n_reduce, s);
+    return r;
+  });
+  const int used = note_use(plan, s);
+  if (e != hipSuccess) return hip_fail(e, "causal forward kernel launch");
+  return used;
+}
+
+int causal_bwd_impl(CausalCall& c, const void* out, const float* lse, const void* dout, void* dq, void* dk, void* dv,
+                    float* delta_ws, void* ws, uint64_t ws_bytes, uint64_t* need, void* stream) {
+  if (need != nullptr) *need = 0;
+  if (int st = validate_causal(c)) return st;
+  if (c.tq == 0 && c.tk == 0) return T2V_OK;
+  const int64_t qb = tensor_bytes(c.tq, c.heads, c.head_dim), kb = tensor_bytes(c.tk, c.kv_heads, c.head_dim);
+  const int64_t lb = c.tq * c.heads * 4;
+  if (int st = validate_nonempty({{c.q, strided_bytes(c.tq, c.q_stride, c.heads, c.head_dim), "q"},
+                                  {c.k, strided_bytes(c.tk, c.k_stride, c.kv_heads, c.head_dim), "k"},
+                                  {c.v, strided_bytes(c.tk, c.v_stride, c.kv_heads, c.head_dim), "v"},
+                                  {out, qb, "out"},
+                                  {lse, lb, "lse"},
+                                  {dout, qb, "dout"}},
+                                 {{dq, qb, "dq"},
+                                  {dk, kb, "dk"},
+                                  {dv, kb, "dv"},
+                                  {delta_ws, 2 * lb, "delta_ws"},
+                                  {ws, static_cast<int64_t>(ws_bytes), "ws"}}))
+    return st;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  PlanRef pk, pq;
+  if (int st = causal_get(kCausalDkdv, c, s, &pk)) return st;
+  if (int st = causal_get(kCausalDq, c, s, &pq)) return st;
+  // The two kernels use the workspace one after the other.
+  const uint64_t bytes = std::max(causal_workspace(pk), causal_workspace(pq));
+  if (need != nullptr) *need = bytes;
+  if (int st = check_workspace(ws_bytes, bytes)) return st;
+#if T2V_CHECKED
+  if (int st = check_causal_plan(pk, c.cu_q, c.cu_k, c.nseq, "causal dK/dV")) return st;
+  if (int st = check_causal_plan(pq, c.cu_q, c.cu_k, c.nseq, "causal dQ")) return st;
+  if (int st = check_arm()) return st;
+#endif
+  hipError_t e = hipSuccess;
+  if (c.tq > 0) {
+    AttnArgs p{};
+    p.out = out;
+    p.dout = dout;
+    p.lse = lse;
+    p.delta = delta_ws;
+    p.heads = c.heads;
+    p.head_dim = c.head_dim;
+    p.total_tokens = c.tq;
+    e = timer().run(kSlotPre, s, [&] { return launch_bwd_pre(p, s); });
+    if (e != hipSuccess) return hip_fail(e, "backward preprocess launch");
+  }
+  CausalArgs a = causal_args(c, ws);
+  a.dout = dout;
+  a.delta = delta_ws;
+  a.dq = dq;
+  a.dk = dk;
+  a.dv = dv;
+  if (pk->n_items > 0) {
+    a.trace = tracer().reserve(pk->n_items);
+    e = timer().run(kSlotDkdv, s, [&] {
+      hipError_t r = launch_causal_dkdv(a, pk->causal(), pk->n_items, s);
+      if (r == hipSuccess && pk->n_reduce > 0)
+        r = launch_causal_dkdv_join(a, pk->causal() + pk->n_items, pk->n_reduce, s);
+      return r;
+    });
+    const int used = note_use(pk, s);
+    if (e != hipSuccess) return hip_fail(e, "causal dK/dV kernel launch");
+    if (used != T2V_OK) return used;
+  }
+  if (pq->n_items > 0) {
+    a.trace = tracer().reserve(pq->n_items);
+    e = timer().run(kSlotDq, s, [&] {
+      hipError_t r = launch_causal_dq(a, pq->block, pq->causal(), pq->n_items, s);
+      if (r == hipSuccess && pq->n_reduce > 0)
+        r = launch_causal_dq_join(a, pq->block, pq->causal() + pq->n_items, pq->n_reduce, s);
+      return r;
+    });
+    const int used = note_use(pq, s);
+    if (e != hipSuccess) return hip_fail(e, "causal dQ kernel launch");
+    if (used != T2V_OK) return used;
+  }
+  return T2V_OK;
+}
+
 // Runs f, turning host exceptions into statuses (none may cross the C ABI).
 template <typename F>
 int guarded(F&& f) {
@@ -1331,6 +1639,28 @@ int t2v_attn_bwd_qk_ws(const void* q, const void* k, const void* v, const void* 
       need[1] = w.need[1];
     }
     return st;
+  });
+}
+
+int t2v_causal_fwd(const void* q, const void* k, const void* v, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                   const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k, int nseq, int heads, int kv_heads,
+                   int head_dim, float scale, void* out, float* lse, void* ws, uint64_t ws_bytes, uint64_t* need,
+                   void* stream) {
+  return t2v::guarded([&] {
+    t2v::CausalCall c{q, k, v, q_stride, k_stride, v_stride, cu_seqlens_q, cu_seqlens_k, nseq, heads, kv_heads, head_dim, scale};
+    return t2v::checked_call(stream, [&] { return t2v::causal_fwd_impl(c, out, lse, ws, ws_bytes, need, stream); });
+  });
+}
+
+int t2v_causal_bwd(const void* q, const void* k, const void* v, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                   const void* out, const float* lse, const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k, int nseq,
+                   int heads, int kv_heads, int head_dim, float scale, const void* dout, void* dq, void* dk, void* dv,
+                   float* delta_ws, void* ws, uint64_t ws_bytes, uint64_t* need, void* stream) {
+  return t2v::guarded([&] {
+    t2v::CausalCall c{q, k, v, q_stride, k_stride, v_stride, cu_seqlens_q, cu_seqlens_k, nseq, heads, kv_heads, head_dim, scale};
+    return t2v::checked_call(stream, [&] {
+      return t2v::causal_bwd_impl(c, out, lse, dout, dq, dk, dv, delta_ws, ws, ws_bytes, need, stream);
+    });
   });
 }
 

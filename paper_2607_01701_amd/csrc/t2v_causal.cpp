@@ -1,0 +1,212 @@
+// Work lists of causal attention (t2v_causal.h): no HIP, compiled with g++ for CPU tests too.
+#include "t2v_causal.h"
+
+#include <algorithm>
+#include <cmath>
+#include <functional>
+#include <queue>
+
+#include "../../include/t2vattn.h"
+#include "t2v_host.h"
+
+namespace t2v {
+
+namespace {
+
+// Tiles and the loop of tile t of one (sequence, key head).
+struct Loops {
+  CausalKernel kind;
+  int32_t lq, lk;
+  int group, block, stage;
+  int tiles() const {
+    const int64_t rows = kind == kCausalDkdv ? lk : static_cast<int64_t>(lq) * group;
+    return static_cast<int>((rows + block - 1) / block);
+  }
+  int32_t length(int t) const {
+    const int64_t r0 = static_cast<int64_t>(t) * block;
+    if (kind == kCausalDkdv) return group * causal_stages(static_cast<int32_t>(r0), lq, lk, stage);
+    const int64_t last = std::min<int64_t>(r0 + block, static_cast<int64_t>(lq) * group) - 1;
+    return causal_keys(static_cast<int32_t>(last / group), lq, lk);
+  }
+  // The longest loop is that of the last tile of rows, of the first tile of keys.
+  int32_t longest() const { return tiles() == 0 ? 0 : length(kind == kCausalDkdv ? 0 : tiles() - 1); }
+};
+
+Loops loops_of(CausalKernel kind, const CausalShape& a, int s, int block, int stage) {
+  return {kind, a.cu_q[s + 1] - a.cu_q[s], a.cu_k[s + 1] - a.cu_k[s], a.group, block, stage};
+}
+
+// Equal pieces of a loop of n units cut at chunk: *count of *step units, the last shorter.
+void pieces_of(CausalKernel kind, int n, int chunk, int* count, int* step) {
+  *count = 1;
+  *step = n;
+  if (chunk <= 0 || n <= chunk) return;
+  const int unit = kind == kCausalDkdv ? 1 : 64;
+  const int most = (n + chunk - 1) / chunk;
+  *step = ((n + most - 1) / most + unit - 1) / unit * unit;
+  *count = (n + *step - 1) / *step;
+}
+
+}  // namespace
+
+CausalList build_causal_list(CausalKernel kind, const CausalShape& a, int block, int stage, int order, int chunk,
+                             double fixed) {
+  CausalList out;
+  struct Group {
+    int seq, head;
+    double longest, cost;
+    std::vector<CausalItem> items;
+  };
+  std::vector<Group> groups;
+  size_t n = 0;
+  for (int s = 0; s < a.nseq; ++s) {
+    const Loops l = loops_of(kind, a, s, block, stage);
+    const int tiles = l.tiles();
+    if (tiles == 0) continue;
+    for (int h = 0; h < a.kv_heads; ++h) {
+      Group g{s, h, 0.0, 0.0, {}};
+      for (int i = 0; i < tiles; ++i) {
+        // Longest loop first: rows from the last tile, keys from the first.
+        const int t = order == T2V_ORDER_NATURAL || kind == kCausalDkdv ? i : tiles - 1 - i;
+        const int len = l.length(t);
+        int count = 1, step = len;
+        pieces_of(kind, len, chunk, &count, &step);
+        CausalItem it{a.cu_q[s], l.lq, a.cu_k[s], l.lk, t * block, h, 0, len, -1, 1, 0, 0};
+        if (count > 1) {
+          CausalItem r = it;
+          r.slot = static_cast<int32_t>(out.slots);
+          r.pieces = count;
+          r.end = 0;
+          out.reduce.push_back(r);
+        }
+        for (int p = 0; p < count; ++p) {
+          it.begin = p * step;
+          it.end = std::min(len, (p + 1) * step);
+          if (count > 1) {
+            it.slot = static_cast<int32_t>(out.slots++);
+            it.pieces = count;
+          }
+          g.items.push_back(it);
+          const double c = fixed + (it.end - it.begin);
+          g.cost += c;
+          g.longest = std::max(g.longest, c);
+        }
+      }
+      n += g.items.size();
+      groups.push_back(std::move(g));
+    }
+  }
+  out.items.reserve(n);
+  if (order == T2V_ORDER_NATURAL) {
+    for (const Group& g : groups) out.items.insert(out.items.end(), g.items.begin(), g.items.end());
+    return out;
+  }
+  // Workgroup b runs on die b % 8. A (sequence, key head) goes to one die, whose L2 then serves its keys
+  // or queries to all its tiles, longest tiles first; groups by their longest loop, each to the
+  // least loaded die, and on to the next when that die has an even share of the cost.
+  std::stable_sort(groups.begin(), groups.end(), [](const Group& x, const Group& y) { return x.longest > y.longest; });
+  double total = 0.0;
+  for (const Group& g : groups) total += g.cost;
+  const double share = total / kNumXcd * (1.0 + 1e-9);
+  std::vector<std::vector<CausalItem>> q(kNumXcd);
+  std::vector<double> load(kNumXcd, 0.0);
+  for (const Group& g : groups) {
+    int x = static_cast<int>(std::min_element(load.begin(), load.end()) - load.begin());
+    for (const CausalItem& it : g.items) {
+      const double c = fixed + (it.end - it.begin);
+      if (load[x] + 0.5 * c > share) x = static_cast<int>(std::min_element(load.begin(), load.end()) - load.begin());
+      q[x].push_back(it);
+      load[x] += c;
+    }
+  }
+  // One list: position b takes the next item of die b % 8, or, when that die has no more, the last
+  // (shortest) item of the die with the most left, so that no position is empty.
+  std::vector<size_t> next(kNumXcd, 0);
+  for (size_t b = 0; b < n; ++b) {
+    const size_t x = b % kNumXcd;
+    if (next[x] < q[x].size()) {
+      out.items.push_back(q[x][next[x]++]);
+      continue;
+    }
+    size_t most = 0;
+    for (size_t y = 1; y < kNumXcd; ++y)
+      if (q[y].size() - next[y] > q[most].size() - next[most]) most = y;
+    out.items.push_back(q[most].back());
+    q[most].pop_back();
+  }
+  return out;
+}
+
+int causal_chunk(CausalKernel kind, const CausalShape& a, int block, int stage, double fixed, int workers, int least,
+                 int64_t max_slots) {
+  double total = 0.0, longest = 0.0;
+  for (int s = 0; s < a.nseq; ++s) {
+    const Loops l = loops_of(kind, a, s, block, stage);
+    for (int t = 0; t < l.tiles(); ++t) total += (fixed + l.length(t)) * a.kv_heads;
+    longest = std::max(longest, static_cast<double>(l.longest()));
+  }
+  const double share = total / std::max(workers, 1);
+  if (longest + fixed <= share || longest <= least) return 0;
+  for (int64_t chunk = std::max<int64_t>(least, static_cast<int64_t>(std::ceil(0.5 * share)));
+       static_cast<double>(chunk) < longest; chunk *= 2) {
+    int64_t slots = 0;
+    for (int s = 0; s < a.nseq; ++s) {
+      const Loops l = loops_of(kind, a, s, block, stage);
+      for (int t = 0; t < l.tiles(); ++t) {
+        int count = 1, step = 0;
+        pieces_of(kind, l.length(t), static_cast<int>(chunk), &count, &step);
+        slots += count > 1 ? static_cast<int64_t>(count) * a.kv_heads : 0;
+      }
+    }
+    if (slots <= max_slots) return slots == 0 ? 0 : static_cast<int>(chunk);
+  }
+  return 0;
+}
+
+double causal_makespan(const CausalList& l, double fixed, int workers) {
+  double span = 0.0;
+  const size_t dies = workers % kNumXcd == 0 && workers >= kNumXcd ? kNumXcd : 1;
+  for (size_t x = 0; x < dies; ++x) {
+    std::priority_queue<double, std::vector<double>, std::greater<double>> free_at;
+    for (int i = 0; i < std::max<int>(1, workers / static_cast<int>(dies)); ++i) free_at.push(0.0);
+    for (size_t i = x; i < l.items.size(); i += dies) {
+      const double end = free_at.top() + fixed + (l.items[i].end - l.items[i].begin);
+      free_at.pop();
+      free_at.push(end);
+      span = std::max(span, end);
+    }
+  }
+  return span;
+}
+
+std::string check_causal_items(CausalKernel kind, const CausalItem* items, int n, const CausalShape& a, int block,
+                               int stage, int64_t max_slots, bool reduce) {
+  for (int i = 0; i < n; ++i) {
+    const CausalItem& it = items[i];
+    auto bad = [&](const char* what) {
+      return "item " + std::to_string(i) + " {qrow0 " + std::to_string(it.qrow0) + ", lq " + std::to_string(it.lq) +
+             ", krow0 " + std::to_string(it.krow0) + ", lk " + std::to_string(it.lk) + ", tile0 " +
+             std::to_string(it.tile0) + ", head " + std::to_string(it.head) + ", begin " + std::to_string(it.begin) +
+             ", end " + std::to_string(it.end) + ", slot " + std::to_string(it.slot) + ", pieces " +
+             std::to_string(it.pieces) + "}: " + what;
+    };
+    int s = 0;
+    while (s < a.nseq && !(a.cu_q[s] == it.qrow0 && a.cu_q[s + 1] - a.cu_q[s] == it.lq && a.cu_k[s] == it.krow0 &&
+                           a.cu_k[s + 1] - a.cu_k[s] == it.lk))
+      ++s;
+    if (s == a.nseq) return bad("its rows and keys are no sequence's");
+    const Loops l = loops_of(kind, a, s, block, stage);
+    if (it.tile0 < 0 || it.tile0 % block != 0 || it.tile0 / block >= l.tiles()) return bad("tile0 is outside");
+    if (it.head < 0 || it.head >= a.kv_heads) return bad("head is out of range");
+    if (reduce ? it.slot < 0 || it.pieces < 2 || it.slot + static_cast<int64_t>(it.pieces) > max_slots
+               : it.slot < -1 || it.slot >= max_slots || (it.slot < 0) != (it.pieces == 1))
+      return bad("partial slots are out of range");
+    const int len = l.length(it.tile0 / block);
+    if (!reduce && (it.begin < 0 || it.end < it.begin || it.end > len || (it.begin == it.end && len > 0)))
+      return bad("the loop leaves the rows that the tile sees");
+    if (!reduce && it.slot < 0 && (it.begin != 0 || it.end != len)) return bad("an uncut loop must be whole");
+  }
+  return std::string();
+}
+
+}  // namespace t2v

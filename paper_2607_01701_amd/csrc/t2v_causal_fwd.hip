@@ -1,0 +1,301 @@
+// Forward kernel of causal attention with grouped heads.
+//
+// A workgroup owns a tile of packed rows (query, head of the group) of one (sequence, key head):
+// 8 waves and 256 rows, or 4 waves and 128; a wave owns 32 rows, one per lane pair. It loops over the
+// keys that the tile's last row sees, staged through LDS 64 at a time and shared by all heads
+// of the group. Scores are computed transposed (S^T = K Q^T), the softmax runs online over 32-key
+// steps with a lazily moved reference maximum (it moves when a step exceeds it by 2^kTau). A wave skips
+// steps that none of its rows sees and masks those that only some see: two at most, besides a
+// sequence's first rows. A cut loop leaves the unnormalised sums, the reference and the sum of each row in its
+// slot; the join weighs and adds the pieces in order.
+#include "t2v_causal_device.hpp"
+
+namespace t2v {
+
+using namespace kern;
+
+namespace {
+
+constexpr int kBN = 64;  // keys per LDS stage
+constexpr int kThreadsWide = 512, kThreadsNarrow = 256;
+
+T2V_DEV float sum16(const f32x16& x) {
+  float a[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) a[i] = x[i] + x[i + 8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) a[i] += a[i + 4];
+  return (a[0] + a[2]) + (a[1] + a[3]);
+}
+
+T2V_DEV float max16(const f32x16& x) {
+  float a[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) a[i] = max_nan(x[i], x[i + 8]);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) a[i] = max_nan(a[i], a[i + 4]);
+  return max_nan(max_nan(a[0], a[2]), max_nan(a[1], a[3]));
+}
+
+// One 32-key step. MASK: this lane's row sees keys 0 .. lim of the step. c > 0.
+template <int D, bool MASK>
+T2V_DEV void fwd_step(uint32_t kbase, uint32_t vbase0, uint32_t vbase1, int kb, int lim, float c,
+                      const bf16x8 (&qop)[D / 16], f32x16 (&o)[D / 32], float& m_run, float& l_run, int lane) {
+  __builtin_amdgcn_iglp_opt(0);
+  constexpr int KK = D / 16;
+  constexpr int DB = D / 32;
+  const int G = lane >> 5;
+  // S^T (32 keys x 32 rows): lane = row, register r = key 8 (r / 4) + 4 G + r % 4.
+  bf16x8 ka[KK];
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) ka[kk] = read_opnd<D>(kbase, kb, kk);
+  f32x16 s = zero16();
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) s = mfma(ka[kk], qop[kk], s);
+  bf16x8 va[2][DB];
+#pragma unroll
+  for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+    for (int db = 0; db < DB; ++db) va[hf][db] = read_rows_opnd<D>(vbase0, vbase1, kb + hf * 16, db);
+  if constexpr (MASK) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = (r >> 2) * 8 + G * 4 + (r & 3) <= lim ? s[r] : -kInf;
+  }
+  const float mblk = half_max(max16(s)) * c;  // largest scaled score of this step
+  if (__any(mblk > m_run + kTau)) {
+    // Each row by itself, so that no row's rounding depends on its neighbours in the tile.
+    const float mn = mblk > m_run + kTau ? mblk : m_run;
+    // A row that has seen no key (or only scores of -inf) keeps a reference of -inf: its sums are zero.
+    const float alpha = __builtin_amdgcn_exp2f(m_run - (mn == -kInf ? 0.0f : mn));
+    l_run *= alpha;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) o[db] *= alpha;
+    m_run = mn;
+  }
+  const float nm = m_run == -kInf ? 0.0f : -m_run;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, nm));  // a masked score gives 0
+  l_run += sum16(s);
+  // P in bf16 for its product (at most 2^-9 of each weight); the row sum above took it in 32 bits.
+  const bf16x8 pb[2] = {to_bf16x8(s, 0), to_bf16x8(s, 8)};
+  const bool odd = MASK && take_nonfinite(va);
+#pragma unroll
+  for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+    for (int db = 0; db < DB; ++db) o[db] = mfma(va[hf][db], pb[hf], o[db]);
+  if constexpr (MASK) {
+    if (odd)
+      add_nonfinite<true>(o, pb, G, [&](int half, int db) { return read_rows_opnd<D>(vbase0, vbase1, kb + half, db); },
+                          [&](int kk, int) { return kk <= lim; });
+  }
+}
+
+template <int D, int NT>
+__global__ __launch_bounds__(NT, 512 / NT) void causal_fwd_kernel(
+    const bf16* __restrict__ q, const bf16* __restrict__ k, const bf16* __restrict__ v, int64_t qs, int64_t ks,
+    int64_t vs, const CausalItem* __restrict__ items, int H, int g, int64_t T, float c, unsigned qkeep, unsigned qflip,
+    bf16* __restrict__ out, float* __restrict__ lse, float* __restrict__ partial,
+    unsigned long long* __restrict__ trace) {
+  constexpr int KK = D / 16;
+  constexpr int DB = D / 32;
+  constexpr int R = NT / 2;  // rows of the tile
+  __shared__ __attribute__((aligned(1024))) bf16 sK[2][kBN * D];
+  __shared__ __attribute__((aligned(1024))) bf16 sV[2][kBN * D];
+  const unsigned long long trace_t0 = trace != nullptr ? trace_clock() : 0ull;
+  const CausalItem it = items[blockIdx.x];
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = lane >> 5;
+  const bool wave_active = it.tile0 + wave * 32 < it.lq * g;
+  const LaneRow me = lane_row(it, g, wave, lane);
+  const int lim = me.lim, lim_lo = __builtin_amdgcn_readlane(lim, 0), lim_hi = __builtin_amdgcn_readlane(lim, 31);
+
+  f32x16 o[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) o[db] = zero16();
+  float m_run = -kInf, l_run = 0.0f;
+
+  const int ntiles = (it.end - it.begin + kBN - 1) / kBN;
+  if (ntiles > 0) {
+    const bf16* kh = k + it.krow0 * ks + static_cast<int64_t>(it.head) * D;
+    const bf16* vh = v + it.krow0 * vs + static_cast<int64_t>(it.head) * D;
+    const TileDma<D, kBN, NT> kdma(tid, ks), vdma(tid, vs);
+    kdma.copy(sK[0], kh, ks, it.begin, it.lk);
+    vdma.copy(sV[0], vh, vs, it.begin, it.lk);
+    // A negative scale turns the sign of Q (so that the largest scaled score is that of the largest
+    // product), a scale of 0 clears it.
+    bf16x8 qop[KK];
+    const bf16* qp = q + me.token * qs + static_cast<int64_t>(me.head) * D;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      u32x4 w = load_raw16(qp + kk * 16 + G * 8, me.ok);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = (w[e] & qkeep) ^ qflip;
+      qop[kk] = __builtin_bit_cast(bf16x8, w);
+    }
+    const uint32_t ko = opnd_lane_off<D>(lane);
+    const uint32_t vo0 = rows_lane_off<D>(lane, 0), vo1 = rows_lane_off<D>(lane, 1);
+    wait_vmcnt0();
+    __syncthreads();
+    auto prefetch = [&](int tt) {
+      if (tt + 1 < ntiles) {
+        kdma.copy(sK[(tt & 1) ^ 1], kh, ks, it.begin + (tt + 1) * kBN, it.lk);
+        vdma.copy(sV[(tt & 1) ^ 1], vh, vs, it.begin + (tt + 1) * kBN, it.lk);
+      }
+    };
+    // Stages that all rows of this wave see whole, then the others: every wave passes ntiles barriers.
+    const int nfull = wave_active ? min(max(lim_lo + 1 - it.begin, 0) / kBN, ntiles) : 0;
+    int tt = 0;
+    for (; tt < nfull; ++tt) {
+      const int b = tt & 1;
+      prefetch(tt);
+      const uint32_t kbase = lds_addr(sK[b]) + ko;
+      const uint32_t vb0 = lds_addr(sV[b]) + vo0, vb1 = lds_addr(sV[b]) + vo1;
+#pragma unroll
+      for (int kb = 0; kb < kBN; kb += 32)
+        fwd_step<D, false>(kbase, vb0, vb1, kb, 0, c, qop, o, m_run, l_run, lane);
+      wait_vmcnt0();
+      __syncthreads();
+    }
+    for (; tt < ntiles; ++tt) {
+      const int b = tt & 1;
+      const int key0 = it.begin + tt * kBN;
+      prefetch(tt);
+      if (wave_active) {
+        const uint32_t kbase = lds_addr(sK[b]) + ko;
+        const uint32_t vb0 = lds_addr(sV[b]) + vo0, vb1 = lds_addr(sV[b]) + vo1;
+#pragma unroll 1
+        for (int kb = 0; kb < kBN && key0 + kb <= lim_hi; kb += 32)
+          fwd_step<D, true>(kbase, vb0, vb1, kb, lim - key0 - kb, c, qop, o, m_run, l_run, lane);
+      }
+      wait_vmcnt0();
+      __syncthreads();
+    }
+  }
+
+  if (wave_active) {
+    // Worked out again, rather than kept in registers through the loop.
+    const int lane = lane_again(), G = lane >> 5, l32 = lane & 31;
+    const LaneRow me = lane_row(it, g, wave, lane);
+    const float lt = half_sum(l_run);
+    if (it.slot >= 0) {  // one piece: unnormalised sums, reference and sum of each row
+      float* po = partial + static_cast<int64_t>(it.slot) * (R * (D + 2));
+      float* pm = po + R * D;
+      const int r = wave * 32 + l32;
+      if (me.ok) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            f32x4 w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = o[db][i * 4 + e];
+            *reinterpret_cast<f32x4*>(po + r * D + db * 32 + i * 8 + G * 4) = w;
+          }
+        if (G == 0) {
+          pm[2 * r] = m_run;
+          pm[2 * r + 1] = lt;
+        }
+      }
+    } else {
+      // A row that sees no key has no softmax: its output is 0 and its lse -inf.
+      const float inv = me.lim < 0 ? 0.0f : 1.0f / lt;
+      bf16* op = out + (me.token * H + me.head) * D;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) store_rows(op + db * 32, o[db], inv, G, me.ok);
+      if (me.ok && G == 0)
+        lse[static_cast<int64_t>(me.head) * T + me.token] = (m_run + __builtin_amdgcn_logf(lt)) * kLn2;
+    }
+  }
+  if (trace != nullptr) trace_end(trace, trace_t0, 0, blockIdx.x);
+}
+
+// Joins the pieces of the cut tiles: with the largest reference m of a row, out = sum_p 2^(m_p - m) O_p / l,
+// l = sum_p 2^(m_p - m) l_p, in piece order. D / 8 lanes hold a row, eight columns each.
+template <int D>
+__global__ __launch_bounds__(kThreads) void causal_fwd_join_kernel(const float* __restrict__ partial,
+                                                                    const CausalItem* __restrict__ tiles, int R, int H,
+                                                                    int g, int64_t T, bf16* __restrict__ out,
+                                                                    float* __restrict__ lse) {
+  constexpr int LPR = D / 8, RPB = kThreads / LPR;
+  const int blocks = R / RPB;
+  const CausalItem it = tiles[blockIdx.x / blocks];
+  const int r = (blockIdx.x % blocks) * RPB + threadIdx.x / LPR;  // row of the tile
+  const int col = threadIdx.x % LPR * 8;
+  const int row = it.tile0 + r;
+  if (row >= it.lq * g) return;
+  const PackedRow pr = packed_row(row, g);
+  const int64_t slot = static_cast<int64_t>(R) * (D + 2);
+  const float* po = partial + it.slot * slot;
+  const float* pm = po + R * D + 2 * r;
+  po += r * D + col;
+  float m = -kInf;
+  for (int p = 0; p < it.pieces; ++p) m = max_nan(m, pm[p * slot]);
+  const float ref = m == -kInf ? 0.0f : m;
+  float l = 0.0f;
+  f32x4 a = {0.0f, 0.0f, 0.0f, 0.0f}, b = a;
+  for (int p = 0; p < it.pieces; ++p) {
+    const float w = __builtin_amdgcn_exp2f(pm[p * slot] - ref);
+    l = fmaf(w, pm[p * slot + 1], l);
+    const f32x4 x = *reinterpret_cast<const f32x4*>(po + p * slot), y = *reinterpret_cast<const f32x4*>(po + p * slot + 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      a[e] = fmaf(w, x[e], a[e]);
+      b[e] = fmaf(w, y[e], b[e]);
+    }
+  }
+  const float inv = pr.query + it.lk - it.lq < 0 ? 0.0f : 1.0f / l;
+  const int64_t token = static_cast<int64_t>(it.qrow0) + pr.query;
+  const int head = it.head * g + pr.head;
+  bf16x8 w;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    w[e] = static_cast<bf16>(a[e] * inv);
+    w[4 + e] = static_cast<bf16>(b[e] * inv);
+  }
+  *reinterpret_cast<bf16x8*>(out + (token * H + head) * D + col) = w;
+  if (col == 0) lse[static_cast<int64_t>(head) * T + token] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+template <int D, int NT>
+void launch_as(const CausalArgs& a, const CausalItem* items, int n, hipStream_t s) {
+  const float c = a.scale == 0.0f ? 1.0f : fabsf(a.scale) * kLog2e;
+  const unsigned keep = a.scale == 0.0f ? 0u : ~0u, flip = a.scale < 0.0f ? 0x80008000u : 0u;
+  hipLaunchKernelGGL((causal_fwd_kernel<D, NT>), dim3(n), dim3(NT), 0, s, static_cast<const bf16*>(a.q),
+                     static_cast<const bf16*>(a.k), static_cast<const bf16*>(a.v), a.q_stride, a.k_stride, a.v_stride,
+                     items, a.heads, a.heads / a.kv_heads, a.tq, c, keep, flip, static_cast<bf16*>(a.out), a.lse,
+                     a.partial, a.trace);
+}
+
+}  // namespace
+
+int causal_fwd_rows(bool narrow) { return (narrow ? kThreadsNarrow : kThreadsWide) / 2; }
+int64_t causal_fwd_slot_bytes(int rows, int head_dim) { return static_cast<int64_t>(rows) * (head_dim + 2) * 4; }
+
+hipError_t launch_causal_fwd(const CausalArgs& a, int rows, const CausalItem* items, int n, hipStream_t s) {
+  const bool narrow = rows == causal_fwd_rows(true);
+  if (a.head_dim == 128)
+    narrow ? launch_as<128, kThreadsNarrow>(a, items, n, s) : launch_as<128, kThreadsWide>(a, items, n, s);
+  else
+    narrow ? launch_as<64, kThreadsNarrow>(a, items, n, s) : launch_as<64, kThreadsWide>(a, items, n, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_causal_fwd_join(const CausalArgs& a, int rows, const CausalItem* tiles, int n, hipStream_t s) {
+  const int per = rows / (kThreads / (a.head_dim / 8));
+  auto* o = static_cast<bf16*>(a.out);
+  const int g = a.heads / a.kv_heads;
+  if (a.head_dim == 128)
+    hipLaunchKernelGGL((causal_fwd_join_kernel<128>), dim3(n * per), dim3(kThreads), 0, s, a.partial, tiles, rows,
+                       a.heads, g, a.tq, o, a.lse);
+  else
+    hipLaunchKernelGGL((causal_fwd_join_kernel<64>), dim3(n * per), dim3(kThreads), 0, s, a.partial, tiles, rows,
+                       a.heads, g, a.tq, o, a.lse);
+  return hipGetLastError();
+}
+
+#if T2V_CHECKED
+hipError_t causal_fwd_check_take(unsigned int* rec, unsigned int canary) { return kern::check_take_here(rec, canary); }
+#endif
+}  // namespace t2v

@@ -1,0 +1,145 @@
+"""Rotary positions for q and k (t2v_rotary): frequencies, the call, and its autograd wrapper. The
+binding marshals arguments; the computation is in the HIP library."""
+from __future__ import annotations
+
+import ctypes
+import math
+
+import numpy as np
+
+from . import _lib
+
+LAYOUTS = {"half": 0, "interleaved": 1}
+SCALINGS = (None, "linear", "ntk", "yarn")
+
+
+def rotary_frequencies(sections, theta: float = 10000.0, scaling=None, factor: float = 1.0, trained=None,
+                       slow: float = 1.0, fast: float = 32.0):
+    """Frequencies (float64, radians a position) and the factor on the turned dimensions, for rotary().
+
+    sections: pairs of dimensions turned (an int), or pairs for each axis of the positions (up to three, e.g.
+    frame, row and column of a latent patch). Pair j of n turns by theta^(-j / n) a position. To reach
+    ``factor`` times the ``trained`` positions:
+      "linear"  positions shrink by the factor;
+      "ntk"     theta grows by factor^(n / (n - 1)), so that the slowest pair shrinks by the factor and the
+                fastest not at all;
+      "yarn"    pairs that turn at least ``fast`` times over the trained positions stay, those that turn at
+                most ``slow`` times shrink by the factor, with a ramp between, and the turned dimensions
+                are multiplied by 0.1 ln(factor) + 1 (Peng et al. 2023, arXiv:2309.00071)."""
+    sections = (sections,) if isinstance(sections, int) else tuple(sections)
+    if not 1 <= len(sections) <= 3 or any(n < 0 for n in sections) or sum(sections) < 1:
+        raise ValueError(f"sections must be one to three counts of pairs, got {sections}")
+    if scaling not in SCALINGS:
+        raise ValueError(f"scaling must be one of {SCALINGS}, got {scaling!r}")
+    if not (math.isfinite(theta) and theta > 0 and math.isfinite(factor) and factor > 0):
+        raise ValueError("theta and factor must be positive")
+    if scaling == "yarn" and (trained is None or not trained > 0 or not 0 < slow < fast):
+        raise ValueError("yarn needs the trained positions and 0 < slow < fast")
+    freqs = []
+    for n in sections:
+        base = theta * factor ** (n / (n - 1)) if scaling == "ntk" and n > 1 else theta
+        f = base ** -(np.arange(n, dtype=np.float64) / max(n, 1))
+        if scaling == "linear":
+            f = f / factor
+        elif scaling == "yarn":
+            keep = np.clip((trained * f / (2 * np.pi) - slow) / (fast - slow), 0.0, 1.0)
+            f = f * keep + f / factor * (1.0 - keep)
+        freqs.append(f)
+    return np.concatenate(freqs), 0.1 * math.log(factor) + 1.0 if scaling == "yarn" and factor > 1.0 else 1.0
+
+
+def rotary_apply(q, k, positions, freqs, layout: str = "half", sections=None, mscale: float = 1.0,
+                 inverse: bool = False, q_out=None, k_out=None, stream=None):
+    """q [T, H, D] and k [T, Hk, D] (either may be None) turned by their positions: bf16 on the GPU, tokens any
+    distance apart (slices of a fused projection), D 64 or 128. positions: int32 on the GPU, [T], or [axes, T]
+    with ``sections`` counting the pairs of each axis. The first 2 len(freqs) dimensions turn, in pairs
+    (j, j + len(freqs)) ("half") or (2 j, 2 j + 1) ("interleaved"), and are multiplied by mscale; the others are
+    copied. inverse turns back by the same angles (the gradient). Returns contiguous (q, k)."""
+    import torch
+    first = q if q is not None else k
+    if first is None:
+        raise ValueError("q and k are both None")
+    if first.dim() != 3:
+        raise ValueError("q and k must be [tokens, heads, head_dim]")
+    if layout not in LAYOUTS:
+        raise ValueError(f"layout must be one of {tuple(LAYOUTS)}, got {layout!r}")
+    T, _, D = first.shape
+    f = np.ascontiguousarray(freqs, dtype=np.float64)
+    if f.ndim != 1:
+        raise ValueError("freqs must be a 1-D array, one frequency a pair")
+    sec = (ctypes.c_int32 * 3)(*((f.shape[0],) if sections is None else sections))
+    n_sec = 1 if sections is None else len(sections)
+    if sum(sec) != f.shape[0]:
+        raise ValueError(f"sections {tuple(sections)} do not sum to the {f.shape[0]} frequencies")
+    if tuple(positions.shape) not in ((T,), (1, T)) if n_sec == 1 else tuple(positions.shape) != (n_sec, T):
+        raise ValueError(f"positions has shape {tuple(positions.shape)}, expected {(n_sec, T)}")
+    if positions.dtype != torch.int32 or not positions.is_contiguous():
+        raise ValueError("positions must be contiguous int32")
+    named, ptrs, strides, heads, outs = [("positions", positions)], [], [], [], []
+    for x, o, name in ((q, q_out, "q"), (k, k_out, "k")):
+        if x is None:
+            ptrs.append((None, None))
+            strides.append(0)
+            heads.append(0)
+            outs.append(None)
+            continue
+        shape = (T, x.shape[1], D)
+        strides.append(_lib._check_rows(x, name, shape))
+        if o is None:
+            with _lib._on(stream):
+                o = torch.empty(shape, dtype=x.dtype, device=x.device)
+        _lib._check_tensor(o, name + "_out", shape)
+        named += [(name, x), (name + "_out", o)]
+        ptrs.append((x.data_ptr(), o.data_ptr()))
+        heads.append(shape[1])
+        outs.append(o)
+    _lib._check_on_device(named)
+    L = _lib.lib()
+    with _lib._on_device(first):
+        st = L.t2v_rotary(ptrs[0][0], ptrs[1][0], strides[0], strides[1], positions.data_ptr(), T, heads[0], heads[1], D,
+                          f.ctypes.data, sec, n_sec, LAYOUTS[layout], float(mscale), 1 if inverse else 0, ptrs[0][1],
+                          ptrs[1][1], _lib._stream_handle(stream))
+    _lib._check(L, st)
+    return tuple(outs)
+
+
+def _function():
+    import torch
+
+    class _Rotary(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, k, positions, freqs, layout, sections, mscale):
+            ctx.save_for_backward(positions)
+            ctx.args = (freqs, layout, sections, mscale)
+            ctx.set_materialize_grads(False)
+            return rotary_apply(q, k, positions, freqs, layout, sections, mscale)
+
+        @staticmethod
+        def backward(ctx, dq, dk):
+            if dq is None and dk is None:
+                return (None,) * 7
+            (positions,) = ctx.saved_tensors
+            # R(angle) transposed is R(-angle).
+            dq, dk = (x if x is None or _rows(x) else x.contiguous() for x in (dq, dk))
+            return (*rotary_apply(dq, dk, positions, *ctx.args, inverse=True), None, None, None, None, None)
+
+    return _Rotary
+
+
+def _rows(t) -> bool:
+    """Whether the call takes t as it is: each token's heads contiguous, tokens at least a token apart."""
+    T, H, D = t.shape
+    return t.is_contiguous() or (t.stride(2) == 1 and t.stride(1) == D and H * D <= t.stride(0) <= 1 << 22
+                                 and t.stride(0) % 8 == 0 and t.data_ptr() % 16 == 0)
+
+
+_FN = None
+
+
+def rotary(q, k, positions, freqs, layout: str = "half", sections=None, mscale: float = 1.0):
+    """rotary_apply with autograd: gradients flow to q and k (k may be None)."""
+    global _FN
+    if _FN is None:
+        _FN = _function()
+    f = np.array(freqs, dtype=np.float64, copy=True)
+    return _FN.apply(q, k, positions, f, layout, None if sections is None else tuple(sections), float(mscale))
