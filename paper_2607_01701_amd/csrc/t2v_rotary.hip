@@ -2,9 +2,11 @@
 // first rot_dim dimensions, p the token's position on the pair's axis; the other dimensions are copied. The
 // backward pass is the same call with the angles' sign turned.
 //
-// Bound by memory: every element is read once and written once, 16 bytes a lane. A workgroup
-// takes tokens one after another; the sine and cosine of a pair are worked out once a token and shared by
-// all heads through LDS.
+// Bound by memory: every element is read once and written once. Work is cut into units of 16
+// elements, two 16-byte vectors: eight pairs, or 16 dimensions that are copied. A lane has four units in flight
+// and loads them before the sines and cosines, which are worked out once a token and shared by
+// all heads through LDS. Counts of pairs that are no multiple of 8 take the same path: the last unit is moved
+// back to overlap the one before (it writes the same values again), and vectors need not be aligned.
 //
 // Angles. A frequency is held as a 64-bit fraction of a turn, F = f / 2 pi mod 1 in units of 2^-64, so that
 // position * F modulo 2^64 is the angle's fraction of a turn, exact to position * 2^-65 turns at any int32
@@ -22,7 +24,9 @@ namespace t2v {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kUnits = 4;  // in flight per lane
 constexpr int kMaxPairs = 64;
+constexpr int kMaxAngles = 2048;  // of a workgroup (16 KB of LDS: eight workgroups on a CU)
 constexpr int kMaxAxes = 3;
 
 struct RotaryArgs {
@@ -39,14 +43,83 @@ struct RotaryArgs {
   unsigned char axis[kMaxPairs];
 };
 
-// A workgroup's tokens: kTokens of them, their sines and cosines in LDS.
-template <int D, bool INTERLEAVED, bool ALIGNED>
+// Eight bf16 at any 2-byte address (a global access of 16 bytes needs no alignment).
+typedef u32x4 __attribute__((aligned(2))) u32x4_any;
+T2V_DEV bf16x8 load_any(const bf16* p) { return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4_any*>(p)); }
+T2V_DEV void store_any(bf16* p, const bf16x8& x) { *reinterpret_cast<u32x4_any*>(p) = __builtin_bit_cast(u32x4, x); }
+
+// Where a lane is: unit `u` of head `h` (q's heads, then k's) of the workgroup's token `t`.
+struct Place {
+  int t, h, u;
+};
+
+template <int D, bool INTERLEAVED>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, int tokens_per_block) {
-  constexpr int C = D / 8;  // 16-byte chunks of a head
-  __shared__ float2 cs[64 * kMaxPairs];
+  __shared__ __attribute__((aligned(16))) float2 cs[kMaxAngles];
   const int64_t t0 = static_cast<int64_t>(blockIdx.x) * tokens_per_block;
   const int nt = static_cast<int>(min(static_cast<int64_t>(tokens_per_block), a.tokens - t0));
   const int pairs = a.rot_dim / 2;
+  const int turned = (pairs + 7) / 8, units = turned + (D - a.rot_dim + 15) / 16;  // of a head
+  const int heads = a.heads[0] + a.heads[1];
+  const int total = nt * heads * units;
+  // A lane's units are kThreads apart: its place moves by (st, sh, su), with carries.
+  const int su = kThreads % units, sr = kThreads / units, st = sr / heads, sh = sr - st * heads;
+  Place w;
+  {
+    const int e = threadIdx.x, r = e / units;
+    w.u = e - r * units;
+    w.t = r / heads;
+    w.h = r - w.t * heads;
+  }
+  auto advance = [&](Place& x) {
+    x.u += su;
+    int c = x.u >= units;
+    x.u -= c ? units : 0;
+    x.h += sh + c;
+    c = x.h >= heads;
+    x.h -= c ? heads : 0;
+    x.t += st + c;
+  };
+  // First elements of the unit's two vectors within the head, and its first pair (-1: copied).
+  struct Vectors {
+    int first, second, pair;
+  };
+  auto vectors = [&](int u) -> Vectors {
+    if (u < turned) {
+      const int j = max(min(8 * u, pairs - 8), 0);
+      return INTERLEAVED ? Vectors{2 * j, 2 * j + 8, j} : Vectors{j, j + pairs, j};
+    }
+    const int d = min(a.rot_dim + 16 * (u - turned), D - 16);
+    return {d, d + 8, -1};
+  };
+  auto source = [&](const Place& x) {
+    const bool k = x.h >= a.heads[0];
+    return (k ? a.in[1] : a.in[0]) + (t0 + x.t) * (k ? a.stride[1] : a.stride[0]) +
+           static_cast<int64_t>(x.h - (k ? a.heads[0] : 0)) * D;
+  };
+  auto target = [&](const Place& x) {
+    const bool k = x.h >= a.heads[0];
+    return (k ? a.out[1] : a.out[0]) +
+           ((t0 + x.t) * (k ? a.heads[1] : a.heads[0]) + (x.h - (k ? a.heads[0] : 0))) * D;
+  };
+  // With fewer than eight pairs, or 1 .. 15 dimensions to copy, those are taken one by one.
+  const bool few_pairs = pairs < 8, few_copied = D - a.rot_dim < 16;
+  auto whole = [&](int u) { return u < turned ? !few_pairs : !few_copied; };
+
+  bf16x8 x[kUnits], y[kUnits];
+  auto load = [&](Place p, int e0) {
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+      if (e0 + i * kThreads < total && whole(p.u)) {
+        const Vectors v = vectors(p.u);
+        const bf16* s = source(p);
+        x[i] = load_any(s + v.first);
+        y[i] = load_any(s + v.second);
+      }
+      advance(p);
+    }
+  };
+  load(w, threadIdx.x);
   for (int e = threadIdx.x; e < nt * pairs; e += kThreads) {
     const int t = e / pairs, j = e - t * pairs;
     const int p = a.positions[a.axis[j] * a.tokens + t0 + t];
@@ -58,52 +131,57 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, in
     cs[e] = make_float2(c * a.mscale, (a.inverse ? -s : s) * a.mscale);
   }
   __syncthreads();
-  const int heads = a.heads[0] + a.heads[1];
-  const int per_token = heads * C;
-  for (int e = threadIdx.x; e < nt * per_token; e += kThreads) {
-    const int t = e / per_token, r = e - t * per_token;
-    const int h = r / C, c = r % C;
-    const int which = h >= a.heads[0];
-    const int hh = which ? h - a.heads[0] : h;
-    const bf16* x = a.in[which] + (t0 + t) * a.stride[which] + static_cast<int64_t>(hh) * D;
-    bf16* y = a.out[which] + ((t0 + t) * a.heads[which] + hh) * D;
-    const bf16x8 v = *reinterpret_cast<const bf16x8*>(x + c * 8);
-    bf16x8 w = v;
-    const float2* row = cs + t * pairs;
-    if constexpr (INTERLEAVED) {
+  for (int e0 = threadIdx.x; e0 < total; e0 += kUnits * kThreads) {
+    if (e0 != static_cast<int>(threadIdx.x)) load(w, e0);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int j = c * 4 + i;
-        if (j < pairs) {
-          const float u0 = static_cast<float>(v[2 * i]), u1 = static_cast<float>(v[2 * i + 1]);
-          const float2 k = row[j];
-          w[2 * i] = static_cast<bf16>(u0 * k.x - u1 * k.y);
-          w[2 * i + 1] = static_cast<bf16>(u0 * k.y + u1 * k.x);
+    for (int i = 0; i < kUnits; ++i) {
+      if (e0 + i * kThreads < total) {
+        bf16* o = target(w);
+        const float2* row = cs + w.t * pairs;
+        if (whole(w.u)) {
+          const Vectors v = vectors(w.u);
+          if (v.pair >= 0) {
+            float u0[8], u1[8];
+#pragma unroll
+            for (int n = 0; n < 8; ++n) {
+              u0[n] = static_cast<float>(INTERLEAVED ? (n < 4 ? x[i][2 * n] : y[i][2 * n - 8]) : x[i][n]);
+              u1[n] = static_cast<float>(INTERLEAVED ? (n < 4 ? x[i][2 * n + 1] : y[i][2 * n - 7]) : y[i][n]);
+            }
+#pragma unroll
+            for (int n = 0; n < 8; ++n) {
+              const float2 k = row[v.pair + n];
+              const bf16 z0 = static_cast<bf16>(u0[n] * k.x - u1[n] * k.y);
+              const bf16 z1 = static_cast<bf16>(u0[n] * k.y + u1[n] * k.x);
+              if constexpr (!INTERLEAVED) {
+                x[i][n] = z0;
+                y[i][n] = z1;
+              } else if (n < 4) {
+                x[i][2 * n] = z0;
+                x[i][2 * n + 1] = z1;
+              } else {
+                y[i][2 * n - 8] = z0;
+                y[i][2 * n - 7] = z1;
+              }
+            }
+          }
+          store_any(o + v.first, x[i]);
+          store_any(o + v.second, y[i]);
+        } else {
+          const bf16* s = source(w);
+          if (w.u < turned) {
+            for (int j = 0; j < pairs; ++j) {
+              const int d0 = INTERLEAVED ? 2 * j : j, d1 = INTERLEAVED ? 2 * j + 1 : j + pairs;
+              const float u0 = static_cast<float>(s[d0]), u1 = static_cast<float>(s[d1]);
+              o[d0] = static_cast<bf16>(u0 * row[j].x - u1 * row[j].y);
+              o[d1] = static_cast<bf16>(u0 * row[j].y + u1 * row[j].x);
+            }
+          } else {
+            for (int d = a.rot_dim; d < D; ++d) o[d] = s[d];
+          }
         }
       }
-    } else if (c * 8 < a.rot_dim) {
-      // The partner of dimension d is d + pairs or d - pairs: another chunk, read through the cache.
-      bf16x8 o = v;
-      if constexpr (ALIGNED) {
-        o = *reinterpret_cast<const bf16x8*>(x + (c * 8 < pairs ? c * 8 + pairs : c * 8 - pairs));
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int d = c * 8 + i;
-          if (d < a.rot_dim) o[i] = x[d < pairs ? d + pairs : d - pairs];
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int d = c * 8 + i;
-        if (d < a.rot_dim) {
-          const float2 k = row[d < pairs ? d : d - pairs];
-          const float u = static_cast<float>(v[i]), p = static_cast<float>(o[i]);
-          w[i] = static_cast<bf16>(u * k.x + (d < pairs ? -p : p) * k.y);
-        }
-      }
+      advance(w);
     }
-    *reinterpret_cast<bf16x8*>(y + c * 8) = w;
   }
 }
 
@@ -118,11 +196,18 @@ unsigned long long turn_of(double f) {
 template <int D>
 void launch(const RotaryArgs& a, bool interleaved, int blocks, int per, hipStream_t s) {
   if (interleaved)
-    hipLaunchKernelGGL((rotary_kernel<D, true, true>), dim3(blocks), dim3(kThreads), 0, s, a, per);
-  else if (a.rot_dim % 16 == 0)
-    hipLaunchKernelGGL((rotary_kernel<D, false, true>), dim3(blocks), dim3(kThreads), 0, s, a, per);
+    hipLaunchKernelGGL((rotary_kernel<D, true>), dim3(blocks), dim3(kThreads), 0, s, a, per);
   else
-    hipLaunchKernelGGL((rotary_kernel<D, false, false>), dim3(blocks), dim3(kThreads), 0, s, a, per);
+    hipLaunchKernelGGL((rotary_kernel<D, false>), dim3(blocks), dim3(kThreads), 0, s, a, per);
+}
+
+// Tokens of a workgroup: as many as give each lane its kUnits units, as long as there are two workgroups a CU
+// (fewer tokens are spread over the CUs), and no more than the table of angles holds.
+int tokens_per_block(const RotaryArgs& a, int head_dim) {
+  const int pairs = a.rot_dim / 2;
+  const int64_t units = static_cast<int64_t>(a.heads[0] + a.heads[1]) * ((pairs + 7) / 8 + (head_dim - a.rot_dim + 15) / 16);
+  const int64_t per = std::min<int64_t>(kUnits * kThreads / units, a.tokens / 512);
+  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(per, kMaxAngles / pairs)));
 }
 
 int rotary_impl(const void* q, const void* k, int64_t q_stride, int64_t k_stride, const int32_t* positions,
@@ -189,7 +274,7 @@ int rotary_impl(const void* q, const void* k, int64_t q_stride, int64_t k_stride
       a.axis[j] = static_cast<unsigned char>(i);
       a.turn[j] = turn_of(freqs[j]);
     }
-  const int per = 1;
+  const int per = tokens_per_block(a, head_dim);
   const int blocks = static_cast<int>((tokens + per - 1) / per);
   const auto s = static_cast<hipStream_t>(stream);
   const bool interleaved = layout == T2V_ROTARY_INTERLEAVED;
