@@ -223,39 +223,67 @@ int64_t causal_slot_bytes(CausalKernel kind, int rows, int head_dim) {
 
 constexpr int64_t kCausalMaxWorkspace = int64_t(1) << 30;
 
-// An item's fixed part (loads of its rows, stores, filling the pipeline) in keys or stages, and the
-// least length of a piece.
-double causal_fixed(CausalKernel kind) { return kind == kCausalDkdv ? 4.0 : 128.0; }
-int causal_least(CausalKernel kind) { return kind == kCausalDkdv ? 16 : 512; }
+enum CausalForm { kFew, kNarrow, kWide };  // of the forward and dQ kernels; dK/dV has one, kWide
+
+// Times measured on MI355X (microseconds; see CausalCost): a key of a forward item 30 ns at head_dim 128 (256 rows, or
+// 128 with a second workgroup beside it) and 31 at 64 (128 rows, three workgroups), of a dQ item 42 and 40, a
+// stage of a dK/dV item 2.1 us at 128 and 5.1 at 64; a narrow tile with the CU to itself takes about half,
+// and the kernel of few rows 9 ns a key. Where each key is read by one tile only (`once`: single tokens) the
+// memory's 5 TB/s bound the loop instead. Loads, stores and filling the pipeline: `fixed`. A join costs a
+// launch, 0.1 us a piece, and the pieces' results are written and read at 4.5 TB/s.
+CausalCost causal_cost(CausalKernel kind, int head_dim, CausalForm form, bool once, int ncu) {
+  CausalCost c{};
+  const bool d64 = head_dim == 64;
+  c.cus = std::max(1, ncu);
+  c.workers = c.cus * (form == kWide ? 1 : form == kFew ? (d64 ? 2 : 1) : d64 ? 3 : 2);
+  c.unit = kind == kCausalDkdv ? (d64 ? 5.1 : 2.1) : kind == kCausalFwd ? (d64 ? 0.031 : 0.030) : (d64 ? 0.040 : 0.042);
+  c.alone = form == kWide ? c.unit : form == kFew ? 0.009 : 0.55 * c.unit;
+  const double fixed = kind == kCausalDkdv ? (d64 ? 6.0 : 10.0) : form == kFew ? 3.0 : 4.0;
+  if (form == kFew) c.unit = c.alone;
+  if (once) c.unit = std::max(c.unit, 4.0 * head_dim * c.workers / 5e6);
+  c.fixed = fixed / c.unit;
+  c.join = 4.0;
+  c.piece = 0.1;
+  c.byte = 2.0 / 4.5e6;
+  c.slot_row = kind == kCausalDkdv ? 8 * head_dim : kind == kCausalFwd ? 4 * (head_dim + 2) : 4 * head_dim;
+  return c;
+}
 
 CausalList causal_plan(const TileRule& r, const CausalShape& a, int head_dim, int order, bool split, int ncu,
                        int* block) {
   const auto kind = static_cast<CausalKernel>(r.kind);
   const int stage = causal_dkdv_stage(head_dim);
-  const double fixed = causal_fixed(kind);
-  auto workers = [&](int rows) {
-    if (kind == kCausalDkdv || rows == r.wide) return ncu;
-    return ncu * (head_dim == 64 ? 3 : 2);
+  int64_t most_rows = 0;
+  for (int s = 0; s < a.nseq; ++s)
+    most_rows = std::max<int64_t>(most_rows, static_cast<int64_t>(a.cu_q[s + 1] - a.cu_q[s]) * a.group);
+  const int least = kind == kCausalDkdv ? 1 : 64;
+  auto rows_of_form = [&](CausalForm f) { return f == kFew ? causal_fwd_few_rows() : f == kNarrow ? r.narrow : r.wide; };
+  auto cost_of = [&](CausalForm f) {
+    return causal_cost(kind, head_dim, f, kind != kCausalDkdv && most_rows <= rows_of_form(f), ncu);
   };
-  auto list = [&](int rows) {
-    int chunk = 0;
-    if (split && ncu > 0)
-      chunk = causal_chunk(kind, a, rows, stage, fixed, workers(rows), causal_least(kind),
-                           std::min<int64_t>(kCausalMaxWorkspace / causal_slot_bytes(kind, rows, head_dim), INT32_MAX));
-    return build_causal_list(kind, a, rows, stage, order, chunk, fixed);
+  auto choose = [&](CausalForm f, double* time) {
+    const int rows = rows_of_form(f);
+    const int64_t slots =
+        split ? std::min<int64_t>(kCausalMaxWorkspace / causal_slot_bytes(kind, rows, head_dim), INT32_MAX) : 0;
+    return causal_chunk(kind, a, rows, stage, cost_of(f), least, slots, time);
   };
-  *block = r.narrow;
-  if (r.forced == 2 || r.wide == r.narrow || (r.forced == 0 && r.narrow_always)) return list(*block);
-  CausalList wide = list(r.wide);
-  if (r.forced == 1) {
-    *block = r.wide;
-    return wide;
+  CausalForm form = kind == kCausalDkdv || r.forced == 1 ? kWide : kNarrow;
+  int chunk = 0;
+  double time = 0.0;
+  if (kind == kCausalFwd && r.forced == 0 && most_rows <= causal_fwd_few_rows()) form = kFew;
+  if (form == kNarrow && r.forced == 0 && !r.narrow_always && most_rows > r.narrow) {
+    chunk = choose(kNarrow, &time);
+    double wide_time = 0.0;
+    const int wide_chunk = choose(kWide, &wide_time);
+    if (wide_time <= 1.04 * time) {  // wide tiles stage a key once for twice the rows
+      form = kWide;
+      chunk = wide_chunk;
+    }
+  } else {
+    chunk = choose(form, &time);
   }
-  CausalList narrow = list(r.narrow);
-  if (causal_makespan(narrow, fixed, workers(r.narrow)) * 1.04 < causal_makespan(wide, fixed, workers(r.wide)))
-    return narrow;
-  *block = r.wide;
-  return wide;
+  *block = rows_of_form(form);
+  return build_causal_list(kind, a, *block, stage, order, chunk, cost_of(form).fixed);
 }
 
 // T2V_LOG=1: one line on stderr per new work list (items, predicted makespan, bound).

@@ -3,8 +3,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <functional>
-#include <queue>
 
 #include "../../include/t2vattn.h"
 #include "t2v_host.h"
@@ -137,46 +135,72 @@ CausalList build_causal_list(CausalKernel kind, const CausalShape& a, int block,
   return out;
 }
 
-int causal_chunk(CausalKernel kind, const CausalShape& a, int block, int stage, double fixed, int workers, int least,
-                 int64_t max_slots) {
-  double total = 0.0, longest = 0.0;
+namespace {
+
+// Time of the list cut at `chunk`. With a worker for every item: the longest's. Else the even share of all
+// items, and of the longest what a part-empty last round costs: half of it with a round or two, less the more
+// rounds there are (the longest go first). And the join, which goes over a row's pieces in turn.
+// Infinite when it would need more than max_slots slots.
+double causal_time(CausalKernel kind, const CausalShape& a, int block, int stage, const CausalCost& cost, int chunk,
+                   int64_t max_slots, int64_t* items, double* longest) {
+  double total = 0.0, bytes = 0.0;
+  int64_t n = 0, slots = 0;
+  int most = 0, deep = 1;
   for (int s = 0; s < a.nseq; ++s) {
     const Loops l = loops_of(kind, a, s, block, stage);
-    for (int t = 0; t < l.tiles(); ++t) total += (fixed + l.length(t)) * a.kv_heads;
-    longest = std::max(longest, static_cast<double>(l.longest()));
-  }
-  const double share = total / std::max(workers, 1);
-  if (longest + fixed <= share || longest <= least) return 0;
-  for (int64_t chunk = std::max<int64_t>(least, static_cast<int64_t>(std::ceil(0.5 * share)));
-       static_cast<double>(chunk) < longest; chunk *= 2) {
-    int64_t slots = 0;
-    for (int s = 0; s < a.nseq; ++s) {
-      const Loops l = loops_of(kind, a, s, block, stage);
-      for (int t = 0; t < l.tiles(); ++t) {
-        int count = 1, step = 0;
-        pieces_of(kind, l.length(t), static_cast<int>(chunk), &count, &step);
-        slots += count > 1 ? static_cast<int64_t>(count) * a.kv_heads : 0;
+    const int tiles = l.tiles();
+    const int64_t rows = kind == kCausalDkdv ? l.lk : static_cast<int64_t>(l.lq) * l.group;
+    for (int t = 0; t < tiles; ++t) {
+      int count = 1, step = 0;
+      const int len = l.length(t);
+      pieces_of(kind, len, chunk, &count, &step);
+      total += len + count * cost.fixed;
+      n += count;
+      most = std::max(most, step);
+      deep = std::max(deep, count);
+      if (count > 1) {
+        slots += count;
+        bytes += static_cast<double>(count) * std::min<int64_t>(block, rows - static_cast<int64_t>(t) * block) * cost.slot_row;
       }
     }
-    if (slots <= max_slots) return slots == 0 ? 0 : static_cast<int>(chunk);
   }
-  return 0;
+  n *= a.kv_heads;
+  slots *= a.kv_heads;
+  if (items != nullptr) *items = n;
+  if (longest != nullptr) *longest = most;
+  if (slots > max_slots) return HUGE_VAL;
+  // An item's speed follows from how many share its CU.
+  const double per_cu = static_cast<double>(cost.workers) / cost.cus;
+  const double beside = std::min(per_cu, std::ceil(static_cast<double>(n) / cost.cus));
+  const double unit = beside < per_cu ? cost.alone + (cost.unit - cost.alone) * (beside - 1.0) / (per_cu - 1.0)
+                                      : n <= cost.cus ? cost.alone + (cost.unit - cost.alone) * n / cost.cus : cost.unit;
+  const double share = total * a.kv_heads / cost.workers, one = cost.fixed + most;
+  const double run = n <= cost.workers ? unit * one : unit * std::max(one, share + 0.5 * one * cost.workers / n);
+  return run + (slots > 0 ? cost.join + cost.piece * deep + cost.byte * bytes * a.kv_heads : 0.0);
 }
 
-double causal_makespan(const CausalList& l, double fixed, int workers) {
-  double span = 0.0;
-  const size_t dies = workers % kNumXcd == 0 && workers >= kNumXcd ? kNumXcd : 1;
-  for (size_t x = 0; x < dies; ++x) {
-    std::priority_queue<double, std::vector<double>, std::greater<double>> free_at;
-    for (int i = 0; i < std::max<int>(1, workers / static_cast<int>(dies)); ++i) free_at.push(0.0);
-    for (size_t i = x; i < l.items.size(); i += dies) {
-      const double end = free_at.top() + fixed + (l.items[i].end - l.items[i].begin);
-      free_at.pop();
-      free_at.push(end);
-      span = std::max(span, end);
+}  // namespace
+
+int causal_chunk(CausalKernel kind, const CausalShape& a, int block, int stage, const CausalCost& cost, int least,
+                 int64_t max_slots, double* time) {
+  int64_t items = 0;
+  double longest = 0.0;
+  double best = causal_time(kind, a, block, stage, cost, 0, max_slots, &items, &longest);
+  int chunk = 0;
+  // Many rounds of items none of which is long: nothing to gain.
+  if (items < 8 * static_cast<int64_t>(cost.workers) || cost.unit * (cost.fixed + longest) > 0.25 * best) {
+    for (int n : {2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64, 96, 128, 192, 256, 384, 512}) {
+      const int cut = static_cast<int>((longest + n - 1) / n);
+      if (cut < least) break;
+      const double t = causal_time(kind, a, block, stage, cost, cut, max_slots, nullptr, nullptr);
+      if (t < best) {
+        best = t;
+        chunk = cut;
+      }
     }
   }
-  return span;
+  if (time != nullptr) *time = best;
+  return chunk;
 }
 
 std::string check_causal_items(CausalKernel kind, const CausalItem* items, int n, const CausalShape& a, int block,

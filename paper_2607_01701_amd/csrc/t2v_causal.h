@@ -66,14 +66,20 @@ struct CausalList {
 CausalList build_causal_list(CausalKernel kind, const CausalShape& a, int block, int stage, int order, int chunk,
                              double fixed);
 
-// Loop length at which to cut, for `workers` workgroups at a time: 0 unless the longest loop
-// exceeds what an even share of all work gives a worker; then half such a share, at least
-// `least`. `slots` receives nothing above max_slots (the pieces are widened instead).
-int causal_chunk(CausalKernel kind, const CausalShape& a, int block, int stage, double fixed, int workers, int least,
-                 int64_t max_slots);
+// What running a work list costs, in microseconds: an item unit * (fixed + loop length), with `workers`
+// workgroups at a time, or alone * (...) with a CU to itself; joining cut loops `join`, `piece` for each piece
+// of the most cut tile, and byte * the bytes that the pieces write, slot_row of them for each row (or key).
+struct CausalCost {
+  double unit, alone, fixed;
+  int cus, workers;
+  double join, piece, byte;
+  int64_t slot_row;
+};
 
-// Greedy list-scheduling time of a list on `workers` workgroups at a time, in loop units.
-double causal_makespan(const CausalList& l, double fixed, int workers);
+// Loop length at which to cut (0: nowhere) for the least estimated time, which is returned in *time. Pieces have at
+// least `least` keys or stages; at most max_slots slots are used.
+int causal_chunk(CausalKernel kind, const CausalShape& a, int block, int stage, const CausalCost& cost, int least,
+                 int64_t max_slots, double* time);
 
 // Checks items against the offsets that they were built from, as check_work_items does: an empty
 // string, or what is wrong with the first bad one.

@@ -85,8 +85,8 @@ T2V_DEV bf16x8 only_index(const bf16x8& x, int kk, int G) {
 
 // acc[db] += the products of p with the infinities and NaN of the rows operand, over the 32 contraction
 // indices of a step, one at a time; sees(kk, r): whether this lane's result r takes index kk. read(half, db)
-// gives the operand of indices half .. half + 15 again; ROWS_FIRST: it is the MFMA's first operand.
-template <bool ROWS_FIRST, int DB, typename Read, typename Sees>
+// gives the operand of indices half .. half + 15 again.
+template <int DB, typename Read, typename Sees>
 T2V_DEV void add_nonfinite(f32x16 (&acc)[DB], const bf16x8 (&p)[2], int G, Read&& read, Sees&& sees) {
 #pragma unroll 1
   for (int kk = 0; kk < 32; ++kk) {
@@ -99,7 +99,7 @@ T2V_DEV void add_nonfinite(f32x16 (&acc)[DB], const bf16x8 (&p)[2], int G, Read&
     for (int db = 0; db < DB; ++db) {
       fence();  // one product at a time: the sums leave few registers
       const bf16x8 x = only_index(split_finite<false>(read(kk & 16, db)), kk & 15, G);
-      const f32x16 t = ROWS_FIRST ? mfma(x, pk, zero16()) : mfma(pk, x, zero16());
+      const f32x16 t = mfma(x, pk, zero16());
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[db][r] += sees(kk, r) ? t[r] : 0.0f;
     }

@@ -84,11 +84,11 @@ T2V_DEV void dkdv_step(uint32_t qbase, uint32_t gbase, uint32_t qr0, uint32_t qr
     }
     fence();
   }
-  // dV += P^T dO, then dK += dS^T Q: the dS arithmetic finishes under the first.
+  // dV^T += dO^T P, then dK^T += Q^T dS: the dS arithmetic finishes under the first.
   bf16x8 bg[2][DB], bq[2][DB];
   auto read_g = [&](int half, int db) { return read_rows_opnd<D>(gr0, gr1, q0 + half, db); };
   auto read_q = [&](int half, int db) { return read_rows_opnd<D>(qr0, qr1, q0 + half, db); };
-  auto sees = [&](int n, int r) { return (r >> 2) * 8 + G * 4 + (r & 3) <= first + n && n < nq; };
+  auto sees = [&](int n, int) { return (lane & 31) <= first + n && n < nq; };
 #pragma unroll
   for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
@@ -97,7 +97,7 @@ T2V_DEV void dkdv_step(uint32_t qbase, uint32_t gbase, uint32_t qr0, uint32_t qr
 #pragma unroll
   for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
-    for (int db = 0; db < DB; ++db) dva[db] = mfma(pb[hf], bg[hf][db], dva[db]);
+    for (int db = 0; db < DB; ++db) dva[db] = mfma(bg[hf][db], pb[hf], dva[db]);
   if constexpr (MASK) fence();
 #pragma unroll
   for (int hf = 0; hf < 2; ++hf)
@@ -107,10 +107,10 @@ T2V_DEV void dkdv_step(uint32_t qbase, uint32_t gbase, uint32_t qr0, uint32_t qr
 #pragma unroll
   for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
-    for (int db = 0; db < DB; ++db) dka[db] = mfma(sb[hf], bq[hf][db], dka[db]);
+    for (int db = 0; db < DB; ++db) dka[db] = mfma(bq[hf][db], sb[hf], dka[db]);
   if constexpr (MASK) {
-    if (odd_g) add_nonfinite<false>(dva, pb, G, read_g, sees);
-    if (odd_q) add_nonfinite<false>(dka, sb, G, read_q, sees);
+    if (odd_g) add_nonfinite(dva, pb, G, read_g, sees);
+    if (odd_q) add_nonfinite(dka, sb, G, read_q, sees);
   }
 }
 
@@ -223,7 +223,10 @@ __global__ __launch_bounds__(threads<D>(), 1) void causal_dkdv_kernel(
           const int first = i0 + off - key_wave0;  // the wave's last key that query i0 sees
 #pragma unroll 1
           for (int n = 0; n < BM && i0 + n < it.lq; n += 32)
-            if (first + n + 31 >= 0)
+            if (D == 64 && first + n >= 31 && i0 + n + 32 <= it.lq)
+              dkdv_step<D, false>(tq + oo, tg + oo, tq + ro0, tq + ro1, tg + ro0, tg + ro1, sL[b], sD[b], n, 0, 0, c, kop,
+                                  vop, dka, dva, lane);
+            else if (first + n + 31 >= 0)
               dkdv_step<D, true>(tq + oo, tg + oo, tq + ro0, tq + ro1, tg + ro0, tg + ro1, sL[b], sD[b], n, first + n,
                                  it.lq - i0 - n, c, kop, vop, dka, dva, lane);
         }
@@ -247,26 +250,33 @@ __global__ __launch_bounds__(threads<D>(), 1) void causal_dkdv_kernel(
   }
 
   if (wave_active) {
-    const int64_t rs = static_cast<int64_t>(Hk) * D;
-    const int64_t base = static_cast<int64_t>(it.krow0) * rs + static_cast<int64_t>(it.head) * D;
-    // Accumulators: lane = column db * 32 + l32, register r = key 8 (r / 4) + 4 G + r % 4.
-    float* pk = partial + static_cast<int64_t>(it.slot) * (2 * tile_keys<D>() * D);
-    float* pv = pk + tile_keys<D>() * D;
+    // Sums: lane = key, register r = column 8 (r / 4) + 4 G + r % 4 of each 32.
+    const int kr = wave * 32 + l32;  // key of the tile
+    const bool ok = it.tile0 + kr < it.lk;
+    if (it.slot >= 0) {
+      float* pk = partial + static_cast<int64_t>(it.slot) * (2 * tile_keys<D>() * D) + kr * D;
+      float* pv = pk + tile_keys<D>() * D;
+      if (ok) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int kr = wave * 32 + (r >> 2) * 8 + G * 4 + (r & 3);
-      const int64_t kj = it.tile0 + kr;
-      if (kj < it.lk) {
+        for (int db = 0; db < DB; ++db)
 #pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          if (it.slot >= 0) {
-            pk[kr * D + db * 32 + l32] = dka[db][r];
-            pv[kr * D + db * 32 + l32] = dva[db][r];
-          } else {
-            dk[base + kj * rs + db * 32 + l32] = static_cast<bf16>(dka[db][r] * scale);
-            dv[base + kj * rs + db * 32 + l32] = static_cast<bf16>(dva[db][r]);
+          for (int i = 0; i < 4; ++i) {
+            f32x4 x, y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              x[e] = dka[db][i * 4 + e];
+              y[e] = dva[db][i * 4 + e];
+            }
+            *reinterpret_cast<f32x4*>(pk + db * 32 + i * 8 + G * 4) = x;
+            *reinterpret_cast<f32x4*>(pv + db * 32 + i * 8 + G * 4) = y;
           }
-        }
+      }
+    } else {
+      const int64_t at = ((static_cast<int64_t>(it.krow0) + it.tile0 + kr) * Hk + it.head) * D;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        store_rows(dk + at + db * 32, dka[db], scale, G, ok);
+        store_rows(dv + at + db * 32, dva[db], 1.0f, G, ok);
       }
     }
   }
@@ -289,6 +299,7 @@ __global__ __launch_bounds__(kThreads) void causal_dkdv_join_kernel(const float*
     if (r >= nkeys) continue;
     const float* p = partial + it.slot * slot + which * tile_keys<D>() * D + (k0 + r) * D + c4 * 4;
     f32x4 a = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
     for (int i = 0; i < it.pieces; ++i) a += *reinterpret_cast<const f32x4*>(p + i * slot);
     const float m = which == 0 ? scale : 1.0f;
     bf16x4 w;

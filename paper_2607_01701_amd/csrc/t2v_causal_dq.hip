@@ -61,7 +61,7 @@ T2V_DEV void dq_step(uint32_t kbase, uint32_t vbase, uint32_t kr0, uint32_t kr1,
     for (int db = 0; db < DB; ++db) dqa[db] = mfma(kt[hf][db], sb[hf], dqa[db]);
   if constexpr (MASK) {
     if (odd)
-      add_nonfinite<true>(dqa, sb, G, [&](int half, int db) { return read_rows_opnd<D>(kr0, kr1, kb + half, db); },
+      add_nonfinite(dqa, sb, G, [&](int half, int db) { return read_rows_opnd<D>(kr0, kr1, kb + half, db); },
                           [&](int kk, int) { return kk <= lim; });
   }
 }
@@ -192,6 +192,7 @@ __global__ __launch_bounds__(kThreads) void causal_dq_join_kernel(const float* _
   const int64_t slot = static_cast<int64_t>(R) * D;
   const float* p = partial + it.slot * slot + r * D + col;
   f32x4 a = {0.0f, 0.0f, 0.0f, 0.0f}, b = a;
+#pragma unroll 4
   for (int i = 0; i < it.pieces; ++i) {
     a += *reinterpret_cast<const f32x4*>(p + i * slot);
     b += *reinterpret_cast<const f32x4*>(p + i * slot + 4);

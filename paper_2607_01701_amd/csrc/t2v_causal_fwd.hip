@@ -85,7 +85,7 @@ T2V_DEV void fwd_step(uint32_t kbase, uint32_t vbase0, uint32_t vbase1, int kb, 
     for (int db = 0; db < DB; ++db) o[db] = mfma(va[hf][db], pb[hf], o[db]);
   if constexpr (MASK) {
     if (odd)
-      add_nonfinite<true>(o, pb, G, [&](int half, int db) { return read_rows_opnd<D>(vbase0, vbase1, kb + half, db); },
+      add_nonfinite(o, pb, G, [&](int half, int db) { return read_rows_opnd<D>(vbase0, vbase1, kb + half, db); },
                           [&](int kk, int) { return kk <= lim; });
   }
 }
@@ -211,8 +211,174 @@ __global__ __launch_bounds__(NT, 512 / NT) void causal_fwd_kernel(
   if (trace != nullptr) trace_end(trace, trace_t0, 0, blockIdx.x);
 }
 
+// ------------------------------------------------------------------ few rows: single tokens
+//
+// A (sequence, key head) with at most 32 packed rows: a workgroup's four waves hold the same rows and take
+// every fourth 32-key step, each through LDS buffers of its own (the copy of the next step in flight), so
+// nothing but its own copies holds a wave up; the waves' sums meet in LDS at the end. The keys and values, read
+// once, bound it: one workgroup a CU (two at head_dim 64) has 64 KB in flight.
+constexpr int kFewRows = 32;
+
+// Copy of 32 rows of a (sequence, key head) by one wave into a swizzled tile; rows behind the last repeat it.
+// Instruction j covers RPI rows; its swizzle differs from instruction 0's by a constant.
+template <int D>
+struct WaveDma {
+  static constexpr int CPR = D / 8, RPI = 64 / CPR, NJ = 32 / RPI;
+  int r0;
+  uint32_t chunk0;
+  T2V_DEV explicit WaveDma(int lane) : r0(lane / CPR), chunk0(static_cast<uint32_t>((lane % CPR) ^ swz<D>(lane / CPR))) {}
+  T2V_DEV void copy(uint32_t lds, const bf16* g, int64_t rs, int row0, int L) const {
+    const bf16* base = g + row0 * rs;
+    const int last = L - 1 - row0;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int r = min(r0 + RPI * j, last);
+      const uint32_t col = (chunk0 ^ static_cast<uint32_t>(swz<D>(RPI * j))) * 16;
+#if T2V_CHECKED
+      if (!check_row(row0 + r, L)) {
+        dma_lds16_s(g, col, lds + j * 1024);
+        continue;
+      }
+#endif
+      dma_lds16_s(base, static_cast<uint32_t>(r) * static_cast<uint32_t>(rs * 2) + col, lds + j * 1024);
+    }
+  }
+};
+
+template <int D>
+__global__ __launch_bounds__(256, D == 64 ? 2 : 1) void causal_fwd_few_kernel(
+    const bf16* __restrict__ q, const bf16* __restrict__ k, const bf16* __restrict__ v, int64_t qs, int64_t ks,
+    int64_t vs, const CausalItem* __restrict__ items, int H, int g, int64_t T, float c, unsigned qkeep, unsigned qflip,
+    bf16* __restrict__ out, float* __restrict__ lse, float* __restrict__ partial,
+    unsigned long long* __restrict__ trace) {
+  constexpr int KK = D / 16, DB = D / 32, R = kFewRows;
+  constexpr int kTile = 32 * D;                       // elements of a step's K or V
+  constexpr int kOps = 2 * WaveDma<D>::NJ;            // copies of a step
+  __shared__ __attribute__((aligned(1024))) bf16 sKV[4][2][2][kTile];  // [wave][buffer][K, V]
+  __shared__ float sM[4][R], sL[4][R];
+  const unsigned long long trace_t0 = trace != nullptr ? trace_clock() : 0ull;
+  const CausalItem it = items[blockIdx.x];
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = lane >> 5;
+  const LaneRow me = lane_row(it, g, 0, lane);
+  const int lim_lo = __builtin_amdgcn_readlane(me.lim, 0);
+
+  f32x16 o[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) o[db] = zero16();
+  float m_run = -kInf, l_run = 0.0f;
+
+  const int nsteps = (it.end - it.begin + 31) / 32;
+  if (wave < nsteps) {
+    const bf16* kh = k + it.krow0 * ks + static_cast<int64_t>(it.head) * D;
+    const bf16* vh = v + it.krow0 * vs + static_cast<int64_t>(it.head) * D;
+    const WaveDma<D> dma(lane);
+    const uint32_t buf = lds_addr(sKV[wave]);
+    auto fetch = [&](int n, uint32_t b) {
+      dma.copy(buf + b * (4 * kTile), kh, ks, it.begin + n * 32, it.lk);
+      dma.copy(buf + b * (4 * kTile) + 2 * kTile, vh, vs, it.begin + n * 32, it.lk);
+    };
+    fetch(wave, 0);
+    bf16x8 qop[KK];
+    const bf16* qp = q + me.token * qs + static_cast<int64_t>(me.head) * D;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      u32x4 w = load_raw16(qp + kk * 16 + G * 8, me.ok);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = (w[e] & qkeep) ^ qflip;
+      qop[kk] = __builtin_bit_cast(bf16x8, w);
+      pin(qop[kk]);  // the loads end here, not between counted copies
+    }
+    const uint32_t ko = opnd_lane_off<D>(lane);
+    const uint32_t vo0 = rows_lane_off<D>(lane, 0), vo1 = rows_lane_off<D>(lane, 1);
+    uint32_t b = 0;
+    for (int n = wave; n < nsteps; n += 4, b ^= 1) {
+      // This wave's reads of the buffer that is filled next have returned: their results are used.
+      if (n + 4 < nsteps) {
+        fetch(n + 4, b ^ 1);
+        wait_vmcnt<kOps>();
+      } else {
+        wait_vmcnt0();
+      }
+      asm volatile("" ::: "memory");
+      const uint32_t tile = buf + b * (4 * kTile);
+      const uint32_t vb = tile + 2 * kTile;
+      const int key0 = it.begin + n * 32;
+      if (key0 + 31 <= lim_lo)
+        fwd_step<D, false>(tile + ko, vb + vo0, vb + vo1, 0, 0, c, qop, o, m_run, l_run, lane);
+      else
+        fwd_step<D, true>(tile + ko, vb + vo0, vb + vo1, 0, me.lim - key0, c, qop, o, m_run, l_run, lane);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // before the next copy over what this step read
+    }
+  }
+
+  // The waves' sums, unnormalised and each with its own reference, in fp32: wave w's in its buffers.
+  const float lt = half_sum(l_run);
+  float* mine = reinterpret_cast<float*>(sKV[wave]);
+  const int l32 = lane & 31;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f32x4 w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = o[db][i * 4 + e];
+      *reinterpret_cast<f32x4*>(mine + l32 * D + db * 32 + i * 8 + G * 4) = w;
+    }
+  if (G == 0) {
+    sM[wave][l32] = m_run;
+    sL[wave][l32] = lt;
+  }
+  __syncthreads();
+  // A thread takes D / 8 columns of one row.
+  constexpr int C = D / 8;
+  const int r = tid >> 3, col = (tid & 7) * C;
+  const LaneRow row = lane_row(it, g, 0, r);
+  if (row.ok) {
+    float m = sM[0][r];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) m = max_nan(m, sM[w][r]);
+    const float ref = m == -kInf ? 0.0f : m;
+    float l = 0.0f, x[C];
+#pragma unroll
+    for (int e = 0; e < C; ++e) x[e] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float a = __builtin_amdgcn_exp2f(sM[w][r] - ref);
+      l = fmaf(a, sL[w][r], l);
+      const float* src = reinterpret_cast<const float*>(sKV[w]) + r * D + col;
+#pragma unroll
+      for (int e = 0; e < C; ++e) x[e] = fmaf(a, src[e], x[e]);
+    }
+    if (it.slot >= 0) {
+      float* po = partial + static_cast<int64_t>(it.slot) * (R * (D + 2));
+#pragma unroll
+      for (int e = 0; e < C; e += 4) *reinterpret_cast<f32x4*>(po + r * D + col + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
+      if (col == 0) {
+        po[R * D + 2 * r] = m;
+        po[R * D + 2 * r + 1] = l;
+      }
+    } else {
+      const float inv = row.lim < 0 ? 0.0f : 1.0f / l;
+      bf16* op = out + (row.token * H + row.head) * D + col;
+#pragma unroll
+      for (int e = 0; e < C; e += 8) {
+        bf16x8 w;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = static_cast<bf16>(x[e + i] * inv);
+        *reinterpret_cast<bf16x8*>(op + e) = w;
+      }
+      if (col == 0) lse[static_cast<int64_t>(row.head) * T + row.token] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+    }
+  }
+  if (trace != nullptr) trace_end(trace, trace_t0, 0, blockIdx.x);
+}
+
 // Joins the pieces of the cut tiles: with the largest reference m of a row, out = sum_p 2^(m_p - m) O_p / l,
-// l = sum_p 2^(m_p - m) l_p, in piece order. D / 8 lanes hold a row, eight columns each.
+// l = sum_p 2^(m_p - m) l_p, in piece order. D / 8 lanes hold a row, eight columns each; they read the
+// references and sums of D / 8 pieces at once, and the sums of several pieces are in flight together.
 template <int D>
 __global__ __launch_bounds__(kThreads) void causal_fwd_join_kernel(const float* __restrict__ partial,
                                                                     const CausalItem* __restrict__ tiles, int R, int H,
@@ -222,27 +388,39 @@ __global__ __launch_bounds__(kThreads) void causal_fwd_join_kernel(const float* 
   const int blocks = R / RPB;
   const CausalItem it = tiles[blockIdx.x / blocks];
   const int r = (blockIdx.x % blocks) * RPB + threadIdx.x / LPR;  // row of the tile
-  const int col = threadIdx.x % LPR * 8;
+  const int sub = threadIdx.x % LPR, col = sub * 8;
   const int row = it.tile0 + r;
-  if (row >= it.lq * g) return;
+  if (row >= it.lq * g) return;  // all lanes of a row alike
   const PackedRow pr = packed_row(row, g);
   const int64_t slot = static_cast<int64_t>(R) * (D + 2);
   const float* po = partial + it.slot * slot;
   const float* pm = po + R * D + 2 * r;
   po += r * D + col;
   float m = -kInf;
-  for (int p = 0; p < it.pieces; ++p) m = max_nan(m, pm[p * slot]);
+  for (int p = sub; p < it.pieces; p += LPR) m = max_nan(m, pm[p * slot]);
+#pragma unroll
+  for (int off = LPR / 2; off > 0; off >>= 1) m = max_nan(m, __shfl_xor(m, off, LPR));
   const float ref = m == -kInf ? 0.0f : m;
   float l = 0.0f;
   f32x4 a = {0.0f, 0.0f, 0.0f, 0.0f}, b = a;
-  for (int p = 0; p < it.pieces; ++p) {
-    const float w = __builtin_amdgcn_exp2f(pm[p * slot] - ref);
-    l = fmaf(w, pm[p * slot + 1], l);
-    const f32x4 x = *reinterpret_cast<const f32x4*>(po + p * slot), y = *reinterpret_cast<const f32x4*>(po + p * slot + 4);
+  for (int p0 = 0; p0 < it.pieces; p0 += LPR) {
+    const int mine = p0 + sub;
+    const bool has = mine < it.pieces;
+    const float w_mine = has ? __builtin_amdgcn_exp2f(pm[mine * slot] - ref) : 0.0f;
+    const float l_mine = has ? pm[mine * slot + 1] : 0.0f;
+    const int n = min(LPR, it.pieces - p0);
+    const float* x = po + p0 * slot;
+#pragma unroll 4
+    for (int p = 0; p < n; ++p) {
+      const float w = __shfl(w_mine, p, LPR);
+      l = fmaf(w, __shfl(l_mine, p, LPR), l);
+      const f32x4 u = *reinterpret_cast<const f32x4*>(x + p * slot);
+      const f32x4 v = *reinterpret_cast<const f32x4*>(x + p * slot + 4);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      a[e] = fmaf(w, x[e], a[e]);
-      b[e] = fmaf(w, y[e], b[e]);
+      for (int e = 0; e < 4; ++e) {
+        a[e] = fmaf(w, u[e], a[e]);
+        b[e] = fmaf(w, v[e], b[e]);
+      }
     }
   }
   const float inv = pr.query + it.lk - it.lq < 0 ? 0.0f : 1.0f / l;
@@ -258,24 +436,32 @@ __global__ __launch_bounds__(kThreads) void causal_fwd_join_kernel(const float* 
   if (col == 0) lse[static_cast<int64_t>(head) * T + token] = (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-template <int D, int NT>
+template <int D, int NT>  // NT 0: the kernel of few rows
 void launch_as(const CausalArgs& a, const CausalItem* items, int n, hipStream_t s) {
   const float c = a.scale == 0.0f ? 1.0f : fabsf(a.scale) * kLog2e;
   const unsigned keep = a.scale == 0.0f ? 0u : ~0u, flip = a.scale < 0.0f ? 0x80008000u : 0u;
-  hipLaunchKernelGGL((causal_fwd_kernel<D, NT>), dim3(n), dim3(NT), 0, s, static_cast<const bf16*>(a.q),
-                     static_cast<const bf16*>(a.k), static_cast<const bf16*>(a.v), a.q_stride, a.k_stride, a.v_stride,
-                     items, a.heads, a.heads / a.kv_heads, a.tq, c, keep, flip, static_cast<bf16*>(a.out), a.lse,
-                     a.partial, a.trace);
+  auto launch = [&](auto kernel, int threads) {
+    hipLaunchKernelGGL(kernel, dim3(n), dim3(threads), 0, s, static_cast<const bf16*>(a.q), static_cast<const bf16*>(a.k),
+                       static_cast<const bf16*>(a.v), a.q_stride, a.k_stride, a.v_stride, items, a.heads,
+                       a.heads / a.kv_heads, a.tq, c, keep, flip, static_cast<bf16*>(a.out), a.lse, a.partial, a.trace);
+  };
+  if constexpr (NT == 0)
+    launch(causal_fwd_few_kernel<D>, 256);
+  else
+    launch(causal_fwd_kernel<D, NT>, NT);
 }
 
 }  // namespace
 
 int causal_fwd_rows(bool narrow) { return (narrow ? kThreadsNarrow : kThreadsWide) / 2; }
+int causal_fwd_few_rows() { return kFewRows; }
 int64_t causal_fwd_slot_bytes(int rows, int head_dim) { return static_cast<int64_t>(rows) * (head_dim + 2) * 4; }
 
 hipError_t launch_causal_fwd(const CausalArgs& a, int rows, const CausalItem* items, int n, hipStream_t s) {
-  const bool narrow = rows == causal_fwd_rows(true);
-  if (a.head_dim == 128)
+  const bool narrow = rows == causal_fwd_rows(true), d128 = a.head_dim == 128;
+  if (rows == kFewRows)
+    d128 ? launch_as<128, 0>(a, items, n, s) : launch_as<64, 0>(a, items, n, s);
+  else if (d128)
     narrow ? launch_as<128, kThreadsNarrow>(a, items, n, s) : launch_as<128, kThreadsWide>(a, items, n, s);
   else
     narrow ? launch_as<64, kThreadsNarrow>(a, items, n, s) : launch_as<64, kThreadsWide>(a, items, n, s);

@@ -29,6 +29,7 @@ struct CausalArgs {
 };
 
 int causal_fwd_rows(bool narrow);
+int causal_fwd_few_rows();  // the kernel for at most so many rows of a (sequence, key head)
 int causal_dq_rows(bool narrow);
 int causal_dkdv_keys(int head_dim);
 int causal_dkdv_stage(int head_dim);
