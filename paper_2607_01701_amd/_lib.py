@@ -461,7 +461,7 @@ def _check_rows(t, name, shape):
     if t.dtype != torch.bfloat16:
         raise ValueError(f"{name} has dtype {t.dtype}, expected {torch.bfloat16}")
     T, H, D = shape
-    if t.numel() == 0 or t.is_contiguous():
+    if t.is_contiguous() or t.numel() == 0:
         return H * D
     step = t.stride(0) if T > 1 else H * D
     if t.stride(2) != 1 or (H > 1 and t.stride(1) != D) or step < H * D:
@@ -474,33 +474,60 @@ def _causal_arguments(q, k, v, cu_seqlens, cu_seqlens_k):
     if q.dim() != 3 or k.dim() != 3:
         raise ValueError("q and k must be [tokens, heads, head_dim]")
     T, H, D = q.shape
-    Tk, Hk = k.shape[:2]
+    Tk, Hk, _ = k.shape
     strides = (_check_rows(q, "q", (T, H, D)), _check_rows(k, "k", (Tk, Hk, D)), _check_rows(v, "v", (Tk, Hk, D)))
     cq = _cu_array(cu_seqlens)
     _check_offsets(cq, T, "cu_seqlens")
-    ck = cq if cu_seqlens_k is None else _cu_array(cu_seqlens_k)
-    _check_offsets(ck, Tk, "cu_seqlens" if cu_seqlens_k is None else "cu_seqlens_k")
+    if cu_seqlens_k is None:
+        _check_offsets(cq, Tk, "cu_seqlens")
+        return T, H, D, Tk, Hk, strides, cq, cq
+    ck = _cu_array(cu_seqlens_k)
+    _check_offsets(ck, Tk, "cu_seqlens_k")
     if ck.shape != cq.shape:
         raise ValueError(f"cu_seqlens has {cq.shape[0]} entries, cu_seqlens_k {ck.shape[0]}")
     return T, H, D, Tk, Hk, strides, cq, ck
 
 
-def _on_device(t):
-    """The library works on the current device: make it the tensors' own."""
+def _call_on(device, stream, fn, *args):
+    """fn(*args, stream handle) with the tensors' device current (the library works on the current one)."""
     import torch
-    return contextlib.nullcontext() if t.device.index == torch.cuda.current_device() else torch.cuda.device(t.device)
+    if device.index == torch.cuda.current_device():
+        return fn(*args, _stream_handle(stream))
+    with torch.cuda.device(device):
+        return fn(*args, _stream_handle(stream))
 
 
-def _with_workspace(call, device, stream):
-    """call(ws address, ws bytes, need) until it has the workspace it asks for: twice at most."""
+def _call_with_workspace(L, fn, device, stream, *args):
+    """fn(*args, workspace, its bytes, need, stream handle): a second time if the first says what it needs."""
     import torch
     need = ctypes.c_uint64(0)
-    st = call(None, 0, ctypes.byref(need))
+    ref = ctypes.byref(need)
+    st = _call_on(device, stream, fn, *args, None, 0, ref)
     if st == T2V_ERR_WORKSPACE:
         with _on(stream):
             ws = torch.empty(need.value, dtype=torch.uint8, device=device)
-        st = call(ws.data_ptr(), ws.numel(), ctypes.byref(need))
-    return st
+        st = _call_on(device, stream, fn, *args, ws.data_ptr(), need.value, ref)
+    if st != T2V_OK:
+        _check(L, st)
+
+
+def _outputs(specs, device, stream):
+    """The tensors of specs (name, given or None, shape, dtype): checked if given, else allocated for work on
+    `stream`. Returns them and the given ones by name, for the check of their device."""
+    import torch
+    outs, given = [], []
+    for name, t, shape, dtype in specs:
+        if t is None:
+            if stream is None:
+                t = torch.empty(shape, dtype=dtype, device=device)
+            else:
+                with _on(stream):
+                    t = torch.empty(shape, dtype=dtype, device=device)
+        else:
+            _check_tensor(t, name, shape, dtype)
+            given.append((name, t))
+        outs.append(t)
+    return outs, given
 
 
 def causal_attn_fwd(q, k, v, cu_seqlens, scale: float, out=None, lse=None, stream=None, cu_seqlens_k=None):
@@ -509,21 +536,17 @@ def causal_attn_fwd(q, k, v, cu_seqlens, scale: float, out=None, lse=None, strea
     keys sees keys 0 .. i + Lk - Lq; cu_seqlens_k None: Lk = Lq. Returns (out [Tq, H, D] bf16, lse [H, Tq] fp32).
     """
     import torch
-    T, H, D, Tk, Hk, strides, cq, ck = _causal_arguments(q, k, v, cu_seqlens, cu_seqlens_k)
-    if out is None or lse is None:
-        with _on(stream):
-            out = torch.empty((T, H, D), dtype=q.dtype, device=q.device) if out is None else out
-            lse = torch.empty((H, T), dtype=torch.float32, device=q.device) if lse is None else lse
-    _check_tensor(out, "out", (T, H, D))
-    _check_tensor(lse, "lse", (H, T), torch.float32)
-    _check_on_device((("q", q), ("k", k), ("v", v), ("out", out), ("lse", lse)))
+    T, H, D, Tk, Hk, (sq, sk, sv), cq, ck = _causal_arguments(q, k, v, cu_seqlens, cu_seqlens_k)
+    _check_on_device((("q", q), ("k", k), ("v", v)))
+    device = q.device
+    (out, lse), given = _outputs((("out", out, (T, H, D), torch.bfloat16), ("lse", lse, (H, T), torch.float32)),
+                                 device, stream)
+    if given:
+        _check_on_device((("q", q), *given))
     L = lib()
-    with _on_device(q):
-        _check(L, _with_workspace(
-            lambda ws, n, need: L.t2v_causal_fwd(
-                q.data_ptr(), k.data_ptr(), v.data_ptr(), *strides, _offsets_ptr(cq), _offsets_ptr(ck),
-                cq.shape[0] - 1, H, Hk, D, float(scale), out.data_ptr(), lse.data_ptr(), ws, n, need,
-                _stream_handle(stream)), q.device, stream))
+    _call_with_workspace(L, L.t2v_causal_fwd, device, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(), sq, sk, sv,
+                         _offsets_ptr(cq), _offsets_ptr(ck), cq.shape[0] - 1, H, Hk, D, float(scale), out.data_ptr(),
+                         lse.data_ptr())
     return out, lse
 
 
@@ -531,28 +554,20 @@ def causal_attn_bwd(q, k, v, out, lse, dout, cu_seqlens, scale: float, dq=None, 
                     stream=None, cu_seqlens_k=None):
     """Backward of causal_attn_fwd; returns (dq [Tq, H, D], dk, dv [Tk, Hk, D]) in bf16."""
     import torch
-    T, H, D, Tk, Hk, strides, cq, ck = _causal_arguments(q, k, v, cu_seqlens, cu_seqlens_k)
+    T, H, D, Tk, Hk, (sq, sk, sv), cq, ck = _causal_arguments(q, k, v, cu_seqlens, cu_seqlens_k)
     for name, t in (("out", out), ("dout", dout)):
         _check_tensor(t, name, (T, H, D))
     _check_tensor(lse, "lse", (H, T), torch.float32)
-    with _on(stream):
-        dq = torch.empty((T, H, D), dtype=q.dtype, device=q.device) if dq is None else dq
-        dk = torch.empty((Tk, Hk, D), dtype=q.dtype, device=q.device) if dk is None else dk
-        dv = torch.empty((Tk, Hk, D), dtype=q.dtype, device=q.device) if dv is None else dv
-        if delta_ws is None:
-            delta_ws = torch.empty((2, H, T), dtype=torch.float32, device=q.device)
-    _check_tensor(dq, "dq", (T, H, D))
-    _check_tensor(dk, "dk", (Tk, Hk, D))
-    _check_tensor(dv, "dv", (Tk, Hk, D))
-    _check_tensor(delta_ws, "delta_ws", (2, H, T), torch.float32)
-    _check_on_device((("q", q), ("k", k), ("v", v), ("out", out), ("lse", lse), ("dout", dout), ("dq", dq),
-                      ("dk", dk), ("dv", dv), ("delta_ws", delta_ws)))
+    _check_on_device((("q", q), ("k", k), ("v", v), ("out", out), ("lse", lse), ("dout", dout)))
+    device, bf16 = q.device, torch.bfloat16
+    (dq, dk, dv, delta_ws), given = _outputs(
+        (("dq", dq, (T, H, D), bf16), ("dk", dk, (Tk, Hk, D), bf16), ("dv", dv, (Tk, Hk, D), bf16),
+         ("delta_ws", delta_ws, (2, H, T), torch.float32)), device, stream)
+    if given:
+        _check_on_device((("q", q), *given))
     L = lib()
-    with _on_device(q):
-        _check(L, _with_workspace(
-            lambda ws, n, need: L.t2v_causal_bwd(
-                q.data_ptr(), k.data_ptr(), v.data_ptr(), *strides, out.data_ptr(), lse.data_ptr(), _offsets_ptr(cq),
-                _offsets_ptr(ck), cq.shape[0] - 1, H, Hk, D, float(scale), dout.data_ptr(), dq.data_ptr(),
-                dk.data_ptr(), dv.data_ptr(), delta_ws.data_ptr(), ws, n, need, _stream_handle(stream)),
-            q.device, stream))
+    _call_with_workspace(L, L.t2v_causal_bwd, device, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(), sq, sk, sv,
+                         out.data_ptr(), lse.data_ptr(), _offsets_ptr(cq), _offsets_ptr(ck), cq.shape[0] - 1, H, Hk, D,
+                         float(scale), dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+                         delta_ws.data_ptr())
     return dq, dk, dv

@@ -230,7 +230,7 @@ enum CausalForm { kFew, kNarrow, kWide };  // of the forward and dQ kernels; dK/
 // stage of a dK/dV item 2.1 us at 128 and 5.1 at 64; a narrow tile with the CU to itself takes about half,
 // and the kernel of few rows 9 ns a key. Where each key is read by one tile only (`once`: single tokens) the
 // memory's 5 TB/s bound the loop instead. Loads, stores and filling the pipeline: `fixed`. A join costs a
-// launch, 0.1 us a piece, and the pieces' results are written and read at 4.5 TB/s.
+// launch (and a second call that brings the workspace), 0.1 us a piece, and the pieces' results are written and read at 4.5 TB/s.
 CausalCost causal_cost(CausalKernel kind, int head_dim, CausalForm form, bool once, int ncu) {
   CausalCost c{};
   const bool d64 = head_dim == 64;
@@ -238,11 +238,10 @@ CausalCost causal_cost(CausalKernel kind, int head_dim, CausalForm form, bool on
   c.workers = c.cus * (form == kWide ? 1 : form == kFew ? (d64 ? 2 : 1) : d64 ? 3 : 2);
   c.unit = kind == kCausalDkdv ? (d64 ? 5.1 : 2.1) : kind == kCausalFwd ? (d64 ? 0.031 : 0.030) : (d64 ? 0.040 : 0.042);
   c.alone = form == kWide ? c.unit : form == kFew ? 0.009 : 0.55 * c.unit;
-  const double fixed = kind == kCausalDkdv ? (d64 ? 6.0 : 10.0) : form == kFew ? 3.0 : 4.0;
+  c.fixed = kind == kCausalDkdv ? (d64 ? 6.0 : 10.0) : form == kFew ? 3.0 : 4.0;
   if (form == kFew) c.unit = c.alone;
   if (once) c.unit = std::max(c.unit, 4.0 * head_dim * c.workers / 5e6);
-  c.fixed = fixed / c.unit;
-  c.join = 4.0;
+  c.join = 6.0;
   c.piece = 0.1;
   c.byte = 2.0 / 4.5e6;
   c.slot_row = kind == kCausalDkdv ? 8 * head_dim : kind == kCausalFwd ? 4 * (head_dim + 2) : 4 * head_dim;
@@ -283,7 +282,7 @@ CausalList causal_plan(const TileRule& r, const CausalShape& a, int head_dim, in
     chunk = choose(form, &time);
   }
   *block = rows_of_form(form);
-  return build_causal_list(kind, a, *block, stage, order, chunk, cost_of(form).fixed);
+  return build_causal_list(kind, a, *block, stage, order, chunk, cost_of(form).fixed / cost_of(form).unit);
 }
 
 // T2V_LOG=1: one line on stderr per new work list (items, predicted makespan, bound).

@@ -143,7 +143,7 @@ namespace {
 // Infinite when it would need more than max_slots slots.
 double causal_time(CausalKernel kind, const CausalShape& a, int block, int stage, const CausalCost& cost, int chunk,
                    int64_t max_slots, int64_t* items, double* longest) {
-  double total = 0.0, bytes = 0.0;
+  double keys = 0.0, bytes = 0.0;  // loop lengths, and the pieces' results
   int64_t n = 0, slots = 0;
   int most = 0, deep = 1;
   for (int s = 0; s < a.nseq; ++s) {
@@ -154,7 +154,7 @@ double causal_time(CausalKernel kind, const CausalShape& a, int block, int stage
       int count = 1, step = 0;
       const int len = l.length(t);
       pieces_of(kind, len, chunk, &count, &step);
-      total += len + count * cost.fixed;
+      keys += len;
       n += count;
       most = std::max(most, step);
       deep = std::max(deep, count);
@@ -174,8 +174,8 @@ double causal_time(CausalKernel kind, const CausalShape& a, int block, int stage
   const double beside = std::min(per_cu, std::ceil(static_cast<double>(n) / cost.cus));
   const double unit = beside < per_cu ? cost.alone + (cost.unit - cost.alone) * (beside - 1.0) / (per_cu - 1.0)
                                       : n <= cost.cus ? cost.alone + (cost.unit - cost.alone) * n / cost.cus : cost.unit;
-  const double share = total * a.kv_heads / cost.workers, one = cost.fixed + most;
-  const double run = n <= cost.workers ? unit * one : unit * std::max(one, share + 0.5 * one * cost.workers / n);
+  const double share = (unit * keys * a.kv_heads + cost.fixed * n) / cost.workers, one = cost.fixed + unit * most;
+  const double run = n <= cost.workers ? one : std::max(one, share + 0.5 * one * cost.workers / n);
   return run + (slots > 0 ? cost.join + cost.piece * deep + cost.byte * bytes * a.kv_heads : 0.0);
 }
 
@@ -188,7 +188,7 @@ int causal_chunk(CausalKernel kind, const CausalShape& a, int block, int stage, 
   double best = causal_time(kind, a, block, stage, cost, 0, max_slots, &items, &longest);
   int chunk = 0;
   // Many rounds of items none of which is long: nothing to gain.
-  if (items < 8 * static_cast<int64_t>(cost.workers) || cost.unit * (cost.fixed + longest) > 0.25 * best) {
+  if (items < 8 * static_cast<int64_t>(cost.workers) || cost.fixed + cost.unit * longest > 0.25 * best) {
     for (int n : {2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64, 96, 128, 192, 256, 384, 512}) {
       const int cut = static_cast<int>((longest + n - 1) / n);
       if (cut < least) break;

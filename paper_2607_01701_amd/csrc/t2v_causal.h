@@ -66,8 +66,8 @@ struct CausalList {
 CausalList build_causal_list(CausalKernel kind, const CausalShape& a, int block, int stage, int order, int chunk,
                              double fixed);
 
-// What running a work list costs, in microseconds: an item unit * (fixed + loop length), with `workers`
-// workgroups at a time, or alone * (...) with a CU to itself; joining cut loops `join`, `piece` for each piece
+// What running a work list costs, in microseconds: an item fixed + unit * loop length, with `workers`
+// workgroups at a time, or alone instead of unit with a CU to itself; joining cut loops `join`, `piece` for each piece
 // of the most cut tile, and byte * the bytes that the pieces write, slot_row of them for each row (or key).
 struct CausalCost {
   double unit, alone, fixed;

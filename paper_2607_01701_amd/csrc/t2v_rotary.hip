@@ -44,9 +44,12 @@ struct RotaryArgs {
 };
 
 // Eight bf16 at any 2-byte address (a global access of 16 bytes needs no alignment).
+typedef __attribute__((address_space(1))) bf16 gbf16;  // in global memory
+typedef __attribute__((address_space(1))) uint32_t gu32;
 typedef u32x4 __attribute__((aligned(2))) u32x4_any;
-T2V_DEV bf16x8 load_any(const bf16* p) { return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4_any*>(p)); }
-T2V_DEV void store_any(bf16* p, const bf16x8& x) { *reinterpret_cast<u32x4_any*>(p) = __builtin_bit_cast(u32x4, x); }
+typedef __attribute__((address_space(1))) u32x4_any gu32x4_any;
+T2V_DEV bf16x8 load_any(const gbf16* p) { return __builtin_bit_cast(bf16x8, *(const gu32x4_any*)(p)); }
+T2V_DEV void store_any(gbf16* p, const bf16x8& x) { *(gu32x4_any*)(p) = __builtin_bit_cast(u32x4, x); }
 
 // Where a lane is: unit `u` of head `h` (q's heads, then k's) of the workgroup's token `t`.
 struct Place {
@@ -92,15 +95,20 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, in
     const int d = min(a.rot_dim + 16 * (u - turned), D - 16);
     return {d, d + 8, -1};
   };
+  // A lane's tensor is picked from scalar registers: a choice between two arguments would become a
+  // load from the argument block at an address of the lane's.
+  const int hq = a.heads[0];
+  const gbf16 *q = (const gbf16*)(a.in[0]), *k = (const gbf16*)(a.in[1]);
+  gbf16 *qo = (gbf16*)(a.out[0]), *ko = (gbf16*)(a.out[1]);
+  int64_t qs = a.stride[0], ks = a.stride[1];
+  asm volatile("" : "+s"(q), "+s"(k), "+s"(qo), "+s"(ko), "+s"(qs), "+s"(ks));
   auto source = [&](const Place& x) {
-    const bool k = x.h >= a.heads[0];
-    return (k ? a.in[1] : a.in[0]) + (t0 + x.t) * (k ? a.stride[1] : a.stride[0]) +
-           static_cast<int64_t>(x.h - (k ? a.heads[0] : 0)) * D;
+    const bool second = x.h >= hq;
+    return (second ? k : q) + (t0 + x.t) * (second ? ks : qs) + static_cast<int64_t>(x.h - (second ? hq : 0)) * D;
   };
   auto target = [&](const Place& x) {
-    const bool k = x.h >= a.heads[0];
-    return (k ? a.out[1] : a.out[0]) +
-           ((t0 + x.t) * (k ? a.heads[1] : a.heads[0]) + (x.h - (k ? a.heads[0] : 0))) * D;
+    const bool second = x.h >= hq;
+    return (second ? ko : qo) + ((t0 + x.t) * (second ? heads - hq : hq) + (x.h - (second ? hq : 0))) * D;
   };
   // With fewer than eight pairs, or 1 .. 15 dimensions to copy, those are taken one by one.
   const bool few_pairs = pairs < 8, few_copied = D - a.rot_dim < 16;
@@ -112,7 +120,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, in
     for (int i = 0; i < kUnits; ++i) {
       if (e0 + i * kThreads < total && whole(p.u)) {
         const Vectors v = vectors(p.u);
-        const bf16* s = source(p);
+        const gbf16* s = source(p);
         x[i] = load_any(s + v.first);
         y[i] = load_any(s + v.second);
       }
@@ -136,7 +144,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, in
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
       if (e0 + i * kThreads < total) {
-        bf16* o = target(w);
+        gbf16* o = target(w);
         const float2* row = cs + w.t * pairs;
         if (whole(w.u)) {
           const Vectors v = vectors(w.u);
@@ -167,7 +175,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, in
           store_any(o + v.first, x[i]);
           store_any(o + v.second, y[i]);
         } else {
-          const bf16* s = source(w);
+          const gbf16* s = source(w);
           if (w.u < turned) {
             for (int j = 0; j < pairs; ++j) {
               const int d0 = INTERLEAVED ? 2 * j : j, d1 = INTERLEAVED ? 2 * j + 1 : j + pairs;
@@ -175,8 +183,9 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, in
               o[d0] = static_cast<bf16>(u0 * row[j].x - u1 * row[j].y);
               o[d1] = static_cast<bf16>(u0 * row[j].y + u1 * row[j].x);
             }
-          } else {
-            for (int d = a.rot_dim; d < D; ++d) o[d] = s[d];
+          } else {  // two at a time: rot_dim is even
+            for (int d = a.rot_dim; d < D; d += 2)
+              *(gu32*)(o + d) = *(const gu32*)(s + d);
           }
         }
       }
@@ -187,7 +196,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, in
 
 // f radians in 2^-64 turns, modulo a turn. long double holds 64 bits of the quotient.
 unsigned long long turn_of(double f) {
-  const long double turns = static_cast<long double>(f) / (2.0L * 3.14159265358979323846264338327950288L);
+  const long double turns = static_cast<long double>(f) * 0.159154943091895335768883763372514362L;  // 1 / (2 pi)
   const long double frac = turns - std::floor(turns);
   const long double scaled = frac * 18446744073709551616.0L;
   return scaled >= 18446744073709551615.0L ? ~0ull : static_cast<unsigned long long>(scaled + 0.5L);

@@ -11,6 +11,7 @@ from . import _lib
 
 LAYOUTS = {"half": 0, "interleaved": 1}
 SCALINGS = (None, "linear", "ntk", "yarn")
+_SECTIONS = {n: ctypes.c_int32 * n for n in (1, 2, 3)}
 
 
 def rotary_frequencies(sections, theta: float = 10000.0, scaling=None, factor: float = 1.0, trained=None,
@@ -64,43 +65,47 @@ def rotary_apply(q, k, positions, freqs, layout: str = "half", sections=None, ms
     if layout not in LAYOUTS:
         raise ValueError(f"layout must be one of {tuple(LAYOUTS)}, got {layout!r}")
     T, _, D = first.shape
-    f = np.ascontiguousarray(freqs, dtype=np.float64)
+    f = freqs
+    if type(f) is not np.ndarray or f.dtype != np.float64 or not f.flags.c_contiguous:
+        f = np.ascontiguousarray(freqs, dtype=np.float64)
     if f.ndim != 1:
         raise ValueError("freqs must be a 1-D array, one frequency a pair")
-    sec = (ctypes.c_int32 * 3)(*((f.shape[0],) if sections is None else sections))
-    n_sec = 1 if sections is None else len(sections)
-    if sum(sec) != f.shape[0]:
-        raise ValueError(f"sections {tuple(sections)} do not sum to the {f.shape[0]} frequencies")
-    if tuple(positions.shape) not in ((T,), (1, T)) if n_sec == 1 else tuple(positions.shape) != (n_sec, T):
+    pairs = f.shape[0]
+    sections = (pairs,) if sections is None else tuple(sections)
+    n_sec = len(sections)
+    if not 1 <= n_sec <= 3 or sum(sections) != pairs:
+        raise ValueError(f"sections {sections} are not one to three counts that sum to the {pairs} frequencies")
+    if positions.shape != (n_sec, T) and (n_sec > 1 or positions.shape != (T,)):
         raise ValueError(f"positions has shape {tuple(positions.shape)}, expected {(n_sec, T)}")
     if positions.dtype != torch.int32 or not positions.is_contiguous():
         raise ValueError("positions must be contiguous int32")
-    named, ptrs, strides, heads, outs = [("positions", positions)], [], [], [], []
+    named = [("positions", positions)]
+    args = []
     for x, o, name in ((q, q_out, "q"), (k, k_out, "k")):
         if x is None:
-            ptrs.append((None, None))
-            strides.append(0)
-            heads.append(0)
-            outs.append(None)
+            args.append((None, 0, 0, None, None))
             continue
         shape = (T, x.shape[1], D)
-        strides.append(_lib._check_rows(x, name, shape))
-        if o is None:
-            with _lib._on(stream):
-                o = torch.empty(shape, dtype=x.dtype, device=x.device)
-        _lib._check_tensor(o, name + "_out", shape)
-        named += [(name, x), (name + "_out", o)]
-        ptrs.append((x.data_ptr(), o.data_ptr()))
-        heads.append(shape[1])
-        outs.append(o)
+        step = _lib._check_rows(x, name, shape)
+        named.append((name, x))
+        args.append((x.data_ptr(), step, shape, o, name + "_out"))
     _lib._check_on_device(named)
+    device = first.device
+    outs, given = _lib._outputs([(name, o, shape, torch.bfloat16) for p, _, shape, o, name in args if p is not None],
+                                device, stream)
+    if given:
+        _lib._check_on_device((named[0], *given))
+    got = iter(outs)
+    q_out, k_out = (None if x is None else next(got) for x in (q, k))
+    (qp, sq, qshape, _, _), (kp, sk, kshape, _, _) = args
     L = _lib.lib()
-    with _lib._on_device(first):
-        st = L.t2v_rotary(ptrs[0][0], ptrs[1][0], strides[0], strides[1], positions.data_ptr(), T, heads[0], heads[1], D,
-                          f.ctypes.data, sec, n_sec, LAYOUTS[layout], float(mscale), 1 if inverse else 0, ptrs[0][1],
-                          ptrs[1][1], _lib._stream_handle(stream))
-    _lib._check(L, st)
-    return tuple(outs)
+    st = _lib._call_on(device, stream, L.t2v_rotary, qp, kp, sq, sk, positions.data_ptr(), T, qshape[1] if qshape else 0,
+                       kshape[1] if kshape else 0, D, f.__array_interface__["data"][0], _SECTIONS[n_sec](*sections),
+                       n_sec, LAYOUTS[layout], float(mscale), 1 if inverse else 0,
+                       None if q_out is None else q_out.data_ptr(), None if k_out is None else k_out.data_ptr())
+    if st != _lib.T2V_OK:
+        _lib._check(L, st)
+    return q_out, k_out
 
 
 def _function():
@@ -137,7 +142,10 @@ _FN = None
 
 
 def rotary(q, k, positions, freqs, layout: str = "half", sections=None, mscale: float = 1.0):
-    """rotary_apply with autograd: gradients flow to q and k (k may be None)."""
+    """rotary_apply with autograd: gradients flow to q and k (either may be None)."""
+    import torch
+    if not torch.is_grad_enabled() or not any(x is not None and x.requires_grad for x in (q, k)):
+        return rotary_apply(q, k, positions, freqs, layout, sections, mscale)
     global _FN
     if _FN is None:
         _FN = _function()
