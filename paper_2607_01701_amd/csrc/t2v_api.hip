@@ -61,12 +61,14 @@ struct TileRule {
   }
 };
 
-int forced_tiles() {
-  const char* s = std::getenv("T2V_QTILE");
+int forced_by(const char* name) {
+  const char* s = std::getenv(name);
   if (s != nullptr && std::strcmp(s, "wide") == 0) return 1;
   if (s != nullptr && std::strcmp(s, "narrow") == 0) return 2;
   return 0;
 }
+int forced_tiles() { return forced_by("T2V_QTILE"); }
+int forced_kv_tiles() { return forced_by("T2V_KVTILE"); }
 
 TileRule fwd_rule(int head_dim) {
   TileRule r;
@@ -107,11 +109,7 @@ TileRule dkdv_rule(int head_dim, int chunk, bool persistent) {
   r.wide = head_dim == 128 ? dkdv_wide_rows() : r.narrow;
   r.forms[0] = {r.wide, 1, 12500.0, 52.8};
   r.forms[1] = {r.narrow, 1, 8000.0, 29.2};
-  const char* s = std::getenv("T2V_KVTILE");
-  if (chunk > 0 || persistent || (s != nullptr && std::strcmp(s, "narrow") == 0))
-    r.forced = 2;
-  else if (s != nullptr && std::strcmp(s, "wide") == 0)
-    r.forced = 1;
+  r.forced = chunk > 0 || persistent ? 2 : forced_kv_tiles();
   return r;
 }
 
@@ -201,12 +199,14 @@ int cu_count() {
 // ------------------------------------------------------- plans of the causal attention kernels
 
 // Rule of a causal work list. The narrow forms of forward and dQ keep two workgroups on a CU at
-// head_dim 128 and three at 64, the wide ones one.
+// head_dim 128 and three at 64, the wide ones one, as both forms of dK/dV do. T2V_QTILE and T2V_KVTILE force one.
 TileRule causal_rule(CausalKernel kind, int head_dim) {
   TileRule r;
   r.kind = kind;
   if (kind == kCausalDkdv) {
-    r.wide = r.narrow = causal_dkdv_keys(head_dim);
+    r.wide = causal_dkdv_keys(head_dim, true);
+    r.narrow = causal_dkdv_keys(head_dim, false);
+    r.forced = forced_kv_tiles();
     return r;
   }
   r.narrow = kind == kCausalFwd ? causal_fwd_rows(true) : causal_dq_rows(true);
@@ -218,71 +218,77 @@ TileRule causal_rule(CausalKernel kind, int head_dim) {
 
 int64_t causal_slot_bytes(CausalKernel kind, int rows, int head_dim) {
   if (kind == kCausalFwd) return causal_fwd_slot_bytes(rows, head_dim);
-  return kind == kCausalDq ? causal_dq_slot_bytes(rows, head_dim) : causal_dkdv_slot_bytes(head_dim);
+  return kind == kCausalDq ? causal_dq_slot_bytes(rows, head_dim) : causal_dkdv_slot_bytes(rows, head_dim);
 }
 
 constexpr int64_t kCausalMaxWorkspace = int64_t(1) << 30;
 
-enum CausalForm { kFew, kNarrow, kWide };  // of the forward and dQ kernels; dK/dV has one, kWide
+enum CausalForm { kFew, kNarrow, kWide };
 
 // Times measured on MI355X (microseconds; see CausalCost): a key of a forward item 30 ns at head_dim 128 (256 rows, or
-// 128 with a second workgroup beside it) and 31 at 64 (128 rows, three workgroups), of a dQ item 42 and 40, a
-// stage of a dK/dV item 2.1 us at 128 and 5.1 at 64; a narrow tile with the CU to itself takes about half,
-// and the kernel of few rows 9 ns a key. Where each key is read by one tile only (`once`: single tokens) the
-// memory's 5 TB/s bound the loop instead. Loads, stores and filling the pipeline: `fixed`. A join costs a
-// launch (and a second call that brings the workspace), 0.1 us a piece, and the pieces' results are written and read at 4.5 TB/s.
+// 128 with a second workgroup beside it) and 31 at 64 (128 rows, three workgroups), of a dQ item 42 and 40; a narrow
+// tile with the CU to itself takes about half, and the kernel of few rows 9 ns a key. Where each key is read
+// by one tile only (`once`: single tokens) the memory's 5 TB/s bound the loop instead. A dK/dV item takes 1.75 us for
+// 32 queries and 256 keys (wide) or 2.1 for 64 and 128 (narrow) at head_dim 128, 5.1 for 128 and 256 at 64.
+// Loads, stores and filling the pipeline: `fixed`. A join costs a launch (and a second call that brings the
+// workspace), 0.1 us a piece, and the pieces' results are written and read at 4.5 TB/s.
 CausalCost causal_cost(CausalKernel kind, int head_dim, CausalForm form, bool once, int ncu) {
   CausalCost c{};
   const bool d64 = head_dim == 64;
   c.cus = std::max(1, ncu);
-  c.workers = c.cus * (form == kWide ? 1 : form == kFew ? (d64 ? 2 : 1) : d64 ? 3 : 2);
-  c.unit = kind == kCausalDkdv ? (d64 ? 5.1 : 2.1) : kind == kCausalFwd ? (d64 ? 0.031 : 0.030) : (d64 ? 0.040 : 0.042);
-  c.alone = form == kWide ? c.unit : form == kFew ? 0.009 : 0.55 * c.unit;
-  c.fixed = kind == kCausalDkdv ? (d64 ? 6.0 : 10.0) : form == kFew ? 3.0 : 4.0;
-  if (form == kFew) c.unit = c.alone;
-  if (once) c.unit = std::max(c.unit, 4.0 * head_dim * c.workers / 5e6);
   c.join = 6.0;
   c.piece = 0.1;
   c.byte = 2.0 / 4.5e6;
-  c.slot_row = kind == kCausalDkdv ? 8 * head_dim : kind == kCausalFwd ? 4 * (head_dim + 2) : 4 * head_dim;
+  if (kind == kCausalDkdv) {
+    c.workers = c.cus;
+    c.unit = c.alone = d64 ? 5.1 : form == kWide ? 1.75 : 2.1;
+    c.fixed = d64 ? 6.0 : form == kWide ? 12.0 : 10.0;
+    c.slot_row = 8 * head_dim;
+    return c;
+  }
+  c.workers = c.cus * (form == kWide ? 1 : form == kFew ? (d64 ? 2 : 1) : d64 ? 3 : 2);
+  c.unit = kind == kCausalFwd ? (d64 ? 0.031 : 0.030) : (d64 ? 0.040 : 0.042);
+  c.alone = form == kWide ? c.unit : form == kFew ? 0.009 : 0.55 * c.unit;
+  c.fixed = form == kFew ? 3.0 : 4.0;
+  if (form == kFew) c.unit = c.alone;
+  if (once) c.unit = std::max(c.unit, 4.0 * head_dim * c.workers / 5e6);
+  c.slot_row = 4 * (head_dim + (kind == kCausalFwd ? 2 : 0));
   return c;
 }
 
 CausalList causal_plan(const TileRule& r, const CausalShape& a, int head_dim, int order, bool split, int ncu,
                        int* block) {
   const auto kind = static_cast<CausalKernel>(r.kind);
-  const int stage = causal_dkdv_stage(head_dim);
+  const bool kv = kind == kCausalDkdv;
   int64_t most_rows = 0;
   for (int s = 0; s < a.nseq; ++s)
     most_rows = std::max<int64_t>(most_rows, static_cast<int64_t>(a.cu_q[s + 1] - a.cu_q[s]) * a.group);
-  const int least = kind == kCausalDkdv ? 1 : 64;
   auto rows_of_form = [&](CausalForm f) { return f == kFew ? causal_fwd_few_rows() : f == kNarrow ? r.narrow : r.wide; };
   auto cost_of = [&](CausalForm f) {
-    return causal_cost(kind, head_dim, f, kind != kCausalDkdv && most_rows <= rows_of_form(f), ncu);
+    return causal_cost(kind, head_dim, f, !kv && most_rows <= rows_of_form(f), ncu);
   };
   auto choose = [&](CausalForm f, double* time) {
     const int rows = rows_of_form(f);
     const int64_t slots =
         split ? std::min<int64_t>(kCausalMaxWorkspace / causal_slot_bytes(kind, rows, head_dim), INT32_MAX) : 0;
-    return causal_chunk(kind, a, rows, stage, cost_of(f), least, slots, time);
+    return causal_chunk(kind, a, rows, causal_dkdv_stage(head_dim, rows), cost_of(f), kv ? 1 : 64, slots, time);
   };
-  CausalForm form = kind == kCausalDkdv || r.forced == 1 ? kWide : kNarrow;
+  CausalForm form = r.forced == 1 || r.narrow == r.wide ? kWide : kNarrow;
+  if (kind == kCausalFwd && r.forced == 0 && most_rows <= causal_fwd_few_rows()) form = kFew;
   int chunk = 0;
   double time = 0.0;
-  if (kind == kCausalFwd && r.forced == 0 && most_rows <= causal_fwd_few_rows()) form = kFew;
-  if (form == kNarrow && r.forced == 0 && !r.narrow_always && most_rows > r.narrow) {
-    chunk = choose(kNarrow, &time);
+  chunk = choose(form, &time);
+  if (form == kNarrow && r.forced == 0 && !r.narrow_always && (kv || most_rows > r.narrow)) {
     double wide_time = 0.0;
     const int wide_chunk = choose(kWide, &wide_time);
-    if (wide_time <= 1.04 * time) {  // wide tiles stage a key once for twice the rows
+    if (wide_time <= (kv ? 1.0 : 1.04) * time) {  // wide tiles of rows stage a key once for twice the rows
       form = kWide;
       chunk = wide_chunk;
     }
-  } else {
-    chunk = choose(form, &time);
   }
   *block = rows_of_form(form);
-  return build_causal_list(kind, a, *block, stage, order, chunk, cost_of(form).fixed / cost_of(form).unit);
+  return build_causal_list(kind, a, *block, causal_dkdv_stage(head_dim, *block), order, chunk,
+                           cost_of(form).fixed / cost_of(form).unit, cost_of(form).workers);
 }
 
 // T2V_LOG=1: one line on stderr per new work list (items, predicted makespan, bound).
@@ -813,7 +819,7 @@ int check_causal_plan(const PlanRef& p, const int32_t* cu_q, const int32_t* cu_k
   const CausalShape a{cu_q, cu_k, nseq, p->heads, p->group};
   const auto kind = static_cast<CausalKernel>(p->rule.kind);
   const CausalItem* items = p->host_causal.data();
-  const int stage = causal_dkdv_stage(p->head_dim);
+  const int stage = causal_dkdv_stage(p->head_dim, p->block);
   std::string why = check_causal_items(kind, items, p->n_items, a, p->block, stage, p->slots, false);
   if (why.empty()) why = check_causal_items(kind, items + p->n_items, p->n_reduce, a, p->block, stage, p->slots, true);
   if (!why.empty()) return set_error(T2V_ERR_BOUNDS, std::string("checked library: ") + kernel + " work list, " + why);
@@ -829,7 +835,7 @@ int check_arm() {
   const unsigned int canary = check_canary();
   unsigned int rec[4];
   for (auto take : {fwd_check_take, dkdv_check_take, dkdv_wide_check_take, dq_check_take, short_check_take,
-                    causal_fwd_check_take, causal_dkdv_check_take, causal_dq_check_take}) {
+                    causal_fwd_check_take, causal_dkdv_check_take, causal_dkdv_wide_check_take, causal_dq_check_take}) {
     const hipError_t e = take(rec, canary);
     if (e != hipSuccess) return hip_fail(e, "clearing the DMA row checks");
   }
@@ -841,12 +847,12 @@ int check_arm() {
 int check_collect(hipStream_t s) {
   hipError_t e = hipStreamSynchronize(s);
   if (e != hipSuccess) return hip_fail(e, "waiting for the checked kernels");
-  constexpr int kSources = 8;
-  const char* names[kSources] = {"forward",        "dK/dV",        "dK/dV",    "dQ", "one-pass backward",
-                                 "causal forward", "causal dK/dV", "causal dQ"};
+  constexpr int kSources = 9;
+  const char* names[kSources] = {"forward",        "dK/dV",        "dK/dV",        "dQ", "one-pass backward",
+                                 "causal forward", "causal dK/dV", "causal dK/dV", "causal dQ"};
   hipError_t (*takes[kSources])(unsigned int*, unsigned int) = {
-      fwd_check_take,   dkdv_check_take,       dkdv_wide_check_take,   dq_check_take,
-      short_check_take, causal_fwd_check_take, causal_dkdv_check_take, causal_dq_check_take};
+      fwd_check_take,        dkdv_check_take,        dkdv_wide_check_take,        dq_check_take,       short_check_take,
+      causal_fwd_check_take, causal_dkdv_check_take, causal_dkdv_wide_check_take, causal_dq_check_take};
   int status = T2V_OK;
   for (int i = 0; i < kSources; ++i) {
     unsigned int rec[4];
@@ -1520,9 +1526,9 @@ int causal_bwd_impl(CausalCall& c, const void* out, const float* lse, const void
   if (pk->n_items > 0) {
     a.trace = tracer().reserve(pk->n_items);
     e = timer().run(kSlotDkdv, s, [&] {
-      hipError_t r = launch_causal_dkdv(a, pk->causal(), pk->n_items, s);
+      hipError_t r = launch_causal_dkdv(a, pk->block, pk->causal(), pk->n_items, s);
       if (r == hipSuccess && pk->n_reduce > 0)
-        r = launch_causal_dkdv_join(a, pk->causal() + pk->n_items, pk->n_reduce, s);
+        r = launch_causal_dkdv_join(a, pk->block, pk->causal() + pk->n_items, pk->n_reduce, s);
       return r;
     });
     const int used = note_use(pk, s);

@@ -11,6 +11,8 @@ namespace t2v {
 
 namespace {
 
+constexpr size_t kGroupedRounds = 8;  // of items, from which a die keeps groups together
+
 // Tiles and the loop of tile t of one (sequence, key head).
 struct Loops {
   CausalKernel kind;
@@ -48,7 +50,7 @@ void pieces_of(CausalKernel kind, int n, int chunk, int* count, int* step) {
 }  // namespace
 
 CausalList build_causal_list(CausalKernel kind, const CausalShape& a, int block, int stage, int order, int chunk,
-                             double fixed) {
+                             double fixed, int workers) {
   CausalList out;
   struct Group {
     int seq, head;
@@ -115,6 +117,24 @@ CausalList build_causal_list(CausalKernel kind, const CausalShape& a, int block,
       if (load[x] + 0.5 * c > share) x = static_cast<int>(std::min_element(load.begin(), load.end()) - load.begin());
       q[x].push_back(it);
       load[x] += c;
+    }
+  }
+  // With few rounds of items the longest go first, whatever their group: a long one that starts in the last round would
+  // outlast the others. With more, only the shortest two rounds are kept for the end, and the others stay with their
+  // group, whose keys or queries are in the die's L2.
+  const size_t per_die = static_cast<size_t>(std::max(workers, 1) + kNumXcd - 1) / kNumXcd;
+  auto longer = [](const CausalItem& x, const CausalItem& y) { return x.end - x.begin > y.end - y.begin; };
+  for (auto& l : q) {
+    std::vector<CausalItem> sorted = l;
+    std::stable_sort(sorted.begin(), sorted.end(), longer);
+    const size_t last = 2 * per_die;
+    if (l.size() < kGroupedRounds * per_die) {
+      l.swap(sorted);
+    } else {
+      const int32_t cut = sorted[sorted.size() - last].end - sorted[sorted.size() - last].begin;
+      std::stable_partition(l.begin(), l.end(), [cut](const CausalItem& x) { return x.end - x.begin > cut; });
+      std::stable_sort(std::find_if(l.begin(), l.end(), [cut](const CausalItem& x) { return x.end - x.begin <= cut; }),
+                       l.end(), longer);
     }
   }
   // One list: position b takes the next item of die b % 8, or, when that die has no more, the last

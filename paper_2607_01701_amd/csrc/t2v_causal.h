@@ -62,9 +62,9 @@ struct CausalList {
 // The work list of tiles of `block` packed rows (forward, dQ) or keys (dK/dV, whose loop is counted
 // in stages of `stage` queries). chunk > 0 cuts loops longer than `chunk` keys or stages into equal
 // pieces (multiples of 64 keys). order as in build_worklist. `fixed` is an item's cost besides its
-// loop, in keys or stages.
+// loop, in keys or stages; `workers` workgroups run at a time.
 CausalList build_causal_list(CausalKernel kind, const CausalShape& a, int block, int stage, int order, int chunk,
-                             double fixed);
+                             double fixed, int workers);
 
 // What running a work list costs, in microseconds: an item fixed + unit * loop length, with `workers`
 // workgroups at a time, or alone instead of unit with a CU to itself; joining cut loops `join`, `piece` for each piece

@@ -35,43 +35,6 @@ T2V_DEV LaneRow lane_row(const CausalItem& it, int group, int wave, int lane) {
   return {row < nrows, pr.query + it.lk - it.lq, it.head * group + pr.head, static_cast<int64_t>(it.qrow0) + pr.query};
 }
 
-typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-
-// The operand's finite elements, or its infinities and NaN (exponent bits all ones); zeros for the others.
-template <bool FINITE>
-T2V_DEV bf16x8 split_finite(const bf16x8& x) {
-  u32x4 w = __builtin_bit_cast(u32x4, x);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const unsigned odd = ((w[e] & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) |
-                         ((w[e] & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
-    w[e] &= FINITE ? ~odd : odd;
-  }
-  return __builtin_bit_cast(bf16x8, w);
-}
-
-// Whether any lane's operands hold an infinity or a NaN, which are then replaced by zeros.
-template <int N>
-T2V_DEV bool take_nonfinite(bf16x8 (&x)[2][N]) {
-  u16x2 m = {0, 0};
-#pragma unroll
-  for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const u32x4 w = __builtin_bit_cast(u32x4, x[hf][i]);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[e] & 0x7FFF7FFFu));
-    }
-  const bool odd = __any(m[0] >= 0x7F80 || m[1] >= 0x7F80);
-  if (odd) {
-#pragma unroll
-    for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-      for (int i = 0; i < N; ++i) x[hf][i] = split_finite<true>(x[hf][i]);
-  }
-  return odd;
-}
-
 // The operand with only contraction index kk (0..15) kept: element t of a lane holds index
 // 8 (t / 4) + 4 G + t % 4, as read_rows_opnd and the packed scores have it.
 T2V_DEV bf16x8 only_index(const bf16x8& x, int kk, int G) {

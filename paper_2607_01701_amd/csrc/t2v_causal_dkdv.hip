@@ -93,7 +93,7 @@ T2V_DEV void dkdv_step(uint32_t qbase, uint32_t gbase, uint32_t qr0, uint32_t qr
   for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
     for (int db = 0; db < DB; ++db) bg[hf][db] = read_g(hf * 16, db);
-  const bool odd_g = MASK && take_nonfinite(bg);
+  const bool odd_g = MASK && (take_nonfinite(bg[0]) | take_nonfinite(bg[1]));
 #pragma unroll
   for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
@@ -103,7 +103,7 @@ T2V_DEV void dkdv_step(uint32_t qbase, uint32_t gbase, uint32_t qr0, uint32_t qr
   for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
     for (int db = 0; db < DB; ++db) bq[hf][db] = read_q(hf * 16, db);
-  const bool odd_q = MASK && take_nonfinite(bq);
+  const bool odd_q = MASK && (take_nonfinite(bq[0]) | take_nonfinite(bq[1]));
 #pragma unroll
   for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
@@ -283,21 +283,22 @@ __global__ __launch_bounds__(threads<D>(), 1) void causal_dkdv_kernel(
   if (trace != nullptr) trace_end(trace, trace_t0, 2, blockIdx.x);
 }
 
-// Adds the pieces of the cut tiles in order. A workgroup takes 32 keys; a thread four columns.
+// Adds the pieces of the cut tiles (of `keys` keys) in order. A workgroup takes 32 keys; a thread four columns.
 template <int D>
 __global__ __launch_bounds__(kThreads) void causal_dkdv_join_kernel(const float* __restrict__ partial,
-                                                                     const CausalItem* __restrict__ tiles, int Hk,
-                                                                     float scale, bf16* __restrict__ dk,
+                                                                     const CausalItem* __restrict__ tiles, int keys,
+                                                                     int Hk, float scale, bf16* __restrict__ dk,
                                                                      bf16* __restrict__ dv) {
-  constexpr int kParts = tile_keys<D>() / 32, C4 = D / 4;
-  const CausalItem it = tiles[blockIdx.x / kParts];
-  const int k0 = (blockIdx.x % kParts) * 32;
+  constexpr int C4 = D / 4;
+  const int parts = keys / 32;
+  const CausalItem it = tiles[blockIdx.x / parts];
+  const int k0 = (blockIdx.x % parts) * 32;
   const int nkeys = min(32, it.lk - it.tile0 - k0);
-  const int64_t rs = static_cast<int64_t>(Hk) * D, slot = 2 * tile_keys<D>() * D;
+  const int64_t rs = static_cast<int64_t>(Hk) * D, slot = 2 * keys * D;
   for (int e = threadIdx.x; e < 2 * 32 * C4; e += kThreads) {
     const int which = e / (32 * C4), r = e / C4 % 32, c4 = e % C4;  // which: 0 dK, 1 dV
     if (r >= nkeys) continue;
-    const float* p = partial + it.slot * slot + which * tile_keys<D>() * D + (k0 + r) * D + c4 * 4;
+    const float* p = partial + it.slot * slot + which * keys * D + (k0 + r) * D + c4 * 4;
     f32x4 a = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
     for (int i = 0; i < it.pieces; ++i) a += *reinterpret_cast<const f32x4*>(p + i * slot);
@@ -321,24 +322,30 @@ void launch_as(const CausalArgs& a, const CausalItem* items, int n, hipStream_t 
 
 }  // namespace
 
-int causal_dkdv_keys(int head_dim) { return head_dim == 64 ? tile_keys<64>() : tile_keys<128>(); }
-int causal_dkdv_stage(int head_dim) { return head_dim == 64 ? stage_queries<64>() : stage_queries<128>(); }
-int64_t causal_dkdv_slot_bytes(int head_dim) { return 2LL * causal_dkdv_keys(head_dim) * head_dim * 4; }
+int causal_dkdv_keys(int head_dim, bool wide) {
+  return head_dim == 64 ? tile_keys<64>() : wide ? causal_dkdv_wide_keys() : tile_keys<128>();
+}
+int causal_dkdv_stage(int head_dim, int keys) {
+  if (head_dim == 64) return stage_queries<64>();
+  return keys == causal_dkdv_wide_keys() ? causal_dkdv_wide_stage() : stage_queries<128>();
+}
+int64_t causal_dkdv_slot_bytes(int keys, int head_dim) { return 8LL * keys * head_dim; }
 
-hipError_t launch_causal_dkdv(const CausalArgs& a, const CausalItem* items, int n, hipStream_t s) {
+hipError_t launch_causal_dkdv(const CausalArgs& a, int keys, const CausalItem* items, int n, hipStream_t s) {
+  if (a.head_dim == 128 && keys == causal_dkdv_wide_keys()) return launch_causal_dkdv_wide(a, items, n, s);
   a.head_dim == 128 ? launch_as<128>(a, items, n, s) : launch_as<64>(a, items, n, s);
   return hipGetLastError();
 }
 
-hipError_t launch_causal_dkdv_join(const CausalArgs& a, const CausalItem* tiles, int n, hipStream_t s) {
-  const dim3 grid(n * (causal_dkdv_keys(a.head_dim) / 32));
+hipError_t launch_causal_dkdv_join(const CausalArgs& a, int keys, const CausalItem* tiles, int n, hipStream_t s) {
+  const dim3 grid(n * (keys / 32));
   auto *dk = static_cast<bf16*>(a.dk), *dv = static_cast<bf16*>(a.dv);
   if (a.head_dim == 128)
-    hipLaunchKernelGGL((causal_dkdv_join_kernel<128>), grid, dim3(kThreads), 0, s, a.partial, tiles, a.kv_heads, a.scale,
-                       dk, dv);
+    hipLaunchKernelGGL((causal_dkdv_join_kernel<128>), grid, dim3(kThreads), 0, s, a.partial, tiles, keys, a.kv_heads,
+                       a.scale, dk, dv);
   else
-    hipLaunchKernelGGL((causal_dkdv_join_kernel<64>), grid, dim3(kThreads), 0, s, a.partial, tiles, a.kv_heads, a.scale,
-                       dk, dv);
+    hipLaunchKernelGGL((causal_dkdv_join_kernel<64>), grid, dim3(kThreads), 0, s, a.partial, tiles, keys, a.kv_heads,
+                       a.scale, dk, dv);
   return hipGetLastError();
 }
 

@@ -54,7 +54,7 @@ T2V_DEV void dq_step(uint32_t kbase, uint32_t vbase, uint32_t kr0, uint32_t kr1,
   for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
     for (int db = 0; db < DB; ++db) kt[hf][db] = read_rows_opnd<D>(kr0, kr1, kb + hf * 16, db);
-  const bool odd = MASK && take_nonfinite(kt);
+  const bool odd = MASK && (take_nonfinite(kt[0]) | take_nonfinite(kt[1]));
 #pragma unroll
   for (int hf = 0; hf < 2; ++hf)
 #pragma unroll

@@ -78,7 +78,7 @@ T2V_DEV void fwd_step(uint32_t kbase, uint32_t vbase0, uint32_t vbase1, int kb, 
   l_run += sum16(s);
   // P in bf16 for its product (at most 2^-9 of each weight); the row sum above took it in 32 bits.
   const bf16x8 pb[2] = {to_bf16x8(s, 0), to_bf16x8(s, 8)};
-  const bool odd = MASK && take_nonfinite(va);
+  const bool odd = MASK && (take_nonfinite(va[0]) | take_nonfinite(va[1]));
 #pragma unroll
   for (int hf = 0; hf < 2; ++hf)
 #pragma unroll

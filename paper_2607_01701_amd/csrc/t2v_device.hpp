@@ -445,4 +445,39 @@ T2V_DEV float half_min(float x) {
   return min_nan(__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1]));
 }
 
+// ------------------------------------------------------- infinities and NaN of operands
+
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+
+// The operand's finite elements, or its infinities and NaN (exponent bits all ones); zeros for the others.
+template <bool FINITE>
+T2V_DEV bf16x8 split_finite(const bf16x8& x) {
+  u32x4 w = __builtin_bit_cast(u32x4, x);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const unsigned odd = ((w[e] & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) |
+                         ((w[e] & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+    w[e] &= FINITE ? ~odd : odd;
+  }
+  return __builtin_bit_cast(bf16x8, w);
+}
+
+// Whether any lane's operands hold an infinity or a NaN, which are then replaced by zeros.
+template <int N>
+T2V_DEV bool take_nonfinite(bf16x8 (&x)[N]) {
+  u16x2 m = {0, 0};
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const u32x4 w = __builtin_bit_cast(u32x4, x[i]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[e] & 0x7FFF7FFFu));
+  }
+  const bool odd = __any(m[0] >= 0x7F80 || m[1] >= 0x7F80);
+  if (odd) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = split_finite<true>(x[i]);
+  }
+  return odd;
+}
+
 }  // namespace t2v

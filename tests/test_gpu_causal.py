@@ -62,9 +62,17 @@ SAME = [(EDGES, 2, 2, 128), (EDGES, 4, 1, 64), (EDGES, 6, 2, 128), ([0, 700, 0, 
         ([1000, 257], 5, 5, 128), ([640, 255], 16, 1, 64), ([333], 7, 1, 128), ([1500], 2, 1, 64)]
 
 
+@pytest.fixture(params=["", "wide", "narrow"])
+def tiles(request, monkeypatch):
+    """The forms that the library would choose, and each of them forced."""
+    for name in ("T2V_QTILE", "T2V_KVTILE"):
+        monkeypatch.setenv(name, request.param)
+    return request.param or "chosen"
+
+
 @pytest.mark.parametrize("lengths,H,Hk,D", SAME)
-def test_prompts(lengths, H, Hk, D):
-    log(f"case prompts {lengths} {H}/{Hk}x{D}")
+def test_prompts(lengths, H, Hk, D, tiles):
+    log(f"case prompts {lengths} {H}/{Hk}x{D} {tiles} tiles")
     p = pack(lengths, lengths, H, Hk, D, 1)
     c = cu(lengths)
     got = run(*p, c, None, D ** -0.5)
@@ -77,8 +85,8 @@ CHUNKS = [([1, 1, 1], [1, 77, 2049], 8, 2, 128), ([1] * 5, [64, 65, 3000, 1, 128
 
 
 @pytest.mark.parametrize("lq,lk,H,Hk,D", CHUNKS)
-def test_chunks_over_a_cache(lq, lk, H, Hk, D):
-    log(f"case chunks {lq} over {lk} {H}/{Hk}x{D}")
+def test_chunks_over_a_cache(lq, lk, H, Hk, D, tiles):
+    log(f"case chunks {lq} over {lk} {H}/{Hk}x{D} {tiles} tiles")
     p = pack(lq, lk, H, Hk, D, 2)
     got = run(*p, cu(lq), cu(lk), D ** -0.5)
     check(got, oracle.causal_attention(*(x.float().cpu().numpy() for x in p), cu(lq), cu(lk), D ** -0.5))
@@ -105,11 +113,11 @@ def test_slices_of_a_fused_projection():
 
 @pytest.mark.parametrize("what", [float("nan"), float("inf")])
 @pytest.mark.parametrize("D", [64, 128])
-def test_what_a_query_does_not_see_does_not_reach_it(what, D):
+def test_what_a_query_does_not_see_does_not_reach_it(what, D, tiles):
     """Later keys and values of infinities and NaN leave earlier rows' results as they are, and a query's own
     reach only the keys that it sees."""
-    log(f"case masked {what} D={D}")
-    n, at, H, Hk = 150, 70, 4, 2
+    log(f"case masked {what} D={D} {tiles} tiles")
+    n, at, H, Hk = 350, 70, 4, 2
     q, k, v, g = pack([n], [n], H, Hk, D, 6)
     clean = run(q, k, v, g, cu([n]), None, 0.1)
     k2, v2 = k.clone(), v.clone()
@@ -126,6 +134,12 @@ def test_what_a_query_does_not_see_does_not_reach_it(what, D):
     for name in ("dk", "dv"):
         assert torch.equal(got[name][at + 1:], clean[name][at + 1:]), name
         assert not torch.isfinite(got[name][:at + 1]).any(), name
+    # the last query, whose step is partial, sees every key
+    g3 = g.clone()
+    g3[n - 1, 0, 5] = what
+    got = run(q, k, v, g3, cu([n]), None, 0.1)
+    assert not torch.isfinite(got["dv"][:, 0, 5]).any() and torch.equal(got["dv"][:, 1], clean["dv"][:, 1])
+    assert torch.equal(got["dv"][:, 0, 6], clean["dv"][:, 0, 6])
 
 
 def test_autograd_equals_the_calls_and_repeats_bitwise():
@@ -139,7 +153,7 @@ def test_autograd_equals_the_calls_and_repeats_bitwise():
         assert torch.equal(x, a[name]), name
 
 
-def test_checked_library_gives_the_same():
+def test_checked_library_gives_the_same(tiles):
     for lq, lk, H, Hk, D in [*CHUNKS, *((n, n, *r) for n, *r in SAME)]:
         log(f"case checked {lq} {lk} {H}/{Hk}x{D}")
         p = pack(lq, lk, H, Hk, D, 8)
