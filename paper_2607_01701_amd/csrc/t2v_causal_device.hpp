@@ -35,6 +35,14 @@ T2V_DEV LaneRow lane_row(const CausalItem& it, int group, int wave, int lane) {
   return {row < nrows, pr.query + it.lk - it.lq, it.head * group + pr.head, static_cast<int64_t>(it.qrow0) + pr.query};
 }
 
+// What rounding to bf16 took from 8 values: hi + lo holds 16 bits of them.
+T2V_DEV bf16x8 rest_bf16x8(const f32x16& x, int base, const bf16x8& hi) {
+  bf16x8 r;
+#pragma unroll
+  for (int t = 0; t < 8; ++t) r[t] = static_cast<bf16>(x[base + t] - static_cast<float>(hi[t]));
+  return r;
+}
+
 // The operand with only contraction index kk (0..15) kept: element t of a lane holds index
 // 8 (t / 4) + 4 G + t % 4, as read_rows_opnd and the packed scores have it.
 T2V_DEV bf16x8 only_index(const bf16x8& x, int kk, int G) {

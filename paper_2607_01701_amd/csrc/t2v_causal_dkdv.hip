@@ -73,7 +73,7 @@ T2V_DEV void dkdv_step(uint32_t qbase, uint32_t gbase, uint32_t qr0, uint32_t qr
     s[r] = sees ? p : 0.0f;
     dp[r] = sees ? p * dp[r] : 0.0f;
   }
-  // P and dS in bf16 for their products, the sums in 32 bits.
+  // P and dS in bf16 for their products, the sums in 32 bits; in masked steps with the rest, as in the forward kernel.
   bf16x8 pb[2] = {to_bf16x8(s, 0), to_bf16x8(s, 8)};
   bf16x8 sb[2] = {to_bf16x8(dp, 0), to_bf16x8(dp, 8)};
   if constexpr (MASK) {  // the operands of the sums only now: read ahead, they and the tests below would spill
@@ -98,7 +98,15 @@ T2V_DEV void dkdv_step(uint32_t qbase, uint32_t gbase, uint32_t qr0, uint32_t qr
   for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
     for (int db = 0; db < DB; ++db) dva[db] = mfma(bg[hf][db], pb[hf], dva[db]);
-  if constexpr (MASK) fence();
+  if constexpr (MASK) {
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      const bf16x8 rest = rest_bf16x8(s, 8 * hf, pb[hf]);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) dva[db] = mfma(bg[hf][db], rest, dva[db]);
+    }
+    fence();
+  }
 #pragma unroll
   for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
@@ -109,6 +117,12 @@ T2V_DEV void dkdv_step(uint32_t qbase, uint32_t gbase, uint32_t qr0, uint32_t qr
 #pragma unroll
     for (int db = 0; db < DB; ++db) dka[db] = mfma(bq[hf][db], sb[hf], dka[db]);
   if constexpr (MASK) {
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      const bf16x8 rest = rest_bf16x8(dp, 8 * hf, sb[hf]);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) dka[db] = mfma(bq[hf][db], rest, dka[db]);
+    }
     if (odd_g) add_nonfinite(dva, pb, G, read_g, sees);
     if (odd_q) add_nonfinite(dka, sb, G, read_q, sees);
   }

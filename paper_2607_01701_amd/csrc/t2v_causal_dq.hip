@@ -42,12 +42,17 @@ T2V_DEV void dq_step(uint32_t kbase, uint32_t vbase, uint32_t kr0, uint32_t kr1,
     const float ds = __builtin_amdgcn_exp2f(fmaf(s[r], c, nl2)) * (dp[r] + ndl);
     s[r] = MASK && (r >> 2) * 8 + G * 4 + (r & 3) > lim ? 0.0f : ds;
   }
-  // dS in bf16 for its product, the sums in 32 bits.
+  // dS in bf16 for its product, the sums in 32 bits; in masked steps with the rest, as P in the forward kernel.
   bf16x8 sb[2] = {to_bf16x8(s, 0), to_bf16x8(s, 8)};
-  if constexpr (MASK) {  // the K operands only now: read ahead, they and the test below would spill
-    pin(sb[0]);
-    pin(sb[1]);
-    fence();
+  bf16x8 rest[2];
+  if constexpr (MASK) {
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      rest[hf] = rest_bf16x8(s, 8 * hf, sb[hf]);
+      pin(sb[hf]);
+      pin(rest[hf]);
+    }
+    fence();  // the K operands only now: read ahead, they and the test below would spill
   }
   bf16x8 kt[2][DB];
 #pragma unroll
@@ -60,6 +65,10 @@ T2V_DEV void dq_step(uint32_t kbase, uint32_t vbase, uint32_t kr0, uint32_t kr1,
 #pragma unroll
     for (int db = 0; db < DB; ++db) dqa[db] = mfma(kt[hf][db], sb[hf], dqa[db]);
   if constexpr (MASK) {
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+      for (int db = 0; db < DB; ++db) dqa[db] = mfma(kt[hf][db], rest[hf], dqa[db]);
     if (odd)
       add_nonfinite(dqa, sb, G, [&](int half, int db) { return read_rows_opnd<D>(kr0, kr1, kb + half, db); },
                           [&](int kk, int) { return kk <= lim; });
