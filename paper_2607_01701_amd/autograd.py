@@ -6,7 +6,22 @@ from __future__ import annotations
 
 import numpy as np
 
-from ._lib import _cu_array, attn_bwd, attn_fwd, causal_attn_bwd, causal_attn_fwd
+from ._lib import _cu_array, _stream_handle, attn_bwd, attn_fwd, causal_attn_bwd, causal_attn_fwd
+
+
+def check_capture(ctx):
+    """Refuses to record, into a graph, a call on a leaf whose gradient node an earlier eager call made on another stream
+    and that call's autograd graph still holds: the backward pass would make that stream part of the capture, which
+    ends the process when the capture does. Called in a Function's forward; costs about 1 us."""
+    import torch
+    stream = _stream_handle(None)
+    for node, _ in ctx.next_functions:
+        if node is None or type(node).__name__ != "AccumulateGrad":
+            continue
+        first = node.metadata.setdefault("t2v_stream", stream)  # lives as long as the node
+        if first != stream and torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("a captured call takes the gradient of a leaf tensor that an eager autograd graph, made on "
+                               "another stream, still holds: drop that graph's outputs before the capture")
 
 
 def _function(attn_fwd, attn_bwd):
@@ -15,6 +30,7 @@ def _function(attn_fwd, attn_bwd):
     class _VarlenAttention(torch.autograd.Function):
         @staticmethod
         def forward(ctx, q, k, v, cu_seqlens, scale, cu_seqlens_k):
+            check_capture(ctx)
             out, lse = attn_fwd(q, k, v, cu_seqlens, scale, cu_seqlens_k=cu_seqlens_k)
             ctx.save_for_backward(q, k, v, out, lse)
             ctx.cu, ctx.cu_k, ctx.scale = cu_seqlens, cu_seqlens_k, scale

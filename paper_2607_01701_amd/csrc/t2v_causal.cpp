@@ -188,6 +188,7 @@ double causal_time(CausalKernel kind, const CausalShape& a, int block, int stage
   slots *= a.kv_heads;
   if (items != nullptr) *items = n;
   if (longest != nullptr) *longest = most;
+  if (n == 0) return 0.0;
   if (slots > max_slots) return HUGE_VAL;
   // An item's speed follows from how many share its CU.
   const double per_cu = static_cast<double>(cost.workers) / cost.cus;

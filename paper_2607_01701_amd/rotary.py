@@ -8,6 +8,7 @@ import math
 import numpy as np
 
 from . import _lib
+from .autograd import check_capture
 
 LAYOUTS = {"half": 0, "interleaved": 1}
 SCALINGS = (None, "linear", "ntk", "yarn")
@@ -114,6 +115,7 @@ def _function():
     class _Rotary(torch.autograd.Function):
         @staticmethod
         def forward(ctx, q, k, positions, freqs, layout, sections, mscale):
+            check_capture(ctx)
             ctx.save_for_backward(positions)
             ctx.args = (freqs, layout, sections, mscale)
             ctx.set_materialize_grads(False)
