@@ -52,105 +52,121 @@ void pieces_of(CausalKernel kind, int n, int chunk, int* count, int* step) {
 CausalList build_causal_list(CausalKernel kind, const CausalShape& a, int block, int stage, int order, int chunk,
                              double fixed, int workers) {
   CausalList out;
-  struct Group {
-    int seq, head;
+  // The items of one key head of a sequence, the same for each of its key heads but for head and slots.
+  struct Sequence {
+    size_t first;  // in `items`
+    int n, slots;
+    int64_t slot0;
     double longest, cost;
-    std::vector<CausalItem> items;
   };
-  std::vector<Group> groups;
+  std::vector<CausalItem> items;
+  std::vector<Sequence> seqs;
   size_t n = 0;
   for (int s = 0; s < a.nseq; ++s) {
     const Loops l = loops_of(kind, a, s, block, stage);
     const int tiles = l.tiles();
     if (tiles == 0) continue;
-    for (int h = 0; h < a.kv_heads; ++h) {
-      Group g{s, h, 0.0, 0.0, {}};
-      for (int i = 0; i < tiles; ++i) {
-        // Longest loop first: rows from the last tile, keys from the first.
-        const int t = order == T2V_ORDER_NATURAL || kind == kCausalDkdv ? i : tiles - 1 - i;
-        const int len = l.length(t);
-        int count = 1, step = len;
-        pieces_of(kind, len, chunk, &count, &step);
-        CausalItem it{a.cu_q[s], l.lq, a.cu_k[s], l.lk, t * block, h, 0, len, -1, 1, 0, 0};
-        if (count > 1) {
-          CausalItem r = it;
-          r.slot = static_cast<int32_t>(out.slots);
-          r.pieces = count;
-          r.end = 0;
+    Sequence q{items.size(), 0, 0, out.slots, 0.0, 0.0};
+    for (int i = 0; i < tiles; ++i) {
+      // Longest loop first: rows from the last tile, keys from the first.
+      const int t = order == T2V_ORDER_NATURAL || kind == kCausalDkdv ? i : tiles - 1 - i;
+      const int len = l.length(t);
+      int count = 1, step = len;
+      pieces_of(kind, len, chunk, &count, &step);
+      CausalItem it{a.cu_q[s], l.lq, a.cu_k[s], l.lk, t * block, 0, 0, len, -1, count, 0, 0};
+      for (int p = 0; p < count; ++p) {
+        it.begin = p * step;
+        it.end = std::min(len, (p + 1) * step);
+        if (count > 1) it.slot = q.slots++;
+        items.push_back(it);
+        const double c = fixed + (it.end - it.begin);
+        q.cost += c;
+        q.longest = std::max(q.longest, c);
+      }
+    }
+    q.n = static_cast<int>(items.size() - q.first);
+    n += static_cast<size_t>(q.n) * a.kv_heads;
+    out.slots += static_cast<int64_t>(q.slots) * a.kv_heads;
+    seqs.push_back(q);
+  }
+  auto item_of = [&](const Sequence& q, int head, size_t i) {
+    CausalItem it = items[q.first + i];
+    it.head = head;
+    if (it.slot >= 0) it.slot += static_cast<int32_t>(q.slot0 + static_cast<int64_t>(q.slots) * head);
+    return it;
+  };
+  for (const Sequence& q : seqs)
+    for (int h = 0; q.slots > 0 && h < a.kv_heads; ++h)
+      for (int i = 0; i < q.n; i += items[q.first + i].pieces)
+        if (items[q.first + i].pieces > 1) {
+          CausalItem r = item_of(q, h, i);
+          r.begin = r.end = 0;
           out.reduce.push_back(r);
         }
-        for (int p = 0; p < count; ++p) {
-          it.begin = p * step;
-          it.end = std::min(len, (p + 1) * step);
-          if (count > 1) {
-            it.slot = static_cast<int32_t>(out.slots++);
-            it.pieces = count;
-          }
-          g.items.push_back(it);
-          const double c = fixed + (it.end - it.begin);
-          g.cost += c;
-          g.longest = std::max(g.longest, c);
-        }
-      }
-      n += g.items.size();
-      groups.push_back(std::move(g));
-    }
-  }
   out.items.reserve(n);
   if (order == T2V_ORDER_NATURAL) {
-    for (const Group& g : groups) out.items.insert(out.items.end(), g.items.begin(), g.items.end());
+    for (const Sequence& q : seqs)
+      for (int h = 0; h < a.kv_heads; ++h)
+        for (int i = 0; i < q.n; ++i) out.items.push_back(item_of(q, h, i));
     return out;
   }
   // Workgroup b runs on die b % 8. A (sequence, key head) goes to one die, whose L2 then serves its keys
   // or queries to all its tiles, longest tiles first; groups by their longest loop, each to the
   // least loaded die, and on to the next when that die has an even share of the cost.
-  std::stable_sort(groups.begin(), groups.end(), [](const Group& x, const Group& y) { return x.longest > y.longest; });
+  std::vector<int> by_length(seqs.size());
+  for (size_t i = 0; i < seqs.size(); ++i) by_length[i] = static_cast<int>(i);
+  std::stable_sort(by_length.begin(), by_length.end(), [&](int x, int y) { return seqs[x].longest > seqs[y].longest; });
   double total = 0.0;
-  for (const Group& g : groups) total += g.cost;
+  for (const Sequence& q : seqs) total += q.cost * a.kv_heads;
   const double share = total / kNumXcd * (1.0 + 1e-9);
-  std::vector<std::vector<CausalItem>> q(kNumXcd);
-  std::vector<double> load(kNumXcd, 0.0);
-  for (const Group& g : groups) {
-    int x = static_cast<int>(std::min_element(load.begin(), load.end()) - load.begin());
-    for (const CausalItem& it : g.items) {
-      const double c = fixed + (it.end - it.begin);
-      if (load[x] + 0.5 * c > share) x = static_cast<int>(std::min_element(load.begin(), load.end()) - load.begin());
-      q[x].push_back(it);
-      load[x] += c;
+  struct Ref {
+    int32_t length, seq, head, item;
+  };
+  std::vector<Ref> q[kNumXcd];
+  double load[kNumXcd] = {};
+  for (int s : by_length)
+    for (int h = 0; h < a.kv_heads; ++h) {
+      int x = static_cast<int>(std::min_element(load, load + kNumXcd) - load);
+      for (int i = 0; i < seqs[s].n; ++i) {
+        const CausalItem& it = items[seqs[s].first + i];
+        const double c = fixed + (it.end - it.begin);
+        if (load[x] + 0.5 * c > share) x = static_cast<int>(std::min_element(load, load + kNumXcd) - load);
+        q[x].push_back({it.end - it.begin, s, h, i});
+        load[x] += c;
+      }
     }
-  }
   // With few rounds of items the longest go first, whatever their group: a long one that starts in the last round would
   // outlast the others. With more, only the shortest two rounds are kept for the end, and the others stay with their
   // group, whose keys or queries are in the die's L2.
   const size_t per_die = static_cast<size_t>(std::max(workers, 1) + kNumXcd - 1) / kNumXcd;
-  auto longer = [](const CausalItem& x, const CausalItem& y) { return x.end - x.begin > y.end - y.begin; };
+  auto longer = [](const Ref& x, const Ref& y) { return x.length > y.length; };
   for (auto& l : q) {
-    std::vector<CausalItem> sorted = l;
-    std::stable_sort(sorted.begin(), sorted.end(), longer);
-    const size_t last = 2 * per_die;
     if (l.size() < kGroupedRounds * per_die) {
-      l.swap(sorted);
-    } else {
-      const int32_t cut = sorted[sorted.size() - last].end - sorted[sorted.size() - last].begin;
-      std::stable_partition(l.begin(), l.end(), [cut](const CausalItem& x) { return x.end - x.begin > cut; });
-      std::stable_sort(std::find_if(l.begin(), l.end(), [cut](const CausalItem& x) { return x.end - x.begin <= cut; }),
-                       l.end(), longer);
+      std::stable_sort(l.begin(), l.end(), longer);
+      continue;
     }
+    std::vector<int32_t> lengths;
+    for (const Ref& r : l) lengths.push_back(r.length);
+    std::nth_element(lengths.begin(), lengths.begin() + 2 * per_die - 1, lengths.end());
+    const int32_t cut = lengths[2 * per_die - 1];
+    const auto last = std::stable_partition(l.begin(), l.end(), [cut](const Ref& x) { return x.length > cut; });
+    std::stable_sort(last, l.end(), longer);
   }
   // One list: position b takes the next item of die b % 8, or, when that die has no more, the last
   // (shortest) item of the die with the most left, so that no position is empty.
-  std::vector<size_t> next(kNumXcd, 0);
+  size_t next[kNumXcd] = {};
   for (size_t b = 0; b < n; ++b) {
-    const size_t x = b % kNumXcd;
+    size_t x = b % kNumXcd;
+    Ref r;
     if (next[x] < q[x].size()) {
-      out.items.push_back(q[x][next[x]++]);
-      continue;
+      r = q[x][next[x]++];
+    } else {
+      for (size_t y = 0; y < kNumXcd; ++y)
+        if (q[y].size() - next[y] > q[x].size() - next[x]) x = y;
+      r = q[x].back();
+      q[x].pop_back();
     }
-    size_t most = 0;
-    for (size_t y = 1; y < kNumXcd; ++y)
-      if (q[y].size() - next[y] > q[most].size() - next[most]) most = y;
-    out.items.push_back(q[most].back());
-    q[most].pop_back();
+    out.items.push_back(item_of(seqs[r.seq], r.head, r.item));
   }
   return out;
 }

@@ -6,7 +6,8 @@ import pytest
 import torch
 
 import oracle
-from paper_2607_01701_amd import _lib, causal_attn_bwd, causal_attn_fwd, use_checked_library, varlen_causal_attention
+from paper_2607_01701_amd import (T2VError, _lib, causal_attn_bwd, causal_attn_fwd, use_checked_library,
+                                  varlen_causal_attention)
 
 from gpu_util import log
 
@@ -174,3 +175,20 @@ def test_empty_calls():
     assert (got["out"] == 0).all() and (got["dq"] == 0).all() and torch.isneginf(got["lse"]).all()
     run(z, z[:, :2], z[:, :2], z, cu([0]), None, 0.1)
     assert _lib.T2V_OK == 0
+
+
+def test_checked_library_reports_rows_out_of_bounds(tiles, monkeypatch):
+    """With a row taken off every bound, correct kernels report their sequences' last rows: each kernel checks its copies."""
+    monkeypatch.setenv("T2V_CHECK_CANARY", "1")
+    for lq, lk, H, Hk, D in (([70], [70], 4, 2, 128), ([300], [300], 2, 2, 64), ([1], [90], 4, 2, 64)):
+        log(f"case canary {lq} {lk} {tiles} tiles")
+        q, k, v, g = pack(lq, lk, H, Hk, D, 9)
+        out, lse = causal_attn_fwd(q, k, v, cu(lq), 0.1, cu_seqlens_k=cu(lk))
+        with use_checked_library():
+            with pytest.raises(T2VError, match="causal forward kernel"):
+                causal_attn_fwd(q, k, v, cu(lq), 0.1, cu_seqlens_k=cu(lk))
+            with pytest.raises(T2VError, match="causal dK/dV kernel"):
+                causal_attn_bwd(q, k, v, out, lse, g, cu(lq), 0.1, cu_seqlens_k=cu(lk))
+    monkeypatch.delenv("T2V_CHECK_CANARY")
+    with use_checked_library():
+        causal_attn_fwd(q, k, v, cu(lq), 0.1, cu_seqlens_k=cu(lk))
