@@ -62,14 +62,20 @@ T2V_DEV void fwd_step(uint32_t kbase, uint32_t vbase0, uint32_t vbase1, int kb, 
     for (int r = 0; r < 16; ++r) s[r] = (r >> 2) * 8 + G * 4 + (r & 3) <= lim ? s[r] : -kInf;
   }
   const float mblk = half_max(max16(s)) * c;  // largest scaled score of this step
-  if (__any(mblk > m_run + kTau)) {
+  if (__builtin_expect(__any(mblk > m_run + kTau), 0)) {
     // Each row by itself, so that no row's rounding depends on its neighbours in the tile.
     const float mn = mblk > m_run + kTau ? mblk : m_run;
     // A row that has seen no key (or only scores of -inf) keeps a reference of -inf: its sums are zero.
     const float alpha = __builtin_amdgcn_exp2f(m_run - (mn == -kInf ? 0.0f : mn));
     l_run *= alpha;
 #pragma unroll
-    for (int db = 0; db < DB; ++db) o[db] *= alpha;
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        float x = o[db][r] * alpha;
+        pin(x);  // in its place: a new tuple would be copied back in every stage (head_dim 64: 31 moves beside 166 others)
+        o[db][r] = x;
+      }
     m_run = mn;
   }
   const float nm = m_run == -kInf ? 0.0f : -m_run;
