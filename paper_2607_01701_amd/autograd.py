@@ -9,28 +9,38 @@ import numpy as np
 from ._lib import _cu_array, _stream_handle, attn_bwd, attn_fwd, causal_attn_bwd, causal_attn_fwd
 
 
-def check_capture(ctx):
-    """Refuses to record, into a graph, a call on a leaf whose gradient node an earlier eager call made on another stream
-    and that call's autograd graph still holds: the backward pass would make that stream part of the capture, which
-    ends the process when the capture does. Called in a Function's forward; costs about 1 us."""
-    import torch
+def _leaves(ctx):
+    return [n for n, _ in ctx.next_functions if n is not None and type(n).__name__ == "AccumulateGrad"]
+
+
+def note_leaves(ctx):
+    """Notes, in a Function's forward, which stream first used a leaf's gradient node (torch keeps one as long as any
+    autograd graph holds it, and its stream with it). Costs about 1 us."""
     stream = _stream_handle(None)
-    for node, _ in ctx.next_functions:
-        if node is None or type(node).__name__ != "AccumulateGrad":
-            continue
-        first = node.metadata.setdefault("t2v_stream", stream)  # lives as long as the node
-        if first != stream and torch.cuda.is_current_stream_capturing():
-            raise RuntimeError("a captured call takes the gradient of a leaf tensor that an eager autograd graph, made on "
-                               "another stream, still holds: drop that graph's outputs before the capture")
+    for node in _leaves(ctx):
+        node.metadata.setdefault("t2v_stream", stream)  # lives as long as the node
 
 
-def _function(attn_fwd, attn_bwd):
+def check_capture(ctx):
+    """Refuses, in a Function's backward, to record into a graph the gradient of a leaf whose node an eager call made on
+    another stream and that call's autograd graph still holds: torch would make that stream part of the capture, which
+    ends the process when the capture does."""
+    import torch
+    if not torch.cuda.is_current_stream_capturing():
+        return
+    stream = _stream_handle(None)
+    if any(node.metadata.get("t2v_stream", stream) != stream for node in _leaves(ctx)):
+        raise RuntimeError("a captured backward pass takes the gradient of a leaf tensor that an eager autograd graph, made "
+                           "on another stream, still holds: drop that graph's outputs before the capture")
+
+
+def _function(attn_fwd, attn_bwd, wrap=lambda f: f):
     import torch
 
     class _VarlenAttention(torch.autograd.Function):
         @staticmethod
         def forward(ctx, q, k, v, cu_seqlens, scale, cu_seqlens_k):
-            check_capture(ctx)
+            note_leaves(ctx)
             out, lse = attn_fwd(q, k, v, cu_seqlens, scale, cu_seqlens_k=cu_seqlens_k)
             ctx.save_for_backward(q, k, v, out, lse)
             ctx.cu, ctx.cu_k, ctx.scale = cu_seqlens, cu_seqlens_k, scale
@@ -42,9 +52,11 @@ def _function(attn_fwd, attn_bwd):
             return out, lse
 
         @staticmethod
+        @wrap
         def backward(ctx, dout, _dlse):
             if dout is None:  # nothing depends on out
                 return None, None, None, None, None, None
+            check_capture(ctx)
             q, k, v, out, lse = ctx.saved_tensors
             dq, dk, dv = attn_bwd(q, k, v, out, lse, dout.contiguous(), ctx.cu, ctx.scale, cu_seqlens_k=ctx.cu_k)
             return dq, dk, dv, None, None, None
@@ -70,10 +82,12 @@ def varlen_attention(q, k, v, cu_seqlens, scale: float, cu_seqlens_k=None):
 
 def varlen_causal_attention(q, k, v, cu_seqlens, scale: float, cu_seqlens_k=None):
     """Causal attention with grouped heads and autograd: q [Tq, H, D], k, v [Tk, Hk, D] as in causal_attn_fwd.
-    Returns (out, lse); gradients flow to q, k and v (lse is not differentiated)."""
+    Returns (out, lse); gradients flow to q, k and v (lse is not differentiated), and have none of their own: asked for,
+    they raise."""
     global _CAUSAL_FN
     if _CAUSAL_FN is None:
-        _CAUSAL_FN = _function(causal_attn_fwd, causal_attn_bwd)
+        from torch.autograd.function import once_differentiable
+        _CAUSAL_FN = _function(causal_attn_fwd, causal_attn_bwd, once_differentiable)
     cu = np.array(_cu_array(cu_seqlens), copy=True)
     ck = None if cu_seqlens_k is None else np.array(_cu_array(cu_seqlens_k), copy=True)
     return _CAUSAL_FN.apply(q, k, v, cu, float(scale), ck)

@@ -8,7 +8,7 @@ import math
 import numpy as np
 
 from . import _lib
-from .autograd import check_capture
+from .autograd import check_capture, note_leaves
 
 LAYOUTS = {"half": 0, "interleaved": 1}
 SCALINGS = (None, "linear", "ntk", "yarn")
@@ -61,7 +61,7 @@ def rotary_apply(q, k, positions, freqs, layout: str = "half", sections=None, ms
     first = q if q is not None else k
     if first is None:
         raise ValueError("q and k are both None")
-    if first.dim() != 3:
+    if any(x is not None and x.dim() != 3 for x in (q, k)):
         raise ValueError("q and k must be [tokens, heads, head_dim]")
     if layout not in LAYOUTS:
         raise ValueError(f"layout must be one of {tuple(LAYOUTS)}, got {layout!r}")
@@ -114,21 +114,23 @@ def _function():
 
     class _Rotary(torch.autograd.Function):
         @staticmethod
-        def forward(ctx, q, k, positions, freqs, layout, sections, mscale):
-            check_capture(ctx)
+        def forward(ctx, q, k, positions, freqs, layout, sections, mscale, inverse):
+            note_leaves(ctx)
             ctx.save_for_backward(positions)
-            ctx.args = (freqs, layout, sections, mscale)
+            ctx.args = (freqs, layout, sections, mscale, not inverse)
             ctx.set_materialize_grads(False)
-            return rotary_apply(q, k, positions, freqs, layout, sections, mscale)
+            return rotary_apply(q, k, positions, freqs, layout, sections, mscale, inverse)
 
         @staticmethod
         def backward(ctx, dq, dk):
             if dq is None and dk is None:
-                return (None,) * 7
+                return (None,) * 8
+            check_capture(ctx)
             (positions,) = ctx.saved_tensors
-            # R(angle) transposed is R(-angle).
+            # R(angle) transposed is R(-angle); with create_graph, the turn back has a gradient of its own.
             dq, dk = (x if x is None or _rows(x) else x.contiguous() for x in (dq, dk))
-            return (*rotary_apply(dq, dk, positions, *ctx.args, inverse=True), None, None, None, None, None)
+            turn = _Rotary.apply if torch.is_grad_enabled() else rotary_apply
+            return (*turn(dq, dk, positions, *ctx.args), None, None, None, None, None, None)
 
     return _Rotary
 
@@ -152,4 +154,4 @@ def rotary(q, k, positions, freqs, layout: str = "half", sections=None, mscale: 
     if _FN is None:
         _FN = _function()
     f = np.array(freqs, dtype=np.float64, copy=True)
-    return _FN.apply(q, k, positions, f, layout, None if sections is None else tuple(sections), float(mscale))
+    return _FN.apply(q, k, positions, f, layout, None if sections is None else tuple(sections), float(mscale), False)

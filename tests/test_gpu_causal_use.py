@@ -141,8 +141,8 @@ def test_captured_calls_replay(lq, lk, H, Hk, D):
 
 
 def test_captured_autograd():
-    """A training step in a graph; and the refusal to record one while an eager graph of the same leaves, made on another
-    stream, is alive (its backward pass would end the process)."""
+    """A training step in a graph; and, while an eager graph of the same leaves, made on another stream, is alive, a forward
+    pass in one, and the refusal to record a backward pass (it would end the process)."""
     log("case captured autograd")
     n, H, Hk, D = [200, 30], 4, 2, 64
     q, k, v = (rand(230, h, D, seed=h).requires_grad_(True) for h in (H, Hk, Hk))
@@ -161,15 +161,23 @@ def test_captured_autograd():
     s.wait_stream(torch.cuda.current_stream())
     torch.cuda.synchronize()
     with torch.cuda.stream(s):
-        for call in (step, lambda: t2v.varlen_causal_attention(q.detach(), k.detach(), v, cu(n), 0.1)):
+        with torch.cuda.graph(forward := torch.cuda.CUDAGraph(), stream=s):
+            out = step()
+        for leaves in ((q, k, v), (q, k)):  # refused by the attention, which meets v first, and by the rotary positions
+            v2 = v if len(leaves) == 3 else v.detach()
             with pytest.raises(RuntimeError, match="eager autograd graph"):
                 with torch.cuda.graph(torch.cuda.CUDAGraph(), stream=s):
-                    call()
+                    q2, k2 = t2v.rotary(q, k, pos, freqs)
+                    torch.autograd.grad(t2v.varlen_causal_attention(q2, k2, v2, cu(n), 0.1)[0], leaves, g)
+        forward.replay()
+        s.synchronize()
+        assert torch.equal(out, eager)
+        del out
         again = step()  # eager calls on any stream are fine
         for a, b in zip(torch.autograd.grad(again, (q, k, v), g), want):
             s.synchronize()
             assert torch.equal(a, b)
-    del eager, again
+    del eager, again, q2, k2
     torch.cuda.synchronize()
     with torch.cuda.stream(s):
         graph = torch.cuda.CUDAGraph()
@@ -183,6 +191,24 @@ def test_captured_autograd():
         for a, b in zip(torch.autograd.grad(step(), (q, k, v), g), want):
             torch.cuda.synchronize()
             assert torch.equal(a, b)
+
+
+def test_second_derivatives():
+    """Those of rotary positions, which are linear: of <R x, y> y's. The attention's are refused."""
+    log("case second derivatives")
+    n = [30]
+    x, y = (rand(30, 2, 64, seed=i).requires_grad_(True) for i in (1, 2))
+    freqs, _ = t2v.rotary_frequencies(32)
+    turned, _ = t2v.rotary(x, None, positions(n), freqs)
+    (dx,) = torch.autograd.grad(turned, x, y, create_graph=True)
+    w = rand(30, 2, 64, seed=3)
+    (dy,) = torch.autograd.grad(dx, y, w)
+    torch.cuda.synchronize()
+    assert torch.equal(dy, t2v.rotary_apply(w, None, positions(n), freqs)[0])
+    out, _ = t2v.varlen_causal_attention(x, x.detach(), x.detach(), cu(n), 0.1)
+    (dx,) = torch.autograd.grad(out, x, y, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        dx.float().sum().backward()
 
 
 def test_other_streams_and_threads():
