@@ -225,33 +225,42 @@ constexpr int64_t kCausalMaxWorkspace = int64_t(1) << 30;
 
 enum CausalForm { kFew, kNarrow, kWide };
 
-// Times measured on MI355X (microseconds; see CausalCost): a key of a forward item 30 ns at head_dim 128 (256 rows, or
-// 128 with a second workgroup beside it) and 31 at 64 (128 rows, three workgroups), of a dQ item 42 and 40; a narrow
-// tile with the CU to itself takes about half, and the kernel of few rows 9 ns a key. Where each key is read
-// by one tile only (`once`: single tokens) the memory's 5 TB/s bound the loop instead. A dK/dV item takes 1.75 us for
-// 32 queries and 256 keys (wide) or 2.1 for 64 and 128 (narrow) at head_dim 128, 5.1 for 128 and 256 at 64.
-// Loads, stores and filling the pipeline: `fixed`. A join costs a launch (and a second call that brings the
-// workspace), 0.1 us a piece, and the pieces' results are written and read at 4.5 TB/s.
+// Times measured on MI355X (microseconds; see CausalCost), with all CUs busy and with one item a CU on few of them.
+// A key of a forward item: 29.5 ns at head_dim 128 with 256 rows (wide), 30.3 with 128 and a second workgroup beside it
+// (narrow), 30 at 64 (128 rows, three workgroups); alone 22, 16 and 12. Of a dQ item 40, 41.5 and 36, alone 26, 20 and 12.
+// So wide tiles are faster where all CUs are busy for many rounds (running 20,280 tokens, 24 heads over 8: 2,315 us
+// against 2,378), narrow ones where the few items' ends count (4 x 1,280 tokens, 12 heads: 36 us against 42). The kernel of few
+// rows 9 ns a key. Where each key is read by one tile only (`once`: single tokens) the memory's 5 TB/s bound
+// the loop instead, and an item that fills its pipeline leaves them to the others. A dK/dV item: 1.75 us (alone 1.25) for 32 queries and 256 keys (wide) or 2.2 (1.6) for 64 and 128
+// (narrow) at head_dim 128, 4.1 (2.85) for 128 and 256 at 64.
+// Loads, stores and filling the pipeline: `fixed`. A join costs a launch, 0.3 us a piece, and reads the pieces' results
+// at 5.5 TB/s (their writes run beside other items' loops, mostly).
 CausalCost causal_cost(CausalKernel kind, int head_dim, CausalForm form, bool once, int ncu) {
   CausalCost c{};
   const bool d64 = head_dim == 64;
   c.cus = std::max(1, ncu);
   c.join = 6.0;
-  c.piece = 0.1;
-  c.byte = 2.0 / 4.5e6;
+  c.piece = 0.3;
+  c.byte = 1.5 / 5.5e6;
   if (kind == kCausalDkdv) {
     c.workers = c.cus;
-    c.unit = c.alone = d64 ? 5.1 : form == kWide ? 1.75 : 2.1;
-    c.fixed = d64 ? 6.0 : form == kWide ? 12.0 : 10.0;
+    c.unit = d64 ? 4.1 : form == kWide ? 1.75 : 2.2;
+    c.alone = d64 ? 2.85 : form == kWide ? 1.25 : 1.6;
+    c.fixed = d64 ? 7.0 : form == kWide ? 12.0 : 10.0;
     c.slot_row = 8 * head_dim;
     return c;
   }
   c.workers = c.cus * (form == kWide ? 1 : form == kFew ? (d64 ? 2 : 1) : d64 ? 3 : 2);
-  c.unit = kind == kCausalFwd ? (d64 ? 0.031 : 0.030) : (d64 ? 0.040 : 0.042);
-  c.alone = form == kWide ? c.unit : form == kFew ? 0.009 : 0.55 * c.unit;
+  const bool fwd = kind == kCausalFwd;
+  c.unit = d64 ? (fwd ? 0.030 : 0.036) : form == kWide ? (fwd ? 0.0295 : 0.040) : fwd ? 0.0303 : 0.0415;
+  c.alone = d64 ? 0.012 : form == kWide ? (fwd ? 0.022 : 0.026) : fwd ? 0.016 : 0.020;
   c.fixed = form == kFew ? 3.0 : 4.0;
-  if (form == kFew) c.unit = c.alone;
-  if (once) c.unit = std::max(c.unit, 4.0 * head_dim * c.workers / 5e6);
+  if (form == kFew) c.unit = c.alone = 0.009;
+  const double bound = 4.0 * head_dim * c.workers / 5e6;
+  if (once && bound > c.unit) {
+    c.fixed *= c.unit / bound;
+    c.unit = bound;
+  }
   c.slot_row = 4 * (head_dim + (kind == kCausalFwd ? 2 : 0));
   return c;
 }
@@ -281,7 +290,7 @@ CausalList causal_plan(const TileRule& r, const CausalShape& a, int head_dim, in
   if (form == kNarrow && r.forced == 0 && !r.narrow_always && (kv || most_rows > r.narrow)) {
     double wide_time = 0.0;
     const int wide_chunk = choose(kWide, &wide_time);
-    if (wide_time <= (kv ? 1.0 : 1.04) * time) {  // wide tiles of rows stage a key once for twice the rows
+    if (wide_time <= time) {
       form = kWide;
       chunk = wide_chunk;
     }
