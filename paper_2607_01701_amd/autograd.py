@@ -1,5 +1,5 @@
-"""PyTorch autograd wrapper over the C ABI: the forward calls t2v_attn_fwd (or _qk), the
-backward t2v_attn_bwd (or _qk) with the saved out and lse, so a training step (the DiT
+"""PyTorch autograd wrapper over the C ABI: the forward calls t2v_attn_fwd (or _qk, or t2v_causal_fwd), the
+backward t2v_attn_bwd (or _qk, or t2v_causal_bwd) with the saved out and lse, so a training step (the DiT
 forward and backward of Fig. 1) can use the library through loss.backward(). Argument
 marshalling only; every step runs in the HIP library."""
 from __future__ import annotations
@@ -34,8 +34,20 @@ def check_capture(ctx):
                            "on another stream, still holds: drop that graph's outputs before the capture")
 
 
-def _function(attn_fwd, attn_bwd, wrap=lambda f: f):
+def _function(attn_fwd, attn_bwd, once=False):
+    """The autograd Function of a pair of calls; once: gradients of its gradients raise."""
     import torch
+    from torch.autograd.function import once_differentiable
+
+    def gradients(ctx, dout, _dlse):
+        if dout is None:  # nothing depends on out
+            return None, None, None, None, None, None
+        check_capture(ctx)
+        q, k, v, out, lse = ctx.saved_tensors
+        dq, dk, dv = attn_bwd(q, k, v, out, lse, dout.contiguous(), ctx.cu, ctx.scale, cu_seqlens_k=ctx.cu_k)
+        return dq, dk, dv, None, None, None
+
+    gradients_once = once_differentiable(gradients)
 
     class _VarlenAttention(torch.autograd.Function):
         @staticmethod
@@ -52,14 +64,8 @@ def _function(attn_fwd, attn_bwd, wrap=lambda f: f):
             return out, lse
 
         @staticmethod
-        @wrap
-        def backward(ctx, dout, _dlse):
-            if dout is None:  # nothing depends on out
-                return None, None, None, None, None, None
-            check_capture(ctx)
-            q, k, v, out, lse = ctx.saved_tensors
-            dq, dk, dv = attn_bwd(q, k, v, out, lse, dout.contiguous(), ctx.cu, ctx.scale, cu_seqlens_k=ctx.cu_k)
-            return dq, dk, dv, None, None, None
+        def backward(ctx, dout, dlse):
+            return (gradients_once if once and torch.is_grad_enabled() else gradients)(ctx, dout, dlse)
 
     return _VarlenAttention
 
@@ -86,8 +92,7 @@ def varlen_causal_attention(q, k, v, cu_seqlens, scale: float, cu_seqlens_k=None
     they raise."""
     global _CAUSAL_FN
     if _CAUSAL_FN is None:
-        from torch.autograd.function import once_differentiable
-        _CAUSAL_FN = _function(causal_attn_fwd, causal_attn_bwd, once_differentiable)
+        _CAUSAL_FN = _function(causal_attn_fwd, causal_attn_bwd, once=True)
     cu = np.array(_cu_array(cu_seqlens), copy=True)
     ck = None if cu_seqlens_k is None else np.array(_cu_array(cu_seqlens_k), copy=True)
     return _CAUSAL_FN.apply(q, k, v, cu, float(scale), ck)

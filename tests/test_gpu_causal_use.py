@@ -85,6 +85,31 @@ def test_rotary_then_attention_trains_and_answers():
         assert (np.abs(one_lse.double().cpu().numpy() - ref["lse"][:, rows]) <= b["lse"][:, rows]).all()
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_tile_shapes_and_workspaces_do_not_change_results(D, monkeypatch):
+    """Where no loop is cut, the shape of a tile of rows is a choice of speed alone; so is the size of the workspace that a
+    call offers first."""
+    log(f"case shapes D={D}")
+    n, H, Hk = [700, 33, 260], 6, 2
+    q, k, v, g = rand(993, H, D, seed=1), rand(993, Hk, D, seed=2), rand(993, Hk, D, seed=3), rand(993, H, D, seed=4)
+
+    def run():
+        out, lse = t2v.causal_attn_fwd(q, k, v, cu(n), 0.1)
+        r = (out, lse, *t2v.causal_attn_bwd(q, k, v, out, lse, g, cu(n), 0.1))
+        torch.cuda.synchronize()
+        return r
+
+    want = run()
+    for offered in (1, 1 << 26):
+        monkeypatch.setattr(_lib, "_WORKSPACE", offered)
+        assert all(torch.equal(a, b) for a, b in zip(run(), want))
+    monkeypatch.setenv("T2V_SPLIT", "off")
+    monkeypatch.setenv("T2V_QTILE", "narrow")
+    want = run()
+    monkeypatch.setenv("T2V_QTILE", "wide")
+    assert all(torch.equal(a, b) for a, b in zip(run(), want))
+
+
 def test_rows_do_not_depend_on_their_neighbours_values():
     """A row's output does not change with other rows' queries, which share its tile and its steps."""
     log("case neighbours")
