@@ -1,6 +1,8 @@
 /*
  * libt2vattn: bidirectional multi-head self-attention, forward and backward,
- * over packed variable-length token sequences, for AMD MI355X (gfx950).
+ * over packed variable-length token sequences, for AMD MI355X (gfx950); and causal
+ * attention with grouped heads over such sequences (t2v_causal_fwd, t2v_causal_bwd)
+ * with rotary positions for its queries and keys (t2v_rotary), described where they are declared.
  *
  * The operation (paper Section III, Observation 2): every clip is one sequence
  * of 3D latent patches, and each token attends to every token of its own clip
@@ -56,6 +58,13 @@
  * computes Delta, dQ, dK and dV of a piece of a sequence's queries (up to 2048, more on the
  * largest packs) and one head, and the fp32 dK / dV of its pieces are added in order. Which path a
  * call takes follows from the entry point, its offsets and sizes, and the environment below alone.
+ * Causal calls: the queries of a key head's group of heads form packed rows (query, head of the group), and the forward and
+ * dQ kernels own 256 or 128 of them (128 at head_dim 64), or, where no sequence has more than 32 (single
+ * tokens), 32 whose keys four waves share; dK/dV tiles own 256 or 128 keys (256 at 64) and loop over the heads of the
+ * group. The host estimates a list's time from measured times per key and item, and takes the tile
+ * shape and the cut of long loops that it finds fastest; cut loops leave fp32 partial results in the call's
+ * workspace, which a second kernel joins in order. Tile shapes of the forward and dQ kernels give bitwise-equal results where
+ * nothing is cut.
  *
  * Environment. T2V_ORDER=natural schedules tiles in pack order instead of longest clip
  * first (for ablations); T2V_QTILE=wide or narrow forces the forward / dQ tile shape,
@@ -63,7 +72,8 @@
  * T2V_SPLIT=off disables the dK/dV loop split (ablations and tests); T2V_PERSISTENT=1 runs the
  * forward and dK/dV kernels on a persistent grid (as many workgroups as the GPU holds at once,
  * each striding over the work list; bitwise-equal results, measured ~1% slower, so off by
- * default). T2V_LOG=1 prints one
+ * default; causal kernels have no such form). T2V_ORDER, T2V_QTILE, T2V_KVTILE and T2V_SPLIT apply to causal calls
+ * too. T2V_LOG=1 prints one
  * line to stderr per new work list: its items, the host's predicted list-scheduling
  * makespan and its lower bound, and the loop split if any. T2V_TEST_FAIL_ALLOC=1 makes
  * building a new work list fail with T2V_ERR_OOM, for testing that path.
@@ -89,7 +99,7 @@
  * t2v_last_error() names the work item, or the kernel, workgroup and row. Calls into it are
  * serialised. T2V_CHECK_CANARY=n takes n rows off every bound the kernels check, so correct
  * kernels report their clips' last rows: a way to see that the checks report. Its results
- * equal the unchecked library's bitwise.
+ * equal the unchecked library's bitwise. (t2v_rotary copies no rows into LDS and is the same in both.)
  */
 #ifndef T2VATTN_H
 #define T2VATTN_H
@@ -328,7 +338,8 @@ int t2v_plan_cascades(int n_cascades, const int32_t* pred_ptr, const int32_t* pr
  * two HIP events recorded on the launch stream. t2v_kernel_times waits for the recorded
  * events, returns the summed elapsed milliseconds and the launch count of each kernel since
  * the previous read (slots: 0 forward, 1 backward Delta, 2 backward dK/dV, 3 backward dQ; the
- * one-pass backward with its reduce counts as 2, once per batch of heads),
+ * one-pass backward with its reduce counts as 2, once per batch of heads; causal kernels with their
+ * joins count alike, rotary launches are not timed),
  * and forgets them. Enabling or disabling also forgets. Calls overlapping with launches on
  * other host threads are serialised by a mutex.
  *   ms_out     host double[4];  counts_out host int[4] */

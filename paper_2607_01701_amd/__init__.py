@@ -1,5 +1,5 @@
-"""libt2vattn: packed variable-length bidirectional attention (forward and backward)
-for AMD MI355X (gfx950), behind a C ABI (include/t2vattn.h).
+"""libt2vattn: packed variable-length attention (bidirectional, and causal with grouped heads; forward and
+backward) and rotary positions for AMD MI355X (gfx950), behind a C ABI (include/t2vattn.h).
 
 The binding below only marshals arguments; all computation is in the HIP library.
 """

@@ -265,6 +265,8 @@ CausalCost causal_cost(CausalKernel kind, int head_dim, CausalForm form, bool on
   return c;
 }
 
+// The tile shape and the cut of least estimated time; forward: the kernel of few rows where no sequence has more (against 128-row
+// tiles: one token over 1,280 keys 11 us against 15, 32 tokens over 198,261 160 against 173, 3 x 4 over 19,300 45 against 44).
 CausalList causal_plan(const TileRule& r, const CausalShape& a, int head_dim, int order, bool split, int ncu,
                        int* block) {
   const auto kind = static_cast<CausalKernel>(r.kind);

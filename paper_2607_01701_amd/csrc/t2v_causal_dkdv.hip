@@ -4,6 +4,12 @@
 // and 128 at 64). The loop starts at the first query that sees the tile; a wave skips 32-query steps
 // that see none of its keys and masks those that see some. A cut loop leaves fp32 sums in its slot, which the
 // join adds in piece order.
+//
+// What bounds it. At 64, power and the waits between stages: an item takes 2.85 us for a stage alone on its CU and 4.1 with
+// all CUs at work; matrix cores busy 50%, LDS 62% of the cycles (seven sequences of 77 to 6,001 tokens, 30 heads over 10:
+// 492 us, 930 TFLOP/s; long ones 1,000). At 128 it serves short loops, where its 128-key tiles fill the GPU (4 x 640 tokens,
+// 24 heads over 8: 58 us against 65 of t2v_causal_dkdv_wide.hip's 256 keys); long ones are the other's (16 clips of 1,280 to
+// 20,280 tokens, 12 heads: 9.6 against 8.3 ms).
 #include "t2v_causal_device.hpp"
 
 namespace t2v {
@@ -297,7 +303,8 @@ __global__ __launch_bounds__(threads<D>(), 1) void causal_dkdv_kernel(
   if (trace != nullptr) trace_end(trace, trace_t0, 2, blockIdx.x);
 }
 
-// Adds the pieces of the cut tiles (of `keys` keys) in order. A workgroup takes 32 keys; a thread four columns.
+// Adds the pieces of the cut tiles (of `keys` keys) in order. A workgroup takes 32 keys; a thread four columns. Bound by the
+// pieces' bytes (95 MB in 18 us).
 template <int D>
 __global__ __launch_bounds__(kThreads) void causal_dkdv_join_kernel(const float* __restrict__ partial,
                                                                      const CausalItem* __restrict__ tiles, int keys,
