@@ -540,23 +540,38 @@ def _outputs(specs, device, stream):
     return outs, given
 
 
+def _causal_fwd(args, q, k, v, scale, out, lse, stream):
+    """The call of causal_attn_fwd with checked arguments (args: those of _causal_arguments)."""
+    _, H, D, _, Hk, (sq, sk, sv), cq, ck = args
+    L = lib()
+    _call_with_workspace(L, L.t2v_causal_fwd, q.device, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(), sq, sk, sv,
+                         _offsets_ptr(cq), _offsets_ptr(ck), cq.shape[0] - 1, H, Hk, D, scale, out.data_ptr(),
+                         lse.data_ptr())
+
+
+def _causal_bwd(args, q, k, v, out, lse, dout, scale, dq, dk, dv, delta_ws, stream):
+    """The call of causal_attn_bwd with checked arguments."""
+    _, H, D, _, Hk, (sq, sk, sv), cq, ck = args
+    L = lib()
+    _call_with_workspace(L, L.t2v_causal_bwd, q.device, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(), sq, sk, sv,
+                         out.data_ptr(), lse.data_ptr(), _offsets_ptr(cq), _offsets_ptr(ck), cq.shape[0] - 1, H, Hk, D,
+                         scale, dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), delta_ws.data_ptr())
+
+
 def causal_attn_fwd(q, k, v, cu_seqlens, scale: float, out=None, lse=None, stream=None, cu_seqlens_k=None):
     """Causal attention with grouped heads: q [Tq, H, D], k, v [Tk, Hk, D] (bf16, on the GPU; H a multiple of
     Hk; tokens may be apart, as in slices of a fused projection). Query i of a sequence with Lq queries and Lk
     keys sees keys 0 .. i + Lk - Lq; cu_seqlens_k None: Lk = Lq. Returns (out [Tq, H, D] bf16, lse [H, Tq] fp32).
     """
     import torch
-    T, H, D, Tk, Hk, (sq, sk, sv), cq, ck = _causal_arguments(q, k, v, cu_seqlens, cu_seqlens_k)
+    args = _causal_arguments(q, k, v, cu_seqlens, cu_seqlens_k)
+    T, H, D = args[:3]
     _check_on_device((("q", q), ("k", k), ("v", v)))
-    device = q.device
     (out, lse), given = _outputs((("out", out, (T, H, D), torch.bfloat16), ("lse", lse, (H, T), torch.float32)),
-                                 device, stream)
+                                 q.device, stream)
     if given:
         _check_on_device((("q", q), *given))
-    L = lib()
-    _call_with_workspace(L, L.t2v_causal_fwd, device, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(), sq, sk, sv,
-                         _offsets_ptr(cq), _offsets_ptr(ck), cq.shape[0] - 1, H, Hk, D, float(scale), out.data_ptr(),
-                         lse.data_ptr())
+    _causal_fwd(args, q, k, v, float(scale), out, lse, stream)
     return out, lse
 
 
@@ -564,20 +579,17 @@ def causal_attn_bwd(q, k, v, out, lse, dout, cu_seqlens, scale: float, dq=None, 
                     stream=None, cu_seqlens_k=None):
     """Backward of causal_attn_fwd; returns (dq [Tq, H, D], dk, dv [Tk, Hk, D]) in bf16."""
     import torch
-    T, H, D, Tk, Hk, (sq, sk, sv), cq, ck = _causal_arguments(q, k, v, cu_seqlens, cu_seqlens_k)
+    args = _causal_arguments(q, k, v, cu_seqlens, cu_seqlens_k)
+    T, H, D, Tk, Hk = args[:5]
     for name, t in (("out", out), ("dout", dout)):
         _check_tensor(t, name, (T, H, D))
     _check_tensor(lse, "lse", (H, T), torch.float32)
     _check_on_device((("q", q), ("k", k), ("v", v), ("out", out), ("lse", lse), ("dout", dout)))
-    device, bf16 = q.device, torch.bfloat16
+    bf16 = torch.bfloat16
     (dq, dk, dv, delta_ws), given = _outputs(
         (("dq", dq, (T, H, D), bf16), ("dk", dk, (Tk, Hk, D), bf16), ("dv", dv, (Tk, Hk, D), bf16),
-         ("delta_ws", delta_ws, (2, H, T), torch.float32)), device, stream)
+         ("delta_ws", delta_ws, (2, H, T), torch.float32)), q.device, stream)
     if given:
         _check_on_device((("q", q), *given))
-    L = lib()
-    _call_with_workspace(L, L.t2v_causal_bwd, device, stream, q.data_ptr(), k.data_ptr(), v.data_ptr(), sq, sk, sv,
-                         out.data_ptr(), lse.data_ptr(), _offsets_ptr(cq), _offsets_ptr(ck), cq.shape[0] - 1, H, Hk, D,
-                         float(scale), dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
-                         delta_ws.data_ptr())
+    _causal_bwd(args, q, k, v, out, lse, dout, float(scale), dq, dk, dv, delta_ws, stream)
     return dq, dk, dv

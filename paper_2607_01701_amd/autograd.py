@@ -6,7 +6,8 @@ from __future__ import annotations
 
 import numpy as np
 
-from ._lib import _cu_array, _stream_handle, attn_bwd, attn_fwd, causal_attn_bwd, causal_attn_fwd
+from . import _lib
+from ._lib import _cu_array, _stream_handle, attn_bwd, attn_fwd
 
 
 def _leaves(ctx):
@@ -35,7 +36,8 @@ def check_capture(ctx):
 
 
 def _function(attn_fwd, attn_bwd, once=False):
-    """The autograd Function of a pair of calls; once: gradients of its gradients raise."""
+    """The autograd Function of attn_fwd(q, k, v, offsets, scale, key offsets) -> out, lse and what attn_bwd(q, k, v, out, lse,
+    dout, kept) needs besides; once: gradients of its gradients raise."""
     import torch
     from torch.autograd.function import once_differentiable
 
@@ -43,9 +45,7 @@ def _function(attn_fwd, attn_bwd, once=False):
         if dout is None:  # nothing depends on out
             return None, None, None, None, None, None
         check_capture(ctx)
-        q, k, v, out, lse = ctx.saved_tensors
-        dq, dk, dv = attn_bwd(q, k, v, out, lse, dout.contiguous(), ctx.cu, ctx.scale, cu_seqlens_k=ctx.cu_k)
-        return dq, dk, dv, None, None, None
+        return (*attn_bwd(*ctx.saved_tensors, dout.contiguous(), ctx.kept), None, None, None)
 
     gradients_once = once_differentiable(gradients)
 
@@ -53,9 +53,8 @@ def _function(attn_fwd, attn_bwd, once=False):
         @staticmethod
         def forward(ctx, q, k, v, cu_seqlens, scale, cu_seqlens_k):
             note_leaves(ctx)
-            out, lse = attn_fwd(q, k, v, cu_seqlens, scale, cu_seqlens_k=cu_seqlens_k)
+            out, lse, ctx.kept = attn_fwd(q, k, v, cu_seqlens, scale, cu_seqlens_k)
             ctx.save_for_backward(q, k, v, out, lse)
-            ctx.cu, ctx.cu_k, ctx.scale = cu_seqlens, cu_seqlens_k, scale
             ctx.mark_non_differentiable(lse)
             # lse never has a gradient: without this, every backward call allocates and fills a
             # zero [H, T] tensor for it, one more launch on an idle queue. With the leaner argument
@@ -70,6 +69,39 @@ def _function(attn_fwd, attn_bwd, once=False):
     return _VarlenAttention
 
 
+def _fwd(q, k, v, cu, scale, cu_k):
+    return (*attn_fwd(q, k, v, cu, scale, cu_seqlens_k=cu_k), (cu, scale, cu_k))
+
+
+def _bwd(q, k, v, out, lse, dout, kept):
+    cu, scale, cu_k = kept
+    return attn_bwd(q, k, v, out, lse, dout, cu, scale, cu_seqlens_k=cu_k)
+
+
+def _causal_fwd(q, k, v, cu, scale, cu_k):
+    import torch
+    args = _lib._causal_arguments(q, k, v, cu, cu_k)
+    T, H, D = args[:3]
+    _lib._check_on_device((("q", q), ("k", k), ("v", v)))
+    out = torch.empty((T, H, D), dtype=torch.bfloat16, device=q.device)
+    lse = torch.empty((H, T), dtype=torch.float32, device=q.device)
+    _lib._causal_fwd(args, q, k, v, scale, out, lse, None)
+    return out, lse, (args, scale)
+
+
+def _causal_bwd(q, k, v, out, lse, dout, kept):
+    # What was checked in the forward pass is not checked again (12 us of a small training step's 180); autograd sees to dout's
+    # shape, type and device.
+    import torch
+    args, scale = kept
+    T, H, D, Tk, Hk = args[:5]
+    empty, device = torch.empty, q.device
+    dq, dk, dv = (empty((t, h, D), dtype=torch.bfloat16, device=device) for t, h in ((T, H), (Tk, Hk), (Tk, Hk)))
+    delta_ws = empty((2, H, T), dtype=torch.float32, device=device)
+    _lib._causal_bwd(args, q, k, v, out, lse, dout, scale, dq, dk, dv, delta_ws, None)
+    return dq, dk, dv
+
+
 _FN = None  # varlen_attention's Function, made at its first call (torch is imported late)
 _CAUSAL_FN = None
 
@@ -80,7 +112,7 @@ def varlen_attention(q, k, v, cu_seqlens, scale: float, cu_seqlens_k=None):
     gradients flow to q, k and v (lse is not differentiated)."""
     global _FN
     if _FN is None:
-        _FN = _function(attn_fwd, attn_bwd)
+        _FN = _function(_fwd, _bwd)
     cu = _cu_array(cu_seqlens)
     ck = None if cu_seqlens_k is None else _cu_array(cu_seqlens_k)
     return _FN.apply(q, k, v, np.array(cu, copy=True), float(scale), None if ck is None else np.array(ck, copy=True))
@@ -92,7 +124,7 @@ def varlen_causal_attention(q, k, v, cu_seqlens, scale: float, cu_seqlens_k=None
     they raise."""
     global _CAUSAL_FN
     if _CAUSAL_FN is None:
-        _CAUSAL_FN = _function(causal_attn_fwd, causal_attn_bwd, once=True)
+        _CAUSAL_FN = _function(_causal_fwd, _causal_bwd, once=True)
     cu = np.array(_cu_array(cu_seqlens), copy=True)
     ck = None if cu_seqlens_k is None else np.array(_cu_array(cu_seqlens_k), copy=True)
     return _CAUSAL_FN.apply(q, k, v, cu, float(scale), ck)

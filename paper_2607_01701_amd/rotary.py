@@ -57,6 +57,12 @@ def rotary_apply(q, k, positions, freqs, layout: str = "half", sections=None, ms
     with ``sections`` counting the pairs of each axis. The first 2 len(freqs) dimensions turn, in pairs
     (j, j + len(freqs)) ("half") or (2 j, 2 j + 1) ("interleaved"), and are multiplied by mscale; the others are
     copied. inverse turns back by the same angles (the gradient). Returns contiguous (q, k)."""
+    args = _arguments(q, k, positions, freqs, layout, sections, mscale)
+    return _turn(q, k, positions, args, inverse, q_out, k_out, stream)
+
+
+def _arguments(q, k, positions, freqs, layout, sections, mscale):
+    """Checks all but the layout of q's and k's tokens; returns what the library takes besides tensors."""
     import torch
     first = q if q is not None else k
     if first is None:
@@ -65,7 +71,7 @@ def rotary_apply(q, k, positions, freqs, layout: str = "half", sections=None, ms
         raise ValueError("q and k must be [tokens, heads, head_dim]")
     if layout not in LAYOUTS:
         raise ValueError(f"layout must be one of {tuple(LAYOUTS)}, got {layout!r}")
-    T, _, D = first.shape
+    T = first.shape[0]
     f = freqs
     if type(f) is not np.ndarray or f.dtype != np.float64 or not f.flags.c_contiguous:
         f = np.ascontiguousarray(freqs, dtype=np.float64)
@@ -80,29 +86,34 @@ def rotary_apply(q, k, positions, freqs, layout: str = "half", sections=None, ms
         raise ValueError(f"positions has shape {tuple(positions.shape)}, expected {(n_sec, T)}")
     if positions.dtype != torch.int32 or not positions.is_contiguous():
         raise ValueError("positions must be contiguous int32")
-    named = [("positions", positions)]
-    args = []
+    return f, _SECTIONS[n_sec](*sections), n_sec, LAYOUTS[layout], float(mscale)
+
+
+def _turn(q, k, positions, args, inverse, q_out=None, k_out=None, stream=None):
+    import torch
+    first = q if q is not None else k
+    T, _, D = first.shape
+    named, specs, ins = [("positions", positions)], [], []
     for x, o, name in ((q, q_out, "q"), (k, k_out, "k")):
         if x is None:
-            args.append((None, 0, 0, None, None))
+            ins.append((None, 0, 0))
             continue
         shape = (T, x.shape[1], D)
         step = _lib._check_rows(x, name, shape)
         named.append((name, x))
-        args.append((x.data_ptr(), step, shape, o, name + "_out"))
+        specs.append((name + "_out", o, shape, torch.bfloat16))
+        ins.append((x.data_ptr(), step, shape[1]))
     _lib._check_on_device(named)
-    device = first.device
-    outs, given = _lib._outputs([(name, o, shape, torch.bfloat16) for p, _, shape, o, name in args if p is not None],
-                                device, stream)
+    outs, given = _lib._outputs(specs, first.device, stream)
     if given:
         _lib._check_on_device((named[0], *given))
-    got = iter(outs)
-    q_out, k_out = (None if x is None else next(got) for x in (q, k))
-    (qp, sq, qshape, _, _), (kp, sk, kshape, _, _) = args
+    q_out = outs[0] if q is not None else None
+    k_out = outs[-1] if k is not None else None
+    (qp, sq, heads), (kp, sk, kv_heads) = ins
+    f, sections, n_sec, layout, mscale = args
     L = _lib.lib()
-    st = _lib._call_on(device, stream, L.t2v_rotary, qp, kp, sq, sk, positions.data_ptr(), T, qshape[1] if qshape else 0,
-                       kshape[1] if kshape else 0, D, f.__array_interface__["data"][0], _SECTIONS[n_sec](*sections),
-                       n_sec, LAYOUTS[layout], float(mscale), 1 if inverse else 0,
+    st = _lib._call_on(first.device, stream, L.t2v_rotary, qp, kp, sq, sk, positions.data_ptr(), T, heads, kv_heads, D,
+                       f.__array_interface__["data"][0], sections, n_sec, layout, mscale, 1 if inverse else 0,
                        None if q_out is None else q_out.data_ptr(), None if k_out is None else k_out.data_ptr())
     if st != _lib.T2V_OK:
         _lib._check(L, st)
@@ -114,23 +125,23 @@ def _function():
 
     class _Rotary(torch.autograd.Function):
         @staticmethod
-        def forward(ctx, q, k, positions, freqs, layout, sections, mscale, inverse):
+        def forward(ctx, q, k, positions, args, inverse):
             note_leaves(ctx)
             ctx.save_for_backward(positions)
-            ctx.args = (freqs, layout, sections, mscale, not inverse)
+            ctx.args, ctx.inverse = args, inverse
             ctx.set_materialize_grads(False)
-            return rotary_apply(q, k, positions, freqs, layout, sections, mscale, inverse)
+            return _turn(q, k, positions, args, inverse)
 
         @staticmethod
         def backward(ctx, dq, dk):
             if dq is None and dk is None:
-                return (None,) * 8
+                return (None,) * 5
             check_capture(ctx)
             (positions,) = ctx.saved_tensors
             # R(angle) transposed is R(-angle); with create_graph, the turn back has a gradient of its own.
             dq, dk = (x if x is None or _rows(x) else x.contiguous() for x in (dq, dk))
-            turn = _Rotary.apply if torch.is_grad_enabled() else rotary_apply
-            return (*turn(dq, dk, positions, *ctx.args), None, None, None, None, None, None)
+            turn = _Rotary.apply if torch.is_grad_enabled() else _turn
+            return (*turn(dq, dk, positions, ctx.args, not ctx.inverse), None, None, None)
 
     return _Rotary
 
@@ -153,5 +164,5 @@ def rotary(q, k, positions, freqs, layout: str = "half", sections=None, mscale: 
     global _FN
     if _FN is None:
         _FN = _function()
-    f = np.array(freqs, dtype=np.float64, copy=True)
-    return _FN.apply(q, k, positions, f, layout, None if sections is None else tuple(sections), float(mscale), False)
+    args = _arguments(q, k, positions, np.array(freqs, dtype=np.float64, copy=True), layout, sections, mscale)
+    return _FN.apply(q, k, positions, args, False)
