@@ -228,8 +228,8 @@ enum CausalForm { kFew, kNarrow, kWide };
 // Times measured on MI355X (microseconds; see CausalCost), with all CUs busy and with one item a CU on few of them.
 // A key of a forward item: 29.5 ns at head_dim 128 with 256 rows (wide), 30.3 with 128 and a second workgroup beside it
 // (narrow), 30 at 64 (128 rows, three workgroups); alone 22, 16 and 12. Of a dQ item 40, 41.5 and 36, alone 26, 20 and 12.
-// So wide tiles are faster where all CUs are busy for many rounds (running 20,280 tokens, 24 heads over 8: 2,315 us
-// against 2,378), narrow ones where the few items' ends count (4 x 1,280 tokens, 12 heads: 36 us against 42). The kernel of few
+// So wide tiles are faster where all CUs are busy for many rounds (running 20,280 tokens, 24 heads over 8: 2,204 us
+// against 2,307), narrow ones where the few items' ends count (4 x 1,280 tokens, 12 heads: 37 us against 42). The kernel of few
 // rows 9 ns a key. Where each key is read by one tile only (`once`: single tokens) the memory's 5 TB/s bound
 // the loop instead, and an item that fills its pipeline leaves them to the others. A dK/dV item: 1.75 us (alone 1.25) for 32 queries and 256 keys (wide) or 2.2 (1.6) for 64 and 128
 // (narrow) at head_dim 128, 4.1 (2.85) for 128 and 256 at 64.
@@ -266,7 +266,7 @@ CausalCost causal_cost(CausalKernel kind, int head_dim, CausalForm form, bool on
 }
 
 // The tile shape and the cut of least estimated time; forward: the kernel of few rows where no sequence has more (against 128-row
-// tiles: one token over 1,280 keys 11 us against 15, 32 tokens over 198,261 160 against 173, 3 x 4 over 19,300 45 against 44).
+// tiles: one token over 1,280 keys 11.5 us against 12.1, 32 tokens over 198,261 161 against 174, 3 x 4 over 19,300 46 against 51).
 CausalList causal_plan(const TileRule& r, const CausalShape& a, int head_dim, int order, bool split, int ncu,
                        int* block) {
   const auto kind = static_cast<CausalKernel>(r.kind);

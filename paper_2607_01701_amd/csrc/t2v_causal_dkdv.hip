@@ -7,9 +7,9 @@
 //
 // What bounds it. At 64, power and the waits between stages: an item takes 2.85 us for a stage alone on its CU and 4.1 with
 // all CUs at work; matrix cores busy 50%, LDS 62% of the cycles (seven sequences of 77 to 6,001 tokens, 30 heads over 10:
-// 492 us, 930 TFLOP/s; long ones 1,000). At 128 it serves short loops, where its 128-key tiles fill the GPU (4 x 640 tokens,
+// 497 us, 920 TFLOP/s; long ones 1,000 to 1,100. 64 keys a wave, as in t2v_causal_dkdv_wide.hip, took 540). At 128 it serves short loops, where its 128-key tiles fill the GPU (4 x 640 tokens,
 // 24 heads over 8: 58 us against 65 of t2v_causal_dkdv_wide.hip's 256 keys); long ones are the other's (16 clips of 1,280 to
-// 20,280 tokens, 12 heads: 9.6 against 8.3 ms).
+// 20,280 tokens, 12 heads: 9.4 against 7.9 ms).
 #include "t2v_causal_device.hpp"
 
 namespace t2v {

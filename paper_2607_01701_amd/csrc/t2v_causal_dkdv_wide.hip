@@ -7,8 +7,8 @@
 // paths over them met again, the compiler would have to copy them.
 //
 // Bound by the matrix cores and power: busy 65% of the cycles with 2.8 vector instructions for each matrix instruction (16 clips
-// of 1,280 to 20,280 tokens, 12 heads: 7.56 to 8.3 ms, 1,170 to 1,280 TFLOP/s). What the masked steps waste counts where
-// loops are short: 8 x 4,096 tokens, 24 heads over 8: 1.41 to 1.49 ms, 1,105 to 1,170.
+// of 1,280 to 20,280 tokens, 12 heads: 7.56 to 7.9 ms, 1,225 to 1,280 TFLOP/s). What the masked steps waste counts where
+// loops are short: 8 x 4,096 tokens, 24 heads over 8: 1.41 to 1.45 ms, 1,140 to 1,170.
 #include "t2v_causal_device.hpp"
 #include "t2v_dkdv_wide_step.hpp"
 

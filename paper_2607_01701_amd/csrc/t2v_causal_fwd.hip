@@ -9,12 +9,12 @@
 // sequence's first rows. A cut loop leaves the unnormalised sums, the reference and the sum of each row in its
 // slot; the join weighs and adds the pieces in order.
 //
-// What bounds it. At head_dim 128 the matrix cores and the card's power: they are busy 57% of the cycles, at 1,040 to
-// 1,140 TFLOP/s of visible pairs (16 clips of 1,280 to 20,280 tokens, 12 heads: 4.24 to 4.65 ms; 20,280 tokens, 24
-// heads over 8: 2.15 to 2.31 ms). 256 rows read a staged key eight times from LDS and once from memory; two waves a SIMD run one's
+// What bounds it. At head_dim 128 the matrix cores and the card's power: they are busy 60 to 63% of the cycles, at 1,120 to
+// 1,160 TFLOP/s of visible pairs (16 clips of 1,280 to 20,280 tokens, 12 heads: 4.28 to 4.33 ms; 20,280 tokens, 24
+// heads over 8: 2.17 to 2.20 ms). 256 rows read a staged key eight times from LDS and once from memory; two waves a SIMD run one's
 // softmax under the other's products. At 64 the vector instructions: 10.7 for each matrix instruction (5.3 at
-// 128), 880 TFLOP/s (seven sequences of 77 to 6,001 tokens, 30 heads over 10: 261 us); three workgroups of 128
-// rows a CU do better there than one of 256 (277 against 307 us before the loops were trimmed).
+// 128), 875 TFLOP/s (seven sequences of 77 to 6,001 tokens, 30 heads over 10: 262 us); three workgroups of 128
+// rows a CU do better there than one of 256 (288 us).
 // Steps that mask something run by themselves after the plain ones: code paths over the sums that meet again in one loop
 // made the compiler spill.
 #include "t2v_causal_device.hpp"
@@ -251,8 +251,8 @@ __global__ __launch_bounds__(NT, 512 / NT) void causal_fwd_kernel(
 // every fourth 32-key step, each through LDS buffers of its own (the copy of the next step in flight), so
 // nothing but its own copies holds a wave up; the waves' sums meet in LDS at the end. The keys and values, read
 // once, bound it: one workgroup a CU (two at head_dim 64) has 64 KB in flight. 32 tokens over 0.81 GB of them (40 heads over
-// 8): 154 us, 5.3 TB/s, 160 with the join; 128-row tiles take 173. One token over 1,280 keys (30 heads of 64 over
-// 10): 11 us with the join against 15.
+// 8): 154 us, 5.3 TB/s, 161 with the join; 128-row tiles take 174. One token over 1,280 keys (30 heads of 64 over
+// 10): 11.5 us with the join against 12.1.
 constexpr int kFewRows = 32;
 
 // Copy of 32 rows of a (sequence, key head) by one wave into a swizzled tile; rows behind the last repeat it.
