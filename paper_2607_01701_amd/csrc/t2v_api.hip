@@ -226,15 +226,18 @@ constexpr int64_t kCausalMaxWorkspace = int64_t(1) << 30;
 enum CausalForm { kFew, kNarrow, kWide };
 
 // Times measured on MI355X (microseconds; see CausalCost), with all CUs busy and with one item a CU on few of them.
-// A key of a forward item: 29.5 ns at head_dim 128 with 256 rows (wide), 30.3 with 128 and a second workgroup beside it
-// (narrow), 30 at 64 (128 rows, three workgroups); alone 22, 16 and 12. Of a dQ item 40, 41.5 and 36, alone 26, 20 and 12.
-// So wide tiles are faster where all CUs are busy for many rounds (running 20,280 tokens, 24 heads over 8: 2,204 us
-// against 2,307), narrow ones where the few items' ends count (4 x 1,280 tokens, 12 heads: 37 us against 42). The kernel of few
-// rows 9 ns a key. Where each key is read by one tile only (`once`: single tokens) the memory's 5 TB/s bound
-// the loop instead, and an item that fills its pipeline leaves them to the others. A dK/dV item: 1.75 us (alone 1.25) for 32 queries and 256 keys (wide) or 2.2 (1.6) for 64 and 128
-// (narrow) at head_dim 128, 4.1 (2.85) for 128 and 256 at 64.
-// Loads, stores and filling the pipeline: `fixed`. A join costs a launch, 0.3 us a piece, and reads the pieces' results
-// at 5.5 TB/s (their writes run beside other items' loops, mostly).
+// A key of a forward item at head_dim 128: 28.1 ns with 256 rows (wide), 29.3 with 128 and a second workgroup beside it
+// (narrow), alone 22 and 16; of a dQ item 37.6 and 39, alone 26 and 20. What an item costs besides (loads, stores, filling the
+// pipeline, masked steps: `fixed`) is hidden in part by the second workgroup: forward 8.5 and 6.6 us, dQ 11.7 and 8.5. So wide
+// tiles are faster for long loops (8,192 tokens, 24 heads over 8: forward 1,500 us against 1,535, dQ 2,010 against 2,045) and narrow
+// ones for shorter ones (2,048 tokens: 480 against 459, 635 against 600). At 64 (128 rows, three workgroups) a key takes 30
+// and 36 ns, alone 12.
+// The kernel of few rows: 9 ns a key. Where each key is read by one tile only (`once`: single tokens) the memory's 5 TB/s
+// bound the loop instead, and an item that fills its pipeline leaves them to the others.
+// A dK/dV item: 1.75 us (alone 1.25) for 32 queries and 256 keys (wide) or 2.2 (1.6) for 64 and 128 (narrow) at head_dim
+// 128, 4.1 (2.85) for 128 and 256 at 64.
+// A join costs a launch, 0.3 us a piece, and reads the pieces' results at 5.5 TB/s (their writes run beside other
+// items' loops, mostly).
 CausalCost causal_cost(CausalKernel kind, int head_dim, CausalForm form, bool once, int ncu) {
   CausalCost c{};
   const bool d64 = head_dim == 64;
@@ -252,9 +255,9 @@ CausalCost causal_cost(CausalKernel kind, int head_dim, CausalForm form, bool on
   }
   c.workers = c.cus * (form == kWide ? 1 : form == kFew ? (d64 ? 2 : 1) : d64 ? 3 : 2);
   const bool fwd = kind == kCausalFwd;
-  c.unit = d64 ? (fwd ? 0.030 : 0.036) : form == kWide ? (fwd ? 0.0295 : 0.040) : fwd ? 0.0303 : 0.0415;
+  c.unit = d64 ? (fwd ? 0.030 : 0.036) : form == kWide ? (fwd ? 0.0281 : 0.0376) : fwd ? 0.0293 : 0.0390;
   c.alone = d64 ? 0.012 : form == kWide ? (fwd ? 0.022 : 0.026) : fwd ? 0.016 : 0.020;
-  c.fixed = form == kFew ? 3.0 : 4.0;
+  c.fixed = form == kFew ? 3.0 : d64 ? 4.0 : form == kWide ? (fwd ? 8.5 : 11.7) : fwd ? 6.6 : 8.5;
   if (form == kFew) c.unit = c.alone = 0.009;
   const double bound = 4.0 * head_dim * c.workers / 5e6;
   if (once && bound > c.unit) {
