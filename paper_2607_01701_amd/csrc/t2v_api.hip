@@ -1518,40 +1518,18 @@ int causal_bwd_impl(CausalCall& c, const void* out, const float* lse, const void
   if (int st = check_causal_plan(pq, c.cu_q, c.cu_k, c.nseq, "causal dQ")) return st;
   if (int st = check_arm()) return st;
 #endif
-  hipError_t e = hipSuccess;
-  if (c.tq > 0) {
-    AttnArgs p{};
-    p.out = out;
-    p.dout = dout;
-    p.lse = lse;
-    p.delta = delta_ws;
-    p.heads = c.heads;
-    p.head_dim = c.head_dim;
-    p.total_tokens = c.tq;
-    e = timer().run(kSlotPre, s, [&] { return launch_bwd_pre(p, s); });
-    if (e != hipSuccess) return hip_fail(e, "backward preprocess launch");
-  }
   CausalArgs a = causal_args(c, ws);
+  a.out = const_cast<void*>(out);
+  a.lse = const_cast<float*>(lse);
   a.dout = dout;
   a.delta = delta_ws;
   a.dq = dq;
   a.dk = dk;
   a.dv = dv;
-  if (pk->n_items > 0) {
-    a.trace = tracer().reserve(pk->n_items);
-    e = timer().run(kSlotDkdv, s, [&] {
-      hipError_t r = launch_causal_dkdv(a, pk->block, pk->causal(), pk->n_items, s);
-      if (r == hipSuccess && pk->n_reduce > 0)
-        r = launch_causal_dkdv_join(a, pk->block, pk->causal() + pk->n_items, pk->n_reduce, s);
-      return r;
-    });
-    const int used = note_use(pk, s);
-    if (e != hipSuccess) return hip_fail(e, "causal dK/dV kernel launch");
-    if (used != T2V_OK) return used;
-  }
+  // dQ first: it works out Delta.
   if (pq->n_items > 0) {
     a.trace = tracer().reserve(pq->n_items);
-    e = timer().run(kSlotDq, s, [&] {
+    const hipError_t e = timer().run(kSlotDq, s, [&] {
       hipError_t r = launch_causal_dq(a, pq->block, pq->causal(), pq->n_items, s);
       if (r == hipSuccess && pq->n_reduce > 0)
         r = launch_causal_dq_join(a, pq->block, pq->causal() + pq->n_items, pq->n_reduce, s);
@@ -1559,6 +1537,18 @@ int causal_bwd_impl(CausalCall& c, const void* out, const float* lse, const void
     });
     const int used = note_use(pq, s);
     if (e != hipSuccess) return hip_fail(e, "causal dQ kernel launch");
+    if (used != T2V_OK) return used;
+  }
+  if (pk->n_items > 0) {
+    a.trace = tracer().reserve(pk->n_items);
+    const hipError_t e = timer().run(kSlotDkdv, s, [&] {
+      hipError_t r = launch_causal_dkdv(a, pk->block, pk->causal(), pk->n_items, s);
+      if (r == hipSuccess && pk->n_reduce > 0)
+        r = launch_causal_dkdv_join(a, pk->block, pk->causal() + pk->n_items, pk->n_reduce, s);
+      return r;
+    });
+    const int used = note_use(pk, s);
+    if (e != hipSuccess) return hip_fail(e, "causal dK/dV kernel launch");
     if (used != T2V_OK) return used;
   }
   return T2V_OK;

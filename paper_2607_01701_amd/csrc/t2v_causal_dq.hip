@@ -1,5 +1,7 @@
 // dQ kernel of causal attention with grouped heads: a workgroup owns a tile of packed rows and loops
-// over the keys that its last row sees, as the forward kernel does; P comes from the stored lse. A cut
+// over the keys that its last row sees, as the forward kernel does; P comes from the stored lse. Before its loop it works out
+// Delta of its rows, of which it holds dO, for itself and for the dK/dV kernel, which runs after it (a kernel of its own for that
+// read dO again and took 2% of a training step). A cut
 // loop leaves fp32 sums in its slot, which the join adds in piece order.
 //
 // Three products a pair against the forward's two, and no maximum: matrix cores and power bound it at both head dims, busy 70%
@@ -93,9 +95,9 @@ T2V_DEV void dq_step(uint32_t kbase, uint32_t vbase, uint32_t kr0, uint32_t kr1,
 template <int D, int NT>
 __global__ __launch_bounds__(NT, 512 / NT) void causal_dq_kernel(
     const bf16* __restrict__ q, const bf16* __restrict__ k, const bf16* __restrict__ v, int64_t qs, int64_t ks,
-    int64_t vs, const bf16* __restrict__ dout, const float* __restrict__ lse2, const float* __restrict__ ndelta,
+    int64_t vs, const bf16* __restrict__ out, const bf16* __restrict__ dout, const float* __restrict__ lse,
     const CausalItem* __restrict__ items, int H, int g, int64_t T, float c, float scale, bf16* __restrict__ dq,
-    float* __restrict__ partial, unsigned long long* __restrict__ trace) {
+    float* __restrict__ delta, float* __restrict__ partial, unsigned long long* __restrict__ trace) {
   constexpr int KK = D / 16;
   constexpr int DB = D / 32;
   constexpr int R = NT / 2;
@@ -116,22 +118,41 @@ __global__ __launch_bounds__(NT, 512 / NT) void causal_dq_kernel(
   for (int db = 0; db < DB; ++db) dqa[db] = zero16();
 
   const int ntiles = (it.end - it.begin + kBN - 1) / kBN;
+  const bf16* kh = k + it.krow0 * ks + static_cast<int64_t>(it.head) * D;
+  const bf16* vh = v + it.krow0 * vs + static_cast<int64_t>(it.head) * D;
+  const TileDma<D, kBN, NT> kdma(tid, ks), vdma(tid, vs);
   if (ntiles > 0) {
-    const bf16* kh = k + it.krow0 * ks + static_cast<int64_t>(it.head) * D;
-    const bf16* vh = v + it.krow0 * vs + static_cast<int64_t>(it.head) * D;
-    const TileDma<D, kBN, NT> kdma(tid, ks), vdma(tid, vs);
     kdma.copy(sK[0], kh, ks, it.begin, it.lk);
     vdma.copy(sV[0], vh, vs, it.begin, it.lk);
-    bf16x8 qop[KK], gop[KK];
-    const bf16* qp = q + me.token * qs + static_cast<int64_t>(me.head) * D;
-    const bf16* gp = dout + (me.token * H + me.head) * D;
+  }
+  // This lane's half of its row of dO (a B operand of every step) and of out, and Delta from them, which goes to the dK/dV
+  // kernel with lse * log2(e) (from the first piece of a cut loop).
+  bf16x8 gop[KK];
+  float nl2, ndl;
+  {
+    const int64_t row = (me.token * H + me.head) * D, at = static_cast<int64_t>(me.head) * T + me.token;
+    bf16x8 oop[KK];
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-      qop[kk] = load8(qp + kk * 16 + G * 8, me.ok);
-      gop[kk] = load8(gp + kk * 16 + G * 8, me.ok);
+    for (int kk = 0; kk < KK; ++kk) gop[kk] = load8(dout + row + kk * 16 + G * 8, me.ok);
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) oop[kk] = load8(out + row + kk * 16 + G * 8, me.ok);
+    nl2 = me.ok ? -kLog2e * lse[at] : 0.0f;
+    float d = 0.0f;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) d = fmaf(static_cast<float>(oop[kk][e]), static_cast<float>(gop[kk][e]), d);
+    ndl = -half_sum(d);
+    if (it.begin == 0 && me.ok && G == 0) {
+      delta[at] = ndl;
+      delta[static_cast<int64_t>(H) * T + at] = -nl2;
     }
-    const int64_t at = static_cast<int64_t>(me.head) * T + me.token;
-    const float nl2 = me.ok ? -lse2[at] : 0.0f, ndl = me.ok ? ndelta[at] : 0.0f;
+  }
+  if (ntiles > 0) {
+    bf16x8 qop[KK];
+    const bf16* qp = q + me.token * qs + static_cast<int64_t>(me.head) * D;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) qop[kk] = load8(qp + kk * 16 + G * 8, me.ok);
     const uint32_t oo = opnd_lane_off<D>(lane);
     const uint32_t ro0 = rows_lane_off<D>(lane, 0), ro1 = rows_lane_off<D>(lane, 1);
     wait_vmcnt0();
@@ -235,8 +256,8 @@ template <int D, int NT>
 void launch_as(const CausalArgs& a, const CausalItem* items, int n, hipStream_t s) {
   hipLaunchKernelGGL((causal_dq_kernel<D, NT>), dim3(n), dim3(NT), 0, s, static_cast<const bf16*>(a.q),
                      static_cast<const bf16*>(a.k), static_cast<const bf16*>(a.v), a.q_stride, a.k_stride, a.v_stride,
-                     static_cast<const bf16*>(a.dout), a.delta + a.tq * a.heads, a.delta, items, a.heads,
-                     a.heads / a.kv_heads, a.tq, a.scale * kLog2e, a.scale, static_cast<bf16*>(a.dq), a.partial,
+                     static_cast<const bf16*>(a.out), static_cast<const bf16*>(a.dout), a.lse, items, a.heads,
+                     a.heads / a.kv_heads, a.tq, a.scale * kLog2e, a.scale, static_cast<bf16*>(a.dq), a.delta, a.partial,
                      a.trace);
 }
 

@@ -15,9 +15,9 @@ struct CausalArgs {
   const void* v;
   int64_t q_stride, k_stride, v_stride;  // elements between tokens of q, k and v
   const void* dout;                      // [Tq, H, D], as out and dq
-  void* out;
-  float* lse;          // [H, Tq]
-  const float* delta;  // [2, H, Tq]: -Delta, then lse * log2(e)
+  void* out;                             // written by the forward kernels, read by the dQ kernel, as lse
+  float* lse;                            // [H, Tq]
+  float* delta;  // [2, H, Tq]: -Delta, then lse * log2(e); the dQ kernel's for the dK/dV kernels
   void* dq;
   void* dk;  // [Tk, Hk, D], as dv
   void* dv;
