@@ -5,7 +5,7 @@
 // loop leaves fp32 sums in its slot, which the join adds in piece order.
 //
 // Three products a pair against the forward's two, and no maximum: matrix cores and power bound it at both head dims, busy 70%
-// of the cycles at 128 (16 clips of 1,280 to 20,280 tokens, 12 heads: 5.66 to 5.9 ms, 1,235 to 1,285 TFLOP/s) and 65% at 64
+// of the cycles at 128 (16 clips of 1,280 to 20,280 tokens, 12 heads: 5.68 to 6.1 ms, 1,195 to 1,280 TFLOP/s) and 65% at 64
 // (seven sequences of 77 to 6,001 tokens, 30 heads over 10: 318 us, 1,080). Wide tiles (256 rows) read each staged key for
 // twice the rows (5.86 against 6.06 ms); narrow ones end sooner where a CU has one or two (4 x 640 tokens, 24 heads
 // over 8: 31 against 35 us).
