@@ -110,6 +110,25 @@ def test_tile_shapes_and_workspaces_do_not_change_results(D, monkeypatch):
     assert all(torch.equal(a, b) for a, b in zip(run(), want))
 
 
+@pytest.mark.parametrize("lq,lk,H,Hk,D", [([70, 40, 3], [70, 9, 0], 4, 2, 128), ([130, 1], [4000, 50], 3, 1, 64)])
+def test_row_statistics_of_the_backward_pass(lq, lk, H, Hk, D):
+    """delta_ws as documented, for every row (with no keys, and of cut loops too): -rowsum(dout * out), exact products summed
+    in 32 bits, and lse * log2(e), rounded once after log2(e) itself was."""
+    log(f"case statistics {lq} over {lk}")
+    q, k, v, g = rand(sum(lq), H, D, seed=1), rand(sum(lk), Hk, D, seed=2), rand(sum(lk), Hk, D, seed=3), rand(sum(lq), H, D, seed=4)
+    out, lse = t2v.causal_attn_fwd(q, k, v, cu(lq), 0.1, cu_seqlens_k=cu(lk))
+    stats = torch.full((2, H, sum(lq)), float("nan"), device="cuda")
+    t2v.causal_attn_bwd(q, k, v, out, lse, g, cu(lq), 0.1, delta_ws=stats, cu_seqlens_k=cu(lk))
+    torch.cuda.synchronize()
+    prod = (out.double() * g.double()).cpu()
+    got, want = stats.double().cpu(), -prod.sum(2).t()
+    assert ((got[0] - want).abs() <= D * 2.0 ** -24 * prod.abs().sum(2).t()).all()
+    scaled = lse.double().cpu() * 1.4426950408889634
+    dead = scaled == -float("inf")
+    assert torch.equal(dead, got[1] == -float("inf"))
+    assert ((got[1] - scaled).abs()[~dead] <= 2.0 ** -23 * scaled.abs()[~dead]).all()
+
+
 def test_rows_do_not_depend_on_their_neighbours_values():
     """A row's output does not change with other rows' queries, which share its tile and its steps."""
     log("case neighbours")
