@@ -90,11 +90,17 @@ def _causal_fwd(q, k, v, cu, scale, cu_k):
 
 
 def _causal_bwd(q, k, v, out, lse, dout, kept):
-    # What was checked in the forward pass is not checked again (12 us of a small training step's 180); autograd sees to dout's
-    # shape, type and device.
+    # Of what the forward pass checked only the offsets still hold: saved-tensor hooks may give other tensors, such as dense
+    # copies of slices, so their strides, shapes, types and devices are taken from themselves.
     import torch
     args, scale = kept
-    T, H, D, Tk, Hk = args[:5]
+    T, H, D, Tk, Hk, _, cq, ck = args
+    strides = tuple(_lib._check_rows(x, n, s) for x, n, s in ((q, "q", (T, H, D)), (k, "k", (Tk, Hk, D)), (v, "v", (Tk, Hk, D))))
+    for x, n in ((out, "out"), (dout, "dout")):
+        _lib._check_tensor(x, n, (T, H, D))
+    _lib._check_tensor(lse, "lse", (H, T), torch.float32)
+    _lib._check_on_device((("q", q), ("k", k), ("v", v), ("out", out), ("lse", lse), ("dout", dout)))
+    args = (T, H, D, Tk, Hk, strides, cq, ck)
     empty, device = torch.empty, q.device
     dq, dk, dv = (empty((t, h, D), dtype=torch.bfloat16, device=device) for t, h in ((T, H), (Tk, Hk), (Tk, Hk)))
     delta_ws = empty((2, H, T), dtype=torch.float32, device=device)

@@ -1,0 +1,95 @@
+"""What the autograd wrappers pass to the library, on the CPU with the library's calls replaced by ones that note
+their arguments and launch nothing."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2607_01701_amd as t2v
+from paper_2607_01701_amd import _lib
+
+CU = np.array([0, 30, 50], dtype=np.int32)
+
+
+class Calls:
+    """Stands for the library: each call is noted with its arguments and succeeds."""
+
+    def __init__(self):
+        self.made = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.made.append((name, args))
+            return _lib.T2V_OK
+        return call
+
+    def args(self, name):
+        (found,) = [a for n, a in self.made if n == name]
+        return found
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    c = Calls()
+    monkeypatch.setattr(_lib, "lib", lambda: c)
+    monkeypatch.setattr(_lib, "_check_on_device", lambda named: None)
+    monkeypatch.setattr(_lib, "_call_on", lambda device, stream, fn, *args: fn(*args, None))
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 0, raising=False)
+    return c
+
+
+def dense(x):
+    return x.clone(memory_format=torch.contiguous_format)
+
+
+def address(x):
+    return getattr(x, "value", x)
+
+
+HOOKS = [None, (dense, lambda x: x), (lambda x: x, dense)]
+
+
+@pytest.mark.parametrize("hooks", HOOKS, ids=["none", "pack", "unpack"])
+def test_causal_backward_describes_the_tensors_that_it_passes(calls, hooks):
+    """Saved-tensor hooks (offloading, compression) may give dense copies of slices of a fused projection."""
+    H, Hk, D = 6, 2, 128
+    w = torch.zeros(50, H + 2 * Hk, D, dtype=torch.bfloat16).requires_grad_(True)
+    q, k, v = w[:, :H], w[:, H:H + Hk], w[:, H + Hk:]
+    seen = {}
+
+    def unpacked(x):
+        y = hooks[1](x)
+        seen[y.data_ptr()] = y
+        return y
+
+    if hooks is None:
+        out, _ = t2v.varlen_causal_attention(q, k, v, CU, 0.1)
+        seen.update({x.data_ptr(): x for x in (q, k, v)})
+    else:
+        with torch.autograd.graph.saved_tensors_hooks(hooks[0], unpacked):
+            out, _ = t2v.varlen_causal_attention(q, k, v, CU, 0.1)
+    out.backward(torch.zeros_like(out))
+    a = calls.args("t2v_causal_bwd")
+    for pointer, stride, heads in zip(a[:3], a[3:6], (H, Hk, Hk)):
+        x = seen[address(pointer)]
+        assert x.shape == (50, heads, D) and x.stride() == (stride, D, 1)
+    assert [ctypes.c_int(n).value for n in a[10:14]] == [2, H, Hk, D]
+
+
+@pytest.mark.parametrize("name,change", [
+    ("q", lambda x: x[:-1]), ("k", lambda x: x.float()), ("v", lambda x: x.transpose(0, 1).contiguous().transpose(0, 1)),
+    ("out", lambda x: x.transpose(0, 1).contiguous().transpose(0, 1)), ("lse", lambda x: x.double()),
+    ("lse", lambda x: x.t().contiguous().t()),
+])
+def test_causal_backward_refuses_what_a_hook_changed(calls, name, change):
+    H, Hk, D = 4, 2, 64
+    q, k, v = (torch.zeros(50, h, D, dtype=torch.bfloat16).requires_grad_(True) for h in (H, Hk, Hk))
+    order = iter(("q", "k", "v", "out", "lse"))
+    with torch.autograd.graph.saved_tensors_hooks(lambda x: (next(order), x), lambda p: change(p[1]) if p[0] == name else p[1]):
+        out, _ = t2v.varlen_causal_attention(q, k, v, CU, 0.1)
+    with pytest.raises(ValueError, match=f"{name} "):
+        out.backward(torch.zeros_like(out))
+    assert "t2v_causal_bwd" not in [n for n, _ in calls.made]
