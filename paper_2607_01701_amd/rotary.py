@@ -63,7 +63,6 @@ def rotary_apply(q, k, positions, freqs, layout: str = "half", sections=None, ms
 
 def _arguments(q, k, positions, freqs, layout, sections, mscale):
     """Checks all but the layout of q's and k's tokens; returns what the library takes besides tensors."""
-    import torch
     first = q if q is not None else k
     if first is None:
         raise ValueError("q and k are both None")
@@ -82,11 +81,16 @@ def _arguments(q, k, positions, freqs, layout, sections, mscale):
     n_sec = len(sections)
     if not 1 <= n_sec <= 3 or sum(sections) != pairs:
         raise ValueError(f"sections {sections} are not one to three counts that sum to the {pairs} frequencies")
-    if positions.shape != (n_sec, T) and (n_sec > 1 or positions.shape != (T,)):
-        raise ValueError(f"positions has shape {tuple(positions.shape)}, expected {(n_sec, T)}")
+    _check_positions(positions, n_sec, T)
+    return f, _SECTIONS[n_sec](*sections), n_sec, LAYOUTS[layout], float(mscale)
+
+
+def _check_positions(positions, axes, T):
+    import torch
+    if positions.shape != (axes, T) and (axes > 1 or positions.shape != (T,)):
+        raise ValueError(f"positions has shape {tuple(positions.shape)}, expected {(axes, T)}")
     if positions.dtype != torch.int32 or not positions.is_contiguous():
         raise ValueError("positions must be contiguous int32")
-    return f, _SECTIONS[n_sec](*sections), n_sec, LAYOUTS[layout], float(mscale)
 
 
 def _turn(q, k, positions, args, inverse, q_out=None, k_out=None, stream=None):
@@ -138,6 +142,7 @@ def _function():
                 return (None,) * 5
             check_capture(ctx)
             (positions,) = ctx.saved_tensors
+            _check_positions(positions, ctx.args[2], (dk if dq is None else dq).shape[0])  # a hook may have changed them
             # R(angle) transposed is R(-angle); with create_graph, the turn back has a gradient of its own.
             dq, dk = (x if x is None or _rows(x) else x.contiguous() for x in (dq, dk))
             turn = _Rotary.apply if torch.is_grad_enabled() else _turn

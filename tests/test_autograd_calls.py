@@ -93,3 +93,16 @@ def test_causal_backward_refuses_what_a_hook_changed(calls, name, change):
     with pytest.raises(ValueError, match=f"{name} "):
         out.backward(torch.zeros_like(out))
     assert "t2v_causal_bwd" not in [n for n, _ in calls.made]
+
+
+@pytest.mark.parametrize("change,msg", [
+    (lambda x: x.long(), "int32"), (lambda x: x[:, :-1], "shape"), (lambda x: x.t().contiguous().t(), "contiguous"),
+])
+def test_rotary_backward_refuses_positions_that_a_hook_changed(calls, change, msg):
+    q = torch.zeros(50, 4, 64, dtype=torch.bfloat16).requires_grad_(True)
+    positions = torch.zeros(2, 50, dtype=torch.int32)
+    with torch.autograd.graph.saved_tensors_hooks(lambda x: x, change):
+        out, _ = t2v.rotary(q, None, positions, np.ones(32), sections=(16, 16))
+    with pytest.raises(ValueError, match=f"positions.*{msg}"):
+        out.backward(torch.zeros_like(out))
+    assert len(calls.made) == 1
