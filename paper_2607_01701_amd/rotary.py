@@ -162,9 +162,12 @@ _FN = None
 
 
 def rotary(q, k, positions, freqs, layout: str = "half", sections=None, mscale: float = 1.0):
-    """rotary_apply with autograd: gradients flow to q and k (either may be None)."""
+    """rotary_apply with autograd: gradients flow to q and k (either may be None), and have gradients of their own.
+    Forward-mode derivatives are refused."""
     import torch
-    if not torch.is_grad_enabled() or not any(x is not None and x.requires_grad for x in (q, k)):
+    from torch.autograd.forward_ad import unpack_dual
+    grads = torch.is_grad_enabled()
+    if not any(x is not None and (grads and x.requires_grad or unpack_dual(x).tangent is not None) for x in (q, k)):
         return rotary_apply(q, k, positions, freqs, layout, sections, mscale)
     global _FN
     if _FN is None:

@@ -106,3 +106,19 @@ def test_rotary_backward_refuses_positions_that_a_hook_changed(calls, change, ms
     with pytest.raises(ValueError, match=f"positions.*{msg}"):
         out.backward(torch.zeros_like(out))
     assert len(calls.made) == 1
+
+
+@pytest.mark.parametrize("grad", [True, False], ids=["grad", "no_grad"])
+@pytest.mark.parametrize("which", ["q", "k", "attention"])
+def test_forward_mode_derivatives_are_refused(calls, which, grad):
+    """A tangent that the calls do not carry on is not dropped in silence; without one, a dual level changes nothing."""
+    x = torch.zeros(50, 4, 64, dtype=torch.bfloat16)
+    positions = torch.zeros(50, dtype=torch.int32)
+    with torch.autograd.forward_ad.dual_level(), torch.set_grad_enabled(grad):
+        assert t2v.rotary(x, x, positions, np.ones(32))[0].shape == x.shape
+        dual = torch.autograd.forward_ad.make_dual(x, torch.ones_like(x))
+        with pytest.raises((RuntimeError, NotImplementedError), match="jvp"):
+            if which == "attention":
+                t2v.varlen_causal_attention(dual, x, x, CU, 0.1)
+            else:
+                t2v.rotary(dual if which == "q" else None, dual if which == "k" else x, positions, np.ones(32))
