@@ -348,6 +348,12 @@ def _check_tensor(t, name, shape, dtype=None):
         raise ValueError(f"{name} must be contiguous")
 
 
+def _aligned(t):
+    """t, contiguous and at a 16-byte address: itself, or a copy (a gradient's place is not its user's choice)."""
+    t = t.contiguous()
+    return t if t.data_ptr() % 16 == 0 else t.clone()
+
+
 def _check_on_device(named):
     """Last of the checks: every tensor is on a GPU (the same one as the first)."""
     first = None

@@ -7,7 +7,7 @@ from __future__ import annotations
 import numpy as np
 
 from . import _lib
-from ._lib import _cu_array, _stream_handle, attn_bwd, attn_fwd
+from ._lib import _aligned, _cu_array, _stream_handle, attn_bwd, attn_fwd
 
 
 def _leaves(ctx):
@@ -45,7 +45,7 @@ def _function(attn_fwd, attn_bwd, once=False):
         if dout is None:  # nothing depends on out
             return None, None, None, None, None, None
         check_capture(ctx)
-        return (*attn_bwd(*ctx.saved_tensors, dout.contiguous(), ctx.kept), None, None, None)
+        return (*attn_bwd(*ctx.saved_tensors, _aligned(dout), ctx.kept), None, None, None)
 
     gradients_once = once_differentiable(gradients)
 

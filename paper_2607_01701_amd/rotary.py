@@ -144,7 +144,7 @@ def _function():
             (positions,) = ctx.saved_tensors
             _check_positions(positions, ctx.args[2], (dk if dq is None else dq).shape[0])  # a hook may have changed them
             # R(angle) transposed is R(-angle); with create_graph, the turn back has a gradient of its own.
-            dq, dk = (x if x is None or _rows(x) else x.contiguous() for x in (dq, dk))
+            dq, dk = (x if x is None or _rows(x) else _lib._aligned(x) for x in (dq, dk))
             turn = _Rotary.apply if torch.is_grad_enabled() else _turn
             return (*turn(dq, dk, positions, ctx.args, not ctx.inverse), None, None, None)
 
@@ -154,8 +154,8 @@ def _function():
 def _rows(t) -> bool:
     """Whether the call takes t as it is: each token's heads contiguous, tokens at least a token apart."""
     T, H, D = t.shape
-    return t.is_contiguous() or (t.stride(2) == 1 and t.stride(1) == D and H * D <= t.stride(0) <= 1 << 22
-                                 and t.stride(0) % 8 == 0 and t.data_ptr() % 16 == 0)
+    return t.data_ptr() % 16 == 0 and (t.is_contiguous() or (
+        t.stride(2) == 1 and t.stride(1) == D and H * D <= t.stride(0) <= 1 << 22 and t.stride(0) % 8 == 0))
 
 
 _FN = None

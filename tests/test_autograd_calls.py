@@ -122,3 +122,21 @@ def test_forward_mode_derivatives_are_refused(calls, which, grad):
                 t2v.varlen_causal_attention(dual, x, x, CU, 0.1)
             else:
                 t2v.rotary(dual if which == "q" else None, dual if which == "k" else x, positions, np.ones(32))
+
+
+@pytest.mark.parametrize("which", ["bidirectional", "causal", "rotary", "rotary k"])
+def test_gradients_at_any_address(calls, which):
+    """The gradient of a concatenation's part is contiguous and may start anywhere; the library takes 16-byte addresses."""
+    x = torch.zeros(50, 4, 64, dtype=torch.bfloat16).requires_grad_(True)
+    if which.startswith("rotary"):
+        both = (x, None) if which == "rotary" else (None, x)
+        out = [y for y in t2v.rotary(*both, torch.zeros(50, dtype=torch.int32), np.ones(32)) if y is not None][0]
+    else:
+        out, _ = (t2v.varlen_attention if which == "bidirectional" else t2v.varlen_causal_attention)(x, x, x, CU, 0.1)
+    g = torch.zeros(out.numel() + 1, dtype=out.dtype)[1:].view(out.shape)
+    assert g.is_contiguous() and g.data_ptr() % 16 == 2
+    out.backward(g)
+    name, place = {"bidirectional": ("t2v_attn_bwd", 10), "causal": ("t2v_causal_bwd", 15), "rotary": ("t2v_rotary", 0),
+                   "rotary k": ("t2v_rotary", 1)}[which]
+    a = [args for n, args in calls.made if n == name][-1]
+    assert a[place] != 0 and a[place] % 16 == 0

@@ -55,3 +55,33 @@ def test_gradients_under_saved_tensor_hooks(H, Hk, D, hooks):
     (got,) = torch.autograd.grad(out, w, g)
     torch.cuda.synchronize()
     assert torch.equal(got, want) and torch.isfinite(want.float()).all() and (want != 0).any()
+
+
+@pytest.mark.parametrize("H,Hk,D", [(4, 2, 128), (2, 2, 64)])
+def test_gradients_of_parts_of_a_concatenation(H, Hk, D):
+    """They start at any even address: the results are those of aligned ones, bitwise."""
+    log(f"case unaligned gradients {H}/{Hk}x{D}")
+    n = [70, 9]
+    q, k, v = (rand(79, h, D, seed=h).requires_grad_(True) for h in (H, Hk, Hk))
+    pos = torch.arange(79, dtype=torch.int32, device="cuda")
+    freqs, _ = t2v.rotary_frequencies(D // 2)
+
+    def outputs():
+        a, b = t2v.rotary(q, k, pos, freqs, "interleaved")
+        o, _ = t2v.varlen_causal_attention(q, k, v, cu(n), 0.1)
+        outs = [a, b, o]
+        if H == Hk:
+            outs.append(t2v.varlen_attention(q, k, v, cu(n), 0.1)[0])
+        return outs
+
+    outs = outputs()
+    sizes = [o.numel() for o in outs]
+    whole = rand(sum(sizes) + len(sizes), seed=9)
+    want = torch.autograd.grad(outs, (q, k, v), [p.clone().view(o.shape) for p, o in zip(
+        (x[1:] for x in whole.split([s + 1 for s in sizes])), outs)])
+    one = torch.zeros(1, dtype=torch.bfloat16, device="cuda")
+    joined = torch.cat([x for o in outputs() for x in (one, o.flatten())])
+    got = torch.autograd.grad(joined, (q, k, v), whole)
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
