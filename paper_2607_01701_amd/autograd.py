@@ -14,25 +14,34 @@ def _leaves(ctx):
     return [n for n, _ in ctx.next_functions if n is not None and type(n).__name__ == "AccumulateGrad"]
 
 
-def note_leaves(ctx):
-    """Notes, in a Function's forward, which stream first used a leaf's gradient node (torch keeps one as long as any
-    autograd graph holds it, and its stream with it). Costs about 1 us."""
-    stream = _stream_handle(None)
-    for node in _leaves(ctx):
-        node.metadata.setdefault("t2v_stream", stream)  # lives as long as the node
+def _on_default_stream(device):
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # as in _stream_handle
+    return (torch.cuda.current_stream(device).cuda_stream if raw is None else raw(device.index)) == 0
+
+
+def note_leaves(ctx, *inputs):
+    """Notes, in a Function's forward, whether the gradient nodes of its leaf inputs were first used on the default stream (torch
+    keeps a node as long as any autograd graph holds it, and the stream that was current when it was made with it). A node
+    that another operation made before is taken for one of this call's stream."""
+    leaves = [x for x in inputs if x is not None and x.requires_grad and x.is_leaf]
+    if leaves:
+        default = _on_default_stream(leaves[0].device)
+        for node in _leaves(ctx):
+            node.metadata.setdefault("t2v_default_stream", default)  # lives as long as the node
 
 
 def check_capture(ctx):
-    """Refuses, in a Function's backward, to record into a graph the gradient of a leaf whose node an eager call made on
-    another stream and that call's autograd graph still holds: torch would make that stream part of the capture, which
-    ends the process when the capture does."""
+    """Refuses, in a Function's backward, to record into a graph the gradient of a leaf whose node an eager call made on the
+    default stream and that call's autograd graph still holds: torch would make that stream part of the capture, which ends the
+    process when the capture does. (Any other stream joins a capture, and leaves it.)"""
     import torch
     if not torch.cuda.is_current_stream_capturing():
         return
-    stream = _stream_handle(None)
-    if any(node.metadata.get("t2v_stream", stream) != stream for node in _leaves(ctx)):
+    if any(node.metadata.get("t2v_default_stream", False) for node in _leaves(ctx)):
         raise RuntimeError("a captured backward pass takes the gradient of a leaf tensor that an eager autograd graph, made "
-                           "on another stream, still holds: drop that graph's outputs before the capture")
+                           "on the default stream, still holds: drop that graph's outputs before the capture, or make them "
+                           "on a side stream")
 
 
 def _function(attn_fwd, attn_bwd, once=False):
@@ -52,7 +61,7 @@ def _function(attn_fwd, attn_bwd, once=False):
     class _VarlenAttention(torch.autograd.Function):
         @staticmethod
         def forward(ctx, q, k, v, cu_seqlens, scale, cu_seqlens_k):
-            note_leaves(ctx)
+            note_leaves(ctx, q, k, v)
             out, lse, ctx.kept = attn_fwd(q, k, v, cu_seqlens, scale, cu_seqlens_k)
             ctx.save_for_backward(q, k, v, out, lse)
             ctx.mark_non_differentiable(lse)

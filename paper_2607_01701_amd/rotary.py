@@ -130,7 +130,7 @@ def _function():
     class _Rotary(torch.autograd.Function):
         @staticmethod
         def forward(ctx, q, k, positions, args, inverse):
-            note_leaves(ctx)
+            note_leaves(ctx, q, k)
             ctx.save_for_backward(positions)
             ctx.args, ctx.inverse = args, inverse
             ctx.set_materialize_grads(False)

@@ -140,3 +140,33 @@ def test_gradients_at_any_address(calls, which):
                    "rotary k": ("t2v_rotary", 1)}[which]
     a = [args for n, args in calls.made if n == name][-1]
     assert a[place] != 0 and a[place] % 16 == 0
+
+
+def attend(name, q, k, v):
+    if name == "rotary":
+        return t2v.rotary(q, k, torch.zeros(50, dtype=torch.int32), np.ones(32))[0]
+    return (t2v.varlen_attention if name == "bidirectional" else t2v.varlen_causal_attention)(q, k, v, CU, 0.1)[0]
+
+
+@pytest.mark.parametrize("name", ["bidirectional", "causal", "rotary"])
+@pytest.mark.parametrize("eager,refused", [(0, True), (7, False), (9, False), (None, False)],
+                         ids=["default stream", "side stream", "the capture's stream", "no eager graph"])
+def test_captured_backward_beside_an_eager_graph(calls, monkeypatch, name, eager, refused):
+    """Only a leaf whose gradient node was made on the default stream cannot be captured: any other stream may
+    join a capture, as that of a warm-up whose outputs are still there."""
+    q, k, v = (torch.zeros(50, 4, 64, dtype=torch.bfloat16).requires_grad_(True) for _ in range(3))
+    current = [eager or 0]
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: current[0], raising=False)
+    alive = attend(name, q, k, v) if eager is not None else None
+    current[0] = 9
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    out = attend(name, q, k, v)
+    g = torch.zeros_like(out)
+    if refused:
+        with pytest.raises(RuntimeError, match="default stream"):
+            out.backward(g)
+    else:
+        out.backward(g)
+    if refused:  # until the eager graph is gone
+        del alive, out
+        attend(name, q, k, v).backward(g)

@@ -85,3 +85,44 @@ def test_gradients_of_parts_of_a_concatenation(H, Hk, D):
     torch.cuda.synchronize()
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("name", ["bidirectional", "causal", "rotary"])
+def test_capture_after_a_warm_up_whose_outputs_are_kept(name):
+    """The eager graph of a side stream, still alive, does not hinder the capture of a training step on another stream; replays
+    give the eager gradients, with eager steps between them."""
+    log(f"case capture beside a warm-up, {name}")
+    n = [200, 30]
+    q, k, v = (rand(230, 2, 64, seed=i).requires_grad_(True) for i in (1, 2, 3))
+    g = rand(230, 2, 64, seed=9)
+    pos = torch.arange(230, dtype=torch.int32, device="cuda")
+    freqs, _ = t2v.rotary_frequencies(32)
+
+    def step():
+        if name == "rotary":
+            a, b = t2v.rotary(q, k, pos, freqs)
+            return a + b
+        return (t2v.varlen_attention if name == "bidirectional" else t2v.varlen_causal_attention)(q, k, v, cu(n), 0.1)[0]
+
+    leaves = (q, k) if name == "rotary" else (q, k, v)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        kept = step()
+        want = torch.autograd.grad(kept, leaves, g, retain_graph=True)
+    torch.cuda.synchronize()
+    want = [x.clone() for x in want]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = torch.autograd.grad(step(), leaves, g)
+    for i in range(3):
+        for x in got:
+            x.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+        with torch.cuda.stream(side):
+            eager = torch.autograd.grad(step(), leaves, g)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(eager, want)), i
+    assert kept.requires_grad
