@@ -61,8 +61,8 @@ def _function(attn_fwd, attn_bwd, once=False):
     class _VarlenAttention(torch.autograd.Function):
         @staticmethod
         def forward(ctx, q, k, v, cu_seqlens, scale, cu_seqlens_k):
-            note_leaves(ctx, q, k, v)
             out, lse, ctx.kept = attn_fwd(q, k, v, cu_seqlens, scale, cu_seqlens_k)
+            note_leaves(ctx, q, k, v)
             ctx.save_for_backward(q, k, v, out, lse)
             ctx.mark_non_differentiable(lse)
             # lse never has a gradient: without this, every backward call allocates and fills a

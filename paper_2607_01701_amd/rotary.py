@@ -130,11 +130,12 @@ def _function():
     class _Rotary(torch.autograd.Function):
         @staticmethod
         def forward(ctx, q, k, positions, args, inverse):
+            out = _turn(q, k, positions, args, inverse)
             note_leaves(ctx, q, k)
             ctx.save_for_backward(positions)
             ctx.args, ctx.inverse = args, inverse
             ctx.set_materialize_grads(False)
-            return _turn(q, k, positions, args, inverse)
+            return out
 
         @staticmethod
         def backward(ctx, dq, dk):

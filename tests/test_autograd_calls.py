@@ -170,3 +170,15 @@ def test_captured_backward_beside_an_eager_graph(calls, monkeypatch, name, eager
     if refused:  # until the eager graph is gone
         del alive, out
         attend(name, q, k, v).backward(g)
+
+
+@pytest.mark.parametrize("name", ["bidirectional", "causal", "rotary"])
+def test_calls_without_a_gpu_name_the_tensor(name, monkeypatch):
+    """The refusal of tensors that are not on a GPU comes before any question about streams."""
+    def none(*_):
+        raise RuntimeError("no GPU")
+    for place in ("current_device", "current_stream"):
+        monkeypatch.setattr(torch.cuda, place, none)
+    q, k, v = (torch.zeros(50, 4, 64, dtype=torch.bfloat16).requires_grad_(True) for _ in range(3))
+    with pytest.raises(ValueError, match="must be a CUDA tensor"):
+        attend(name, q, k, v)
