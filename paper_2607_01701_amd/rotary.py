@@ -100,6 +100,8 @@ def _turn(q, k, positions, args, inverse, q_out=None, k_out=None, stream=None):
     named, specs, ins = [("positions", positions)], [], []
     for x, o, name in ((q, q_out, "q"), (k, k_out, "k")):
         if x is None:
+            if o is not None:
+                raise ValueError(f"{name}_out is given without {name}")
             ins.append((None, 0, 0))
             continue
         shape = (T, x.shape[1], D)
