@@ -268,6 +268,7 @@ int t2v_causal_bwd(const void* q, const void* k, const void* v,
  *                elements between tokens as in t2v_causal_fwd; heads or kv_heads 0: that tensor is left out
  *                (its pointers may be NULL, its stride is not read)
  *   positions    device int32 [n_sections, tokens], any value
+ *   tokens       at most 2^31 - 1, and what 2^24 - 1 workgroups take: 2^29 - 32 of one head of 128 dimensions, fewer of wider ones
  *   freqs        HOST double [n], radians a position, finite: each is held as a fraction of a turn to 2^-64 (for
  *                |freqs| up to 2 pi; beyond, of its own value), and the angle is their product modulo a turn
  *   sections     HOST int32 [n_sections], 1 to 3 counts of pairs (>= 0): the first sections[0] pairs turn by

@@ -286,10 +286,13 @@ int rotary_impl(const void* q, const void* k, int64_t q_stride, int64_t k_stride
       a.turn[j] = turn_of(freqs[j]);
     }
   const int per = tokens_per_block(a, head_dim);
-  const int blocks = static_cast<int>((tokens + per - 1) / per);
+  const int64_t blocks = (tokens + per - 1) / per;
+  if (blocks * kThreads > UINT32_MAX)  // a launch counts its threads in 32 bits
+    return bad("the call takes " + std::to_string(blocks) + " workgroups of " + std::to_string(per) + " tokens, more than one launch holds");
   const auto s = static_cast<hipStream_t>(stream);
   const bool interleaved = layout == T2V_ROTARY_INTERLEAVED;
-  head_dim == 128 ? launch<128>(a, interleaved, blocks, per, s) : launch<64>(a, interleaved, blocks, per, s);
+  head_dim == 128 ? launch<128>(a, interleaved, static_cast<int>(blocks), per, s)
+                  : launch<64>(a, interleaved, static_cast<int>(blocks), per, s);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? T2V_OK : set_error(T2V_ERR_HIP, std::string("rotary kernel launch: ") + hipGetErrorString(e));
 }
