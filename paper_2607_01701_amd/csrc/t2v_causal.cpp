@@ -29,8 +29,6 @@ struct Loops {
     const int64_t last = std::min<int64_t>(r0 + block, static_cast<int64_t>(lq) * group) - 1;
     return causal_keys(static_cast<int32_t>(last / group), lq, lk);
   }
-  // The longest loop is that of the last tile of rows, of the first tile of keys.
-  int32_t longest() const { return tiles() == 0 ? 0 : length(kind == kCausalDkdv ? 0 : tiles() - 1); }
 };
 
 Loops loops_of(CausalKernel kind, const CausalShape& a, int s, int block, int stage) {
