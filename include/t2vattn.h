@@ -228,6 +228,9 @@ int t2v_attn_bwd_qk_ws(const void* q, const void* k, const void* v,
  * query that sees no key has out = 0, lse = -inf and dq = 0, a key that no query sees dk = dv = 0. What a
  * query does not see does not reach its results, infinities and NaN included (those of dk and dv are the sums over
  * the queries that see the key).
+ * Key segments lie back to back. A cache with room behind each sequence, [nseq, room, Hk, D], is a pack of twice the
+ * sequences: after each one a sequence without queries whose keys are the rest of its room, which is not read (the
+ * backward call writes zeros to its dk and dv).
  *   q            device bf16 [Tq, H, D], read only; q_stride elements between tokens, so that q may be a
  *                slice of a fused projection: a multiple of 8, H * D <= q_stride <= 2^22
  *   k, v         device bf16 [Tk, Hk, D] likewise, with k_stride and v_stride
