@@ -63,8 +63,10 @@
  * tokens), 32 whose keys four waves share; dK/dV tiles own 256 or 128 keys (256 at 64) and loop over the heads of the
  * group. The host estimates a list's time from measured times per key and item, and takes the tile
  * shape and the cut of long loops that it finds fastest; cut loops leave fp32 partial results in the call's
- * workspace, which a second kernel joins in order. Tile shapes of the forward and dQ kernels give bitwise-equal results where
- * nothing is cut.
+ * workspace, which a second kernel joins in order. The 256- and 128-row shapes of the forward and dQ kernels give
+ * bitwise-equal results where nothing is cut; the forward form for at most 32 rows and the two dK/dV forms at head_dim 128
+ * agree with the others to rounding. The shape follows from all sequences of a call, so a sequence's last bits may
+ * depend on which others it is packed with.
  *
  * Environment. T2V_ORDER=natural schedules tiles in pack order instead of longest clip
  * first (for ablations); T2V_QTILE=wide or narrow forces the forward / dQ tile shape,

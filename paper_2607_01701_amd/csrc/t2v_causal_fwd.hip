@@ -5,8 +5,8 @@
 // keys that the tile's last row sees, staged through LDS 64 at a time and shared by all heads
 // of the group. Scores are computed transposed (S^T = K Q^T), the softmax runs online over 32-key
 // steps with a lazily moved reference maximum (it moves when a step exceeds it by 2^kTau). A wave skips
-// steps that none of its rows sees and masks those that only some see: two at most, besides a
-// sequence's first rows. A cut loop leaves the unnormalised sums, the reference and the sum of each row in its
+// steps that none of its rows sees, and masks the others from the first 64-key stage on that one of its rows does not see
+// whole: three at most (with one head to a group), the first of which all rows may see. A cut loop leaves the unnormalised sums, the reference and the sum of each row in its
 // slot; the join weighs and adds the pieces in order.
 //
 // What bounds it. At head_dim 128 the matrix cores and the card's power: they are busy 60 to 63% of the cycles, at 1,120 to
