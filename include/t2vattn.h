@@ -286,6 +286,41 @@ int t2v_rotary(const void* q, const void* k, int64_t q_stride, int64_t k_stride,
                int64_t tokens, int heads, int kv_heads, int head_dim, const double* freqs, const int32_t* sections,
                int n_sections, int layout, float mscale, int inverse, void* q_out, void* k_out, void* stream);
 
+/* Norms of the heads of q and k, and rotary positions after them, in one pass:
+ *   n = w x / sqrt(mean(x^2) + eps)   over the head_dim elements x of a token's head, w the weights of its tensor;
+ *   the first 2 n_pairs dimensions of n are then turned and multiplied by mscale as in t2v_rotary, the others are n's.
+ * All in 32 bits, rounded once. */
+typedef struct {
+  const int32_t* positions;   /* the turn: as t2v_rotary's arguments; n_sections 0: none (the other five are not read) */
+  const double* freqs;
+  const int32_t* sections;
+  int n_sections;
+  int layout;
+  float mscale;
+  float eps;                  /* the norm: finite and >= 0; negative: none (the weights must be NULL then) */
+  const void* q_weight;       /* device [head_dim], 16-byte aligned; NULL: ones */
+  const void* k_weight;
+  int weights_f32;            /* the weights are float32 (nonzero) or bfloat16 (0) */
+} t2v_turn;
+
+/*   q, k, strides, tokens, heads, kv_heads, head_dim, q_out, k_out   as in t2v_rotary
+ *   turn         HOST struct, read before the call returns; weights may not overlap the outputs */
+int t2v_norm_rotary(const void* q, const void* k, int64_t q_stride, int64_t k_stride, int64_t tokens, int heads,
+                    int kv_heads, int head_dim, const t2v_turn* turn, void* q_out, void* k_out, void* stream);
+
+/* Backward pass of t2v_norm_rotary for the loss <dq_out, q_out> + <dk_out, k_out>. With x^ = x / sqrt(mean(x^2) + eps), r that
+ * reciprocal root and dn the gradients turned back: dx = r (w dn - x^ mean(w dn x^)), dw = the sum of dn x^ over tokens and heads.
+ *   q, k, strides, turn   as passed to t2v_norm_rotary (a norm is needed: eps >= 0)
+ *   dq_out, dk_out   device bf16 [tokens, heads, D], [tokens, kv_heads, D], read only, with strides of their own
+ *   dq, dk           device bf16, contiguous, written
+ *   dq_weight, dk_weight   device [head_dim] of the weights' type, 16-byte aligned, written; NULL where not wanted or the weight is NULL
+ *   ws, ws_bytes, need     as in t2v_causal_fwd; at most 2 MiB, 0 without gradients of weights
+ * Outputs must not overlap each other or any input. Without tokens the gradients of weights are zeros. Deterministic: no atomics. */
+int t2v_norm_rotary_bwd(const void* q, const void* k, int64_t q_stride, int64_t k_stride, const void* dq_out,
+                        const void* dk_out, int64_t dq_out_stride, int64_t dk_out_stride, int64_t tokens, int heads,
+                        int kv_heads, int head_dim, const t2v_turn* turn, void* dq, void* dk, void* dq_weight,
+                        void* dk_weight, void* ws, uint64_t ws_bytes, uint64_t* need, void* stream);
+
 /* Thread-local message describing the last non-OK status of this thread. */
 const char* t2v_last_error(void);
 

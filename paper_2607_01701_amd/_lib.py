@@ -37,7 +37,7 @@ EXPORTS = ("t2v_attn_fwd", "t2v_attn_bwd", "t2v_attn_fwd_qk", "t2v_attn_bwd_qk",
            "t2v_release_cache", "t2v_build_worklist", "t2v_plan_makespan", "t2v_timing_enable", "t2v_kernel_times",
            "t2v_version", "t2v_list_schedule", "t2v_plan_cascades", "t2v_probe_mfma_peak", "t2v_trace_set",
            "t2v_trace_count", "t2v_attn_bwd_noalloc", "t2v_attn_bwd_qk_ws", "t2v_causal_fwd", "t2v_causal_bwd",
-           "t2v_rotary")
+           "t2v_rotary", "t2v_norm_rotary", "t2v_norm_rotary_bwd")
 KERNEL_SLOTS = ("fwd", "bwd_pre", "bwd_dkdv", "bwd_dq")
 HOST_EXPORTS = ("t2v_last_error", "t2v_build_worklist", "t2v_plan_makespan", "t2v_version", "t2v_list_schedule",
                 "t2v_plan_cascades")
@@ -46,6 +46,13 @@ _vp = ctypes.c_void_p
 _i32p = ctypes.POINTER(ctypes.c_int32)
 _u64p = ctypes.POINTER(ctypes.c_uint64)
 _f32p = ctypes.c_void_p  # device float* passed as an address
+
+
+class Turn(ctypes.Structure):
+    """t2v_turn: a norm and a turn."""
+    _fields_ = [("positions", _vp), ("freqs", _vp), ("sections", _vp), ("n_sections", ctypes.c_int), ("layout", ctypes.c_int),
+                ("mscale", ctypes.c_float), ("eps", ctypes.c_float), ("q_weight", _vp), ("k_weight", _vp),
+                ("weights_f32", ctypes.c_int)]
 
 
 class T2VError(RuntimeError):
@@ -102,6 +109,12 @@ def _declare(lib, full: bool):
         lib.t2v_rotary.argtypes = [_vp, _vp, ctypes.c_int64, ctypes.c_int64, _vp, ctypes.c_int64, ctypes.c_int,
                                    ctypes.c_int, ctypes.c_int, _vp, _i32p, ctypes.c_int, ctypes.c_int, ctypes.c_float,
                                    ctypes.c_int, _vp, _vp, _vp]
+        i64, turnp = ctypes.c_int64, ctypes.POINTER(Turn)
+        lib.t2v_norm_rotary.restype = ctypes.c_int
+        lib.t2v_norm_rotary.argtypes = [_vp, _vp, i64, i64, i64, ctypes.c_int, ctypes.c_int, ctypes.c_int, turnp, _vp, _vp, _vp]
+        lib.t2v_norm_rotary_bwd.restype = ctypes.c_int
+        lib.t2v_norm_rotary_bwd.argtypes = [_vp, _vp, i64, i64, _vp, _vp, i64, i64, i64, ctypes.c_int, ctypes.c_int,
+                                            ctypes.c_int, turnp, _vp, _vp, _vp, _vp, _vp, ctypes.c_uint64, _u64p, _vp]
         lib.t2v_release_cache.restype = None
         lib.t2v_release_cache.argtypes = []
         lib.t2v_timing_enable.restype = ctypes.c_int

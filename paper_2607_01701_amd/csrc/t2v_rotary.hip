@@ -9,10 +9,7 @@
 // and loads them before the sines and cosines, which are worked out once a token and shared by
 // all heads through LDS. Counts of pairs that are no multiple of 8 take the same path: the last unit is moved
 // back to overlap the one before (it writes the same values again), and vectors need not be aligned.
-//
-// Angles. A frequency is held as a 64-bit fraction of a turn, F = f / 2 pi mod 1 in units of 2^-64, so that
-// position * F modulo 2^64 is the angle's fraction of a turn, exact to position * 2^-65 turns at any int32
-// position: no large angle is ever formed or reduced. Its top 24 bits and sign go to 32-bit sine and cosine.
+// Angles: t2v_rotary.hpp.
 #include <algorithm>
 #include <cmath>
 #include <string>
@@ -21,15 +18,14 @@
 #include "../../include/t2vattn.h"
 #include "t2v_device.hpp"
 #include "t2v_host.h"
+#include "t2v_rotary.hpp"
 
 namespace t2v {
 namespace {
 
 constexpr int kThreads = 256;
 constexpr int kUnits = 4;  // in flight per lane
-constexpr int kMaxPairs = 64;
 constexpr int kMaxAngles = 2048;  // of a workgroup (16 KB of LDS: eight workgroups on a CU)
-constexpr int kMaxAxes = 3;
 
 struct RotaryArgs {
   const bf16* in[2];   // q, k
@@ -41,8 +37,7 @@ struct RotaryArgs {
   int rot_dim;
   float mscale;
   int inverse;
-  unsigned long long turn[kMaxPairs];  // a position's angle of each pair, in 2^-64 turns
-  unsigned char axis[kMaxPairs];
+  RotaryAngles angles;
 };
 
 // Eight bf16 at any 2-byte address (a global access of 16 bytes needs no alignment).
@@ -132,13 +127,8 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, in
   load(w, threadIdx.x);
   for (int e = threadIdx.x; e < nt * pairs; e += kThreads) {
     const int t = e / pairs, j = e - t * pairs;
-    const int p = a.positions[a.axis[j] * a.tokens + t0 + t];
-    const unsigned long long turns = static_cast<unsigned long long>(static_cast<long long>(p)) * a.turn[j];
-    // The fraction of a turn in [-1/2, 1/2), in half turns.
-    const float half_turns = static_cast<float>(static_cast<long long>(turns)) * 0x1p-63f;
-    float s, c;
-    sincospif(half_turns, &s, &c);
-    cs[e] = make_float2(c * a.mscale, (a.inverse ? -s : s) * a.mscale);
+    const float2 k = angle_of(a.angles, j, a.positions[a.angles.axis[j] * a.tokens + t0 + t]);
+    cs[e] = make_float2(k.x * a.mscale, (a.inverse ? -k.y : k.y) * a.mscale);
   }
   __syncthreads();
   for (int e0 = threadIdx.x; e0 < total; e0 += kUnits * kThreads) {
@@ -196,14 +186,6 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, in
   }
 }
 
-// f radians in 2^-64 turns, modulo a turn. long double holds 64 bits of the quotient.
-unsigned long long turn_of(double f) {
-  const long double turns = static_cast<long double>(f) * 0.159154943091895335768883763372514362L;  // 1 / (2 pi)
-  const long double frac = turns - std::floor(turns);
-  const long double scaled = frac * 18446744073709551616.0L;
-  return scaled >= 18446744073709551615.0L ? ~0ull : static_cast<unsigned long long>(scaled + 0.5L);
-}
-
 template <int D>
 void launch(const RotaryArgs& a, bool interleaved, int blocks, int per, hipStream_t s) {
   if (interleaved)
@@ -232,18 +214,8 @@ int rotary_impl(const void* q, const void* k, int64_t q_stride, int64_t k_stride
     return bad("heads and kv_heads must be >= 0, and one of them >= 1");
   if ((heads + static_cast<int64_t>(kv_heads)) * head_dim > (int64_t(1) << 22))
     return bad("heads * head_dim is too large");
-  if (freqs == nullptr || sections == nullptr) return bad("freqs or sections is NULL");
-  if (n_sections < 1 || n_sections > kMaxAxes) return bad("there must be 1 to 3 sections");
   int64_t pairs = 0;
-  for (int i = 0; i < n_sections; ++i) {
-    if (sections[i] < 0) return bad("sections must be >= 0");
-    pairs += sections[i];
-  }
-  if (pairs < 1 || 2 * pairs > head_dim) return bad("the sections must sum to 1 .. head_dim / 2 pairs");
-  if (layout != T2V_ROTARY_HALF && layout != T2V_ROTARY_INTERLEAVED) return bad("unknown layout");
-  if (!std::isfinite(mscale)) return bad("mscale must be finite");
-  for (int64_t j = 0; j < pairs; ++j)
-    if (!std::isfinite(freqs[j])) return bad("freqs must be finite");
+  if (int st = check_rotary(freqs, sections, n_sections, layout, mscale, head_dim, &pairs)) return st;
   if (tokens == 0) return T2V_OK;
   const struct {
     const void* in;
@@ -280,11 +252,7 @@ int rotary_impl(const void* q, const void* k, int64_t q_stride, int64_t k_stride
   a.rot_dim = static_cast<int>(2 * pairs);
   a.mscale = mscale;
   a.inverse = inverse != 0;
-  for (int i = 0, j = 0; i < n_sections; ++i)
-    for (int n = 0; n < sections[i]; ++n, ++j) {
-      a.axis[j] = static_cast<unsigned char>(i);
-      a.turn[j] = turn_of(freqs[j]);
-    }
+  fill_angles(&a.angles, freqs, sections, n_sections);
   const int per = tokens_per_block(a, head_dim);
   const int64_t blocks = (tokens + per - 1) / per;
   if (blocks * kThreads > UINT32_MAX)  // a launch counts its threads in 32 bits

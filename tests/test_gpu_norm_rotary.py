@@ -1,0 +1,258 @@
+"""Norms of heads with rotary positions on the GPU against the definition in float64, within the roundings: both layouts, parts
+of the head, several axes, weights of both types and none, slices, gradients, odd values, graphs."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import norm_rotary as oracle
+from paper_2607_01701_amd import norm_rotary, norm_rotary_apply, norm_rotary_bwd, rotary_apply, rotary_frequencies
+
+from gpu_util import log
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+
+
+def np64(x):
+    return None if x is None else x.detach().double().cpu().numpy()
+
+
+def check(got, ref, bound, what):
+    e = np.abs(np64(got) - ref)
+    worst = float((e / (bound + 1e-300)).max()) if e.size else 0.0
+    log(f"{what}: {worst:.3f} of the bound")
+    assert worst <= 1.0, what
+
+
+def same_turn(got, other, q, k):
+    """Two kernels' turns of q and k: the same infinities and NaN, and finite values within twice the bound of one. (Either
+    product of a sum may be the one that is not rounded by itself, so bits may differ. A pair's magnitudes are at most twice
+    the row's largest.)"""
+    for x, y, src in zip(got, other, (q, k)):
+        assert torch.equal(x.isnan(), y.isnan()) and torch.equal(x.isinf(), y.isinf()) and torch.equal(x[x.isinf()], y[y.isinf()])
+        x, y = (t.double().nan_to_num(0.0, 0.0, 0.0) for t in (x, y))
+        largest = src.double().nan_to_num(0.0, 0.0, 0.0).abs().amax(-1, keepdim=True)
+        assert ((x - y).abs() <= 2 * (2.0 ** -8 * y.abs() + 2.0 ** -8 * x.abs()) + 4 * oracle.TURN * largest).all()
+
+
+def case(T, H, Hk, D, sections, start, dtype, seed=0, scale=None):
+    g = torch.Generator().manual_seed(seed + T + H)
+    mk = lambda *s: torch.randn(s, generator=g)  # noqa: E731
+    size = torch.exp(2.0 * mk(T, 1, 1)) if scale is None else scale
+    q, k = (mk(T, h, D).mul(size).bfloat16().cuda() for h in (H, Hk))
+    dq, dk = (mk(T, h, D).bfloat16().cuda() for h in (H, Hk))
+    r = np.random.default_rng(T)
+    pos = np.stack([np.arange(start, start + T, dtype=np.int64).astype(np.int32)] +
+                   [r.integers(-2 ** 31, 2 ** 31, T).astype(np.int32) for _ in sections[1:]])
+    w = [None, None] if dtype is None else [(1.0 + 0.5 * mk(D)).to(dtype).cuda() for _ in range(2)]
+    return q, k, dq, dk, torch.from_numpy(pos).cuda(), *w
+
+
+CASES = [  # tokens, H, Hk, D, sections, first position
+    (1, 40, 8, 128, (64,), 1_000_003), (77, 30, 10, 64, (18,), 0), (300, 2, 2, 128, (16, 24, 24), 0), (129, 3, 1, 128, (1,), -5),
+    (64, 5, 5, 64, (32,), 2 ** 31 - 64), (33, 6, 2, 128, (31,), -2 ** 31), (200, 4, 4, 64, (0, 13, 3), 7),
+    (1000, 24, 8, 128, (32,), 100_000), (65, 12, 12, 128, (40,), 0), (3000, 16, 1, 64, (24,), 0), (2, 100, 1, 64, (7,), 3),
+]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32, None], ids=["bf16", "fp32", "none"])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("T,H,Hk,D,sections,start", CASES)
+def test_values_and_gradients(T, H, Hk, D, sections, start, layout, dtype):
+    log(f"case {T} {H}/{Hk}x{D} {sections} from {start} {layout} {dtype}")
+    q, k, dq, dk, pos, wq, wk = case(T, H, Hk, D, sections, start, dtype)
+    freqs, _ = rotary_frequencies(sections)
+    leaves = [x.requires_grad_(True) for x in (q, k, wq, wk) if x is not None]
+    qr, kr = norm_rotary(q, k, pos, freqs, wq, wk, 1e-5, layout, sections, 1.25)
+    got = torch.autograd.grad((qr, kr), leaves, (dq, dk))
+    torch.cuda.synchronize()
+    turn = (pos.cpu().numpy(), freqs, layout, sections, 1.25)
+    for i, (x, w, y, dy, name) in enumerate(((q, wq, qr, dq, "q"), (k, wk, kr, dk, "k"))):
+        check(y, *oracle.forward(np64(x), np64(w), 1e-5, *turn), name)
+        dx, dw, e_dx, e_dw = oracle.backward(np64(x), np64(dy), np64(w), 1e-5, *turn,
+                                             weight_step=2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -24)
+        check(got[i], dx, e_dx, "d" + name)
+        if w is not None:
+            assert got[2 + i].dtype == dtype
+            check(got[2 + i], dw, e_dw, f"d{name}_weight")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_norm_alone_and_turn_alone(D):
+    log(f"case parts {D}")
+    q, k, dq, dk, pos, wq, wk = case(50, 6, 2, D, (D // 4,), 3, torch.float32)
+    freqs, _ = rotary_frequencies(D // 4)
+    y = norm_rotary_apply(q, k, None, None, wq, wk, 1e-6)
+    for x, w, o in ((q, wq, y[0]), (k, wk, y[1])):
+        check(o, *oracle.forward(np64(x), np64(w), 1e-6, None, None, None, None, None), "norm alone")
+    d = norm_rotary_bwd(q, k, dq, dk, None, None, wq, wk)
+    for x, w, g, o, ow in ((q, wq, dq, d[0], d[2]), (k, wk, dk, d[1], d[3])):
+        dx, dw, e_dx, e_dw = oracle.backward(np64(x), np64(g), np64(w), 1e-6, None, None, None, None, None)
+        check(o, dx, e_dx, "its gradient")
+        check(ow, dw, e_dw, "its weight's")
+    for layout in ("half", "interleaved"):
+        same_turn(norm_rotary_apply(q, k, pos, freqs, eps=None, layout=layout), rotary_apply(q, k, pos, freqs, layout), q, k)
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("pairs", [64, 32, 21])
+def test_slices_single_tensors_and_outputs(pairs, layout):
+    log(f"case slices {pairs} {layout}")
+    T, H, Hk, D = 50, 6, 2, 128
+    qkv = torch.randn(T, H + 2 * Hk, D, generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    grad = torch.randn(T, H + 2 * Hk, D, generator=torch.Generator().manual_seed(2)).bfloat16().cuda()
+    q, k, gq, gk = qkv[:, :H], qkv[:, H:H + Hk], grad[:, 1:H + 1], grad[:, H + 1:H + 1 + Hk]
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")
+    freqs, _ = rotary_frequencies(pairs)
+    w = torch.linspace(0.5, 2.0, 2 * D + 1).bfloat16().cuda()
+    wq, wk = w[1:D + 1], w[D + 1:]  # at odd addresses
+    both = norm_rotary_apply(q, k, pos, freqs, wq, wk, layout=layout)
+    whole = norm_rotary_apply(q.contiguous(), k.contiguous(), pos, freqs, wq.clone(), wk.clone(), layout=layout)
+    buf = torch.full((2, T, H, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    only_q = norm_rotary_apply(q, None, pos, freqs, wq, layout=layout, q_out=buf[0])
+    only_k = norm_rotary_apply(None, k, pos, freqs, k_weight=wk, layout=layout)
+    torch.cuda.synchronize()
+    assert torch.equal(both[0], whole[0]) and torch.equal(both[1], whole[1])
+    assert torch.equal(only_q[0], both[0]) and only_q[1] is None and torch.equal(only_k[1], both[1])
+    assert (buf[1] == 7.0).all()  # rows behind the last are left as they were
+    back = norm_rotary_bwd(q, k, gq, gk, pos, freqs, wq, wk, layout=layout)
+    dense = norm_rotary_bwd(q.contiguous(), k.contiguous(), gq.contiguous(), gk.contiguous(), pos, freqs, wq, wk, layout=layout)
+    assert all(torch.equal(x, y) for x, y in zip(back, dense))
+    one = norm_rotary_bwd(None, k, None, gk, pos, freqs, None, wk, layout=layout)
+    assert one[0] is None and one[2] is None and torch.equal(one[1], back[1]) and torch.equal(one[3], back[3])
+    e = norm_rotary_apply(q[:0], k[:0], pos[:0], freqs, wq, wk, layout=layout)
+    assert e[0].shape == (0, H, D)
+    z = norm_rotary_bwd(q[:0], k[:0], gq[:0], gk[:0], pos[:0], freqs, wq, wk, layout=layout)
+    assert (z[2] == 0).all() and (z[3] == 0).all() and z[2].shape == (D,)
+
+
+@pytest.mark.parametrize("layout,pairs", [("half", 32), ("half", 64), ("half", 19), ("interleaved", 40)])
+def test_odd_values_stay_in_their_rows(layout, pairs):
+    log(f"case odd values {layout} {pairs}")
+    q, k, dq, dk, pos, wq, wk = case(40, 4, 2, 128, (pairs,), 0, torch.float32, scale=1.0)
+    freqs, _ = rotary_frequencies(pairs)
+    clean = norm_rotary_apply(q, k, pos, freqs, wq, wk, layout=layout)
+    clean_d = norm_rotary_bwd(q, k, dq, dk, pos, freqs, wq, wk, layout=layout)
+    q2, k2, dq2 = q.clone(), k.clone(), dq.clone()
+    q2[3, 1, 5] = float("inf")
+    k2[7, 0, 127] = float("nan")
+    q2[9, 2] = 0.0
+    q2[11, 0] *= 2.0 ** 100  # squares pass the range of 32 bits: 1 / inf
+    dq2[13, 3, 0] = float("nan")
+    odd = norm_rotary_apply(q2, k2, pos, freqs, wq, wk, layout=layout)
+    d = norm_rotary_bwd(q2, k2, dq2, dk, pos, freqs, wq, wk, layout=layout)
+    torch.cuda.synchronize()
+    rows = torch.ones(40, 4, dtype=torch.bool)
+    for t, h in ((3, 1), (9, 2), (11, 0)):
+        rows[t, h] = False
+    assert torch.equal(odd[0][rows], clean[0][rows])
+    assert odd[0][3, 1].isnan().any() and (odd[0][9, 2] == 0).all()
+    krows = torch.ones(40, 2, dtype=torch.bool)
+    krows[7, 0] = False
+    assert torch.equal(odd[1][krows], clean[1][krows]) and odd[1][7, 0].isnan().all()
+    rows[13, 3] = False
+    assert torch.equal(d[0][rows], clean_d[0][rows]) and d[0][13, 3].isnan().all()
+    x, g = np64(q2)[9:10, 2:3], np64(dq2)[9:10, 2:3]
+    dx, _, e, _ = oracle.backward(x, g, np64(wq), 1e-6, np.array([[9]]), freqs, layout, (pairs,), 1.0)
+    check(d[0][9:10, 2:3], dx, e, "a row of zeros")
+    # without a norm the copied dimensions keep their infinities beside the turned ones
+    same_turn(norm_rotary_apply(q2, k2, pos, freqs, eps=None, layout=layout), rotary_apply(q2, k2, pos, freqs, layout), q2, k2)
+
+
+def test_gradients_asked_for_in_part():
+    log("case part of the gradients")
+    q, k, dq, dk, pos, wq, wk = case(20, 4, 2, 64, (32,), 0, torch.bfloat16)
+    freqs, _ = rotary_frequencies(32)
+    ref = norm_rotary_bwd(q, k, dq, dk, pos, freqs, wq, wk)
+    k.requires_grad_(True)
+    wk.requires_grad_(True)
+    qr, kr = norm_rotary(q, k, pos, freqs, wq, wk)
+    g = torch.autograd.grad(kr, (k, wk), dk)  # q's output unused
+    assert torch.equal(g[0], ref[1]) and torch.equal(g[1], ref[3])
+    wide = torch.empty(20, 2, 66, dtype=torch.bfloat16, device="cuda")[..., :64].copy_(dk)  # a gradient that no call takes as it is
+    qr, kr = norm_rotary(q, k, pos, freqs, wq, wk)
+    assert torch.equal(torch.autograd.grad(kr, k, wide)[0], ref[1])
+    wq.requires_grad_(True)
+    qr, kr = norm_rotary(q, k.detach(), pos, freqs, wq, wk.detach())
+    assert torch.equal(torch.autograd.grad(qr, wq, dq)[0], ref[2])
+    wq = wq.detach().requires_grad_(True)
+    qr, _ = norm_rotary(q, None, pos, freqs, wq)
+    (gx,) = torch.autograd.grad(qr.float().square().sum(), wq, create_graph=True)
+    with pytest.raises(RuntimeError):
+        gx.float().sum().backward()
+
+
+def test_forward_mode_is_refused():
+    import torch.autograd.forward_ad as fwAD
+    q, k, dq, dk, pos, wq, wk = case(5, 4, 2, 64, (32,), 0, None)
+    freqs, _ = rotary_frequencies(32)
+    with fwAD.dual_level():
+        with pytest.raises(Exception, match="forward"):
+            norm_rotary(fwAD.make_dual(q, torch.ones_like(q)), k, pos, freqs)
+
+
+def test_offsets_beyond_32_bits():
+    log("case large")
+    T, H, D = 600_000, 32, 128  # 2.46e9 elements
+    q = torch.randn(1, H, D, device="cuda").bfloat16().repeat(T, 1, 1)
+    q[-3:] = torch.randn(3, H, D, device="cuda").bfloat16()
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")
+    freqs, _ = rotary_frequencies(64)
+    w = torch.ones(D, device="cuda")
+    out, _ = norm_rotary_apply(q, None, pos, freqs, w)
+    tail, _ = norm_rotary_apply(q[-5:], None, pos[-5:], freqs, w)
+    assert torch.equal(out[-5:], tail)
+    d = norm_rotary_bwd(q, None, out, None, pos, freqs, w)
+    t = norm_rotary_bwd(q[-5:], None, out[-5:], None, pos[-5:], freqs, w)
+    assert torch.equal(d[0][-5:], t[0])
+    # dw = sum n^2 here: every row's squares sum to D
+    assert abs(d[2].double().sum().item() / (T * H * D) - 1.0) < 2.0 ** -7
+
+
+def test_streams_and_determinism():
+    log("case streams")
+    q, k, dq, dk, pos, wq, wk = case(3000, 12, 4, 128, (64,), 0, torch.float32)
+    freqs, _ = rotary_frequencies(64)
+    ref = (*norm_rotary_apply(q, k, pos, freqs, wq, wk), *norm_rotary_bwd(q, k, dq, dk, pos, freqs, wq, wk))
+    torch.cuda.synchronize()
+    s = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for i in range(6):
+        got.append((*norm_rotary_apply(q, k, pos, freqs, wq, wk, stream=s[i % 2]),
+                    *norm_rotary_bwd(q, k, dq, dk, pos, freqs, wq, wk, stream=s[i % 2])))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for g in got for a, b in zip(g, ref))
+
+
+def test_captured_training_step():
+    log("case capture")
+    q, k, dq, dk, pos, wq, wk = case(700, 6, 2, 64, (18,), 0, torch.bfloat16)
+    freqs, _ = rotary_frequencies(18)
+    leaves = [x.requires_grad_(True) for x in (q, k, wq, wk)]
+
+    def step():
+        out = norm_rotary(q, k, pos, freqs, wq, wk)
+        return (*(o.detach() for o in out), *torch.autograd.grad(out, leaves, (dq, dk)))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step()
+    for i in range(4):
+        with torch.no_grad():
+            q.mul_(-0.5 if i % 2 else 1.5)
+            wq.add_(0.125)
+            pos.add_(17)
+        graph.replay()
+        eager = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(captured, eager)), i
