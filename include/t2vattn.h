@@ -321,6 +321,46 @@ int t2v_norm_rotary_bwd(const void* q, const void* k, int64_t q_stride, int64_t 
                         int kv_heads, int head_dim, const t2v_turn* turn, void* dq, void* dk, void* dq_weight,
                         void* dk_weight, void* ws, uint64_t ws_bytes, uint64_t* need, void* stream);
 
+/* A paged cache: the keys and values of many sequences in pages of page_size tokens that a table assigns to them, so that
+ * sequences grow, fork and end without moving each other. Key j of sequence s is row j % page_size of page
+ * table[s * table_stride + j / page_size]. Table, lengths and the calls' offsets are in DEVICE memory and read by the kernels: no host work or
+ * upload follows them, and a captured call, replayed, takes what they hold then. */
+typedef struct {
+  void* k;                  /* device bf16 [pages, page_size, kv_heads, head_dim], 16-byte aligned */
+  void* v;                  /* as k, with strides of its own */
+  int64_t k_strides[3];     /* elements between pages, between a page's tokens, between a token's heads: multiples of 8; a page's */
+  int64_t v_strides[3];     /* rows do not overlap, and pages lie one behind the other (K and V may alternate) */
+  int64_t pages;            /* 0 .. 2^31 - 1 */
+  const int32_t* table;     /* device [nseq, width], rows table_stride entries apart */
+  int64_t table_stride;
+  int width;                /* pages that a sequence may have; width * page_size < 2^31 */
+  const int32_t* lengths;   /* device [nseq]: keys of each sequence, those of the call's own tokens the last; <= 0: none */
+  int nseq;
+  int page_size;            /* a power of two from 16 to 2^16 */
+  int kv_heads;
+  int head_dim;             /* 64 or 128 */
+} t2v_pages;
+
+/* Causal attention with grouped heads over a paged cache, in one call for single tokens, chunks and whole prompts: of sequence s with Lq
+ * queries and lengths[s] keys, query i sees keys 0 .. i + lengths[s] - Lq, as in t2v_causal_fwd (empty rows, infinities
+ * and NaN too; what stands in a page behind a sequence's last key is not read).
+ *   q            device bf16 [tokens, heads, D], read only, q_stride elements between tokens as in t2v_causal_fwd
+ *   cu_seqlens   DEVICE int32 [nseq + 1], rows of q: non-decreasing from 0; rows from cu_seqlens[nseq] on are padding, whose results are
+ *                left as they were
+ *   max_queries  the most queries that a sequence has, or 0 if not known: it saves a launch where it shows that all have few, or that
+ *                one sequence has all, and changes results by rounding only
+ *   cache        HOST struct, read before the call returns
+ *   out, lse     device bf16 [tokens, heads, D], contiguous, and fp32 [heads, tokens], written
+ *   ws, need     as in t2v_causal_fwd; need follows from the sizes given here, not from lengths: at most 80 MiB
+ * The arrays in device memory cannot be checked before the launch. Whatever they hold, nothing outside the tensors is read or written,
+ * and what cannot be right shows: keys in a page outside the cache count as NaN for the queries that see them, a
+ * sequence longer than its row of the table gets NaN results. Offsets that decrease give unspecified results. tokens * heads / kv_heads must stay below 2^31.
+ * Deterministic, no atomics: how the work is divided follows from offsets, lengths and sizes; a
+ * sequence's last bits may depend on the others in the call. T2V_SPLIT and the other settings have no effect here. */
+int t2v_paged_fwd(const void* q, int64_t q_stride, int heads, const int32_t* cu_seqlens, int64_t tokens, int max_queries,
+                  const t2v_pages* cache, float scale, void* out, float* lse, void* ws, uint64_t ws_bytes,
+                  uint64_t* need, void* stream);
+
 /* Thread-local message describing the last non-OK status of this thread. */
 const char* t2v_last_error(void);
 

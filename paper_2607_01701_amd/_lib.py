@@ -37,7 +37,7 @@ EXPORTS = ("t2v_attn_fwd", "t2v_attn_bwd", "t2v_attn_fwd_qk", "t2v_attn_bwd_qk",
            "t2v_release_cache", "t2v_build_worklist", "t2v_plan_makespan", "t2v_timing_enable", "t2v_kernel_times",
            "t2v_version", "t2v_list_schedule", "t2v_plan_cascades", "t2v_probe_mfma_peak", "t2v_trace_set",
            "t2v_trace_count", "t2v_attn_bwd_noalloc", "t2v_attn_bwd_qk_ws", "t2v_causal_fwd", "t2v_causal_bwd",
-           "t2v_rotary", "t2v_norm_rotary", "t2v_norm_rotary_bwd")
+           "t2v_rotary", "t2v_norm_rotary", "t2v_norm_rotary_bwd", "t2v_paged_fwd")
 KERNEL_SLOTS = ("fwd", "bwd_pre", "bwd_dkdv", "bwd_dq")
 HOST_EXPORTS = ("t2v_last_error", "t2v_build_worklist", "t2v_plan_makespan", "t2v_version", "t2v_list_schedule",
                 "t2v_plan_cascades")
@@ -53,6 +53,14 @@ class Turn(ctypes.Structure):
     _fields_ = [("positions", _vp), ("freqs", _vp), ("sections", _vp), ("n_sections", ctypes.c_int), ("layout", ctypes.c_int),
                 ("mscale", ctypes.c_float), ("eps", ctypes.c_float), ("q_weight", _vp), ("k_weight", _vp),
                 ("weights_f32", ctypes.c_int)]
+
+
+class PagesStruct(ctypes.Structure):
+    """t2v_pages: a paged cache."""
+    _fields_ = [("k", _vp), ("v", _vp), ("k_strides", ctypes.c_int64 * 3), ("v_strides", ctypes.c_int64 * 3),
+                ("pages", ctypes.c_int64), ("table", _vp), ("table_stride", ctypes.c_int64), ("width", ctypes.c_int),
+                ("lengths", _vp), ("nseq", ctypes.c_int), ("page_size", ctypes.c_int), ("kv_heads", ctypes.c_int),
+                ("head_dim", ctypes.c_int)]
 
 
 class T2VError(RuntimeError):
@@ -115,6 +123,9 @@ def _declare(lib, full: bool):
         lib.t2v_norm_rotary_bwd.restype = ctypes.c_int
         lib.t2v_norm_rotary_bwd.argtypes = [_vp, _vp, i64, i64, _vp, _vp, i64, i64, i64, ctypes.c_int, ctypes.c_int,
                                             ctypes.c_int, turnp, _vp, _vp, _vp, _vp, _vp, ctypes.c_uint64, _u64p, _vp]
+        lib.t2v_paged_fwd.restype = ctypes.c_int
+        lib.t2v_paged_fwd.argtypes = [_vp, i64, ctypes.c_int, _vp, i64, ctypes.c_int, ctypes.POINTER(PagesStruct), ctypes.c_float,
+                                      _vp, _vp, _vp, ctypes.c_uint64, _u64p, _vp]
         lib.t2v_release_cache.restype = None
         lib.t2v_release_cache.argtypes = []
         lib.t2v_timing_enable.restype = ctypes.c_int

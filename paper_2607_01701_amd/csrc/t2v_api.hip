@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -17,6 +18,8 @@
 #include "t2v_causal_kernels.h"
 #include "t2v_host.h"
 #include "t2v_kernels.h"
+#include "t2v_paged_host.h"
+#include "t2v_paged_kernels.h"
 
 // The no-allocation backward's scratch (see attn_bwd_noalloc_impl): one per GPU, held until
 // the process ends. Host code must not use this name as a device address.
@@ -849,7 +852,8 @@ int check_arm() {
   const unsigned int canary = check_canary();
   unsigned int rec[4];
   for (auto take : {fwd_check_take, dkdv_check_take, dkdv_wide_check_take, dq_check_take, short_check_take,
-                    causal_fwd_check_take, causal_dkdv_check_take, causal_dkdv_wide_check_take, causal_dq_check_take}) {
+                    causal_fwd_check_take, causal_dkdv_check_take, causal_dkdv_wide_check_take, causal_dq_check_take,
+                    paged_fwd_check_take}) {
     const hipError_t e = take(rec, canary);
     if (e != hipSuccess) return hip_fail(e, "clearing the DMA row checks");
   }
@@ -861,12 +865,12 @@ int check_arm() {
 int check_collect(hipStream_t s) {
   hipError_t e = hipStreamSynchronize(s);
   if (e != hipSuccess) return hip_fail(e, "waiting for the checked kernels");
-  constexpr int kSources = 9;
+  constexpr int kSources = 10;
   const char* names[kSources] = {"forward",        "dK/dV",        "dK/dV",        "dQ", "one-pass backward",
-                                 "causal forward", "causal dK/dV", "causal dK/dV", "causal dQ"};
+                                 "causal forward", "causal dK/dV", "causal dK/dV", "causal dQ",    "paged forward"};
   hipError_t (*takes[kSources])(unsigned int*, unsigned int) = {
       fwd_check_take,        dkdv_check_take,        dkdv_wide_check_take,        dq_check_take,       short_check_take,
-      causal_fwd_check_take, causal_dkdv_check_take, causal_dkdv_wide_check_take, causal_dq_check_take};
+      causal_fwd_check_take, causal_dkdv_check_take, causal_dkdv_wide_check_take, causal_dq_check_take,    paged_fwd_check_take};
   int status = T2V_OK;
   for (int i = 0; i < kSources; ++i) {
     unsigned int rec[4];
@@ -1554,6 +1558,84 @@ int causal_bwd_impl(CausalCall& c, const void* out, const float* lse, const void
   return T2V_OK;
 }
 
+// ------------------------------------------------------------------ attention over a paged cache
+
+// The kernels that a call takes, their workgroups and places in the workspace. Where rows of several sequences may be few or many, the
+// kernel of 32-row tiles takes those with few, the other one the rest. Workgroups: as many as the GPU holds at once, or as
+// the call can use at the least share that a workgroup takes.
+int paged_parts(const PagedCall& c, int max_queries, int ncu, PagedPart (&parts)[2], uint64_t* bytes) {
+  const t2v_pages& g = c.cache;
+  const int64_t group = c.heads / g.kv_heads, room = static_cast<int64_t>(g.width) * g.page_size;
+  int64_t most = c.tokens;  // queries of a sequence, as far as is known
+  if (max_queries > 0) most = std::min<int64_t>(most, max_queries);
+  const bool all_few = (max_queries > 0 || c.tokens <= g.nseq ? (max_queries > 0 ? most : 1) : most) * group <= paged_tile_rows(true);
+  const bool all_many = !all_few && g.nseq == 1;
+  int n = 0;
+  if (!all_many) parts[n++] = {all_few ? kPagedAll : kPagedFew, true, 0, 0};
+  if (!all_few) parts[n++] = {all_many ? kPagedAll : kPagedMany, false, 0, 0};
+  *bytes = 0;
+  for (int i = 0; i < n; ++i) {
+    PagedPart& p = parts[i];
+    const double tiles = static_cast<double>(c.tokens * group / paged_tile_rows(p.few) + g.nseq) * g.kv_heads;
+    const double pieces = tiles * static_cast<double>((room + paged_least_share(p.few) - 1) / paged_least_share(p.few) + 1);
+    p.shares = static_cast<int>(std::min<double>(paged_workgroups(p.few, g.head_dim, ncu), std::max(1.0, pieces)));
+    if (p.shares > kNumXcd) p.shares = p.shares / kNumXcd * kNumXcd;
+    p.at = static_cast<int64_t>(*bytes);
+    *bytes += static_cast<uint64_t>(paged_part_bytes(p, g.head_dim));
+  }
+  return n;
+}
+
+int paged_fwd_impl(PagedCall& c, int max_queries, const t2v_pages* cache, void* ws, uint64_t ws_bytes, uint64_t* need, void* stream) {
+  if (need != nullptr) *need = 0;
+  if (int st = check_pages(cache)) return st;
+  c.cache = *cache;
+  const t2v_pages& g = c.cache;
+  auto bad = [](const std::string& what) { return set_error(T2V_ERR_INVALID_ARG, what); };
+  if (c.heads < 1 || c.heads % g.kv_heads != 0)
+    return bad("heads (" + std::to_string(c.heads) + ") must be a multiple of kv_heads (" + std::to_string(g.kv_heads) + ")");
+  if (static_cast<int64_t>(c.heads) * g.head_dim > (int64_t(1) << 22)) return bad("heads * head_dim is too large");
+  if (!std::isfinite(c.scale)) return bad("scale must be finite");
+  if (max_queries < 0) return bad("max_queries must be >= 0");
+  if (c.tokens < 0 || c.tokens * (c.heads / g.kv_heads) > INT32_MAX - 512) return bad("tokens times the heads of a group must be in 0 .. 2^31 - 513");
+  if (c.q_stride < static_cast<int64_t>(c.heads) * g.head_dim || c.q_stride % 8 != 0 || c.q_stride > (int64_t(1) << 22))
+    return bad("q_stride must be a multiple of 8 between heads * head_dim and 2^22, got " + std::to_string(c.q_stride));
+  if (c.tokens == 0 || g.nseq == 0) return T2V_OK;
+  // The kernels count a call's work (at most so much) in 64 bits, a share's number times a share's length included.
+  const double group = c.heads / g.kv_heads, room = static_cast<double>(g.width) * g.page_size;
+  if ((c.tokens * group / paged_tile_rows(true) + g.nseq) * group * (room + 4096.0 + c.tokens) * g.kv_heads > 0x1p52)
+    return bad("the call's largest possible work (queries times the table's width) passes what the kernels count");
+  const std::vector<Range> out = {{c.out, tensor_bytes(c.tokens, c.heads, g.head_dim), "out"}, {c.lse, c.tokens * c.heads * 4, "lse"},
+                                  {ws, static_cast<int64_t>(ws_bytes), "ws"}};
+  if (int st = validate_nonempty({{c.q, strided_bytes(c.tokens, c.q_stride, c.heads, g.head_dim), "q"},
+                                  {g.k, pages_bytes(g, g.k_strides), "cache.k"},
+                                  {g.v, pages_bytes(g, g.v_strides), "cache.v"}}, out))
+    return st;
+  if (int st = check_tables_apart(g, c.cu, out)) return st;
+  PagedPart parts[2];
+  uint64_t bytes = 0;
+  const int n = paged_parts(c, max_queries, cu_count(), parts, &bytes);
+  if (need != nullptr) *need = bytes;
+  if (int st = check_workspace(ws_bytes, bytes)) return st;
+  const auto s = static_cast<hipStream_t>(stream);
+#if T2V_CHECKED
+  if (int st = check_arm()) return st;
+#endif
+  bool cut = false;
+  for (int i = 0; i < n; ++i) {
+    c.trace = tracer().reserve(parts[i].shares);
+    cut |= parts[i].shares > 1;
+    const bool last = i + 1 == n;
+    const hipError_t e = timer().run(kSlotFwd, s, [&] {
+      hipError_t r = launch_paged_fwd(c, parts[i], ws, s);
+      if (r == hipSuccess && last && cut) r = launch_paged_join(c, parts, n, ws, s);
+      return r;
+    });
+    if (e != hipSuccess) return hip_fail(e, "paged forward kernel launch");
+  }
+  return T2V_OK;
+}
+
 // Runs f, turning host exceptions into statuses (none may cross the C ABI).
 template <typename F>
 int guarded(F&& f) {
@@ -1698,6 +1780,15 @@ int t2v_causal_bwd(const void* q, const void* k, const void* v, int64_t q_stride
     return t2v::checked_call(stream, [&] {
       return t2v::causal_bwd_impl(c, out, lse, dout, dq, dk, dv, delta_ws, ws, ws_bytes, need, stream);
     });
+  });
+}
+
+int t2v_paged_fwd(const void* q, int64_t q_stride, int heads, const int32_t* cu_seqlens, int64_t tokens, int max_queries,
+                  const t2v_pages* cache, float scale, void* out, float* lse, void* ws, uint64_t ws_bytes, uint64_t* need,
+                  void* stream) {
+  return t2v::guarded([&] {
+    t2v::PagedCall c{q, q_stride, heads, cu_seqlens, tokens, {}, scale, out, lse, nullptr};
+    return t2v::checked_call(stream, [&] { return t2v::paged_fwd_impl(c, max_queries, cache, ws, ws_bytes, need, stream); });
   });
 }
 

@@ -1,0 +1,111 @@
+// Division of paged attention among workgroups (csrc/t2v_paged.h) on random batches: every key of every tile is taken by exactly one
+// share, pieces fill their slots and no others, no piece is shorter than the rule allows.
+#include <algorithm>
+#include <cstdio>
+#include <cstdlib>
+#include <map>
+#include <random>
+#include <vector>
+
+#include "../paper_2607_01701_amd/csrc/t2v_paged.h"
+
+using namespace t2v;
+
+static void fail(const char* what, int n) {
+  std::printf("batch %d: %s\n", n, what);
+  std::exit(1);
+}
+
+int main() {
+  std::mt19937 g(5);
+  auto pick = [&](int lo, int hi) { return std::uniform_int_distribution<int>(lo, hi)(g); };
+  int64_t cut = 0, empty = 0;
+  for (int n = 0; n < 4000; ++n) {
+    const int group = std::vector<int>{1, 2, 3, 4, 5, 7, 8, 16, 40}[pick(0, 8)];
+    const bool few = pick(0, 1);
+    PagedRule r{group, few ? 32 : 128, few ? 128 : 64, 0, pick(0, 600), 0, pick(0, 2), 32};
+    r.least = r.unit * pick(1, 3);
+    r.share = r.unit * pick(1, 4);
+    const int kv = pick(1, 4), nseq = pick(0, 9), shares = pick(1, 64), room = 5000;
+    std::vector<int> cu{0}, len;
+    for (int s = 0; s < nseq; ++s) {
+      const int longest = pick(0, 3) == 0 ? 6000 : 300;
+      len.push_back(pick(-2, longest));
+      cu.push_back(cu.back() + (pick(0, 3) == 0 ? pick(0, 300) : pick(0, 2)));
+    }
+    const int64_t tokens = std::max(0, cu.back() + pick(-1, 2));
+    if (nseq && pick(0, 9) == 0) cu[pick(0, nseq)] = pick(-3, 900);  // offsets that decrease: nothing outside is touched
+    struct Tile {
+      std::vector<int> seen;
+      int pieces = 0, wanted = -1, starter = -1, whole = 0;
+    };
+    std::map<std::vector<int>, Tile> tiles;
+    int64_t per_head = 0;
+    std::vector<int64_t> cost;
+    for (int s = 0; s < nseq; ++s) {
+      const PagedSeq q = paged_seq(cu[s], cu[s + 1], len[s], tokens, room);
+      if (q.q0 < 0 || q.lq < 0 || q.q0 + q.lq > tokens || q.lk < 0 || q.lk > room) fail("rows outside", n);
+      const PagedTiles t = paged_tiles(r, q);
+      cost.push_back(paged_cost(r, t));
+      per_head += cost.back();
+      for (int h = 0; h < kv; ++h)
+        for (int i = 0; i < t.tiles; ++i) {
+          tiles[{h, s, i}].seen.assign(paged_keys(r, q, t, i), 0);
+          if (paged_before(r, t, i + 1) <= paged_before(r, t, i)) fail("a tile without an interval", n);
+        }
+    }
+    const int64_t total = per_head * kv, length = paged_share(r, total, shares);
+    if (length * shares < total) fail("shares too short", n);
+    std::vector<char> slots(2 * shares, 0);
+    for (int i = 0; i < shares; ++i) {
+      int64_t from = i * length;
+      const int64_t to = std::min(total, (i + 1) * length);
+      int64_t at = 0;
+      for (int h = 0; h < kv; ++h)
+        for (int s = 0; s < nseq; at += cost[s], ++s) {
+          if (from >= to || from < at || from >= at + cost[s]) continue;
+          const PagedSeq q = paged_seq(cu[s], cu[s + 1], len[s], tokens, room);
+          const PagedTiles t = paged_tiles(r, q);
+          for (int k = paged_tile_at(r, t, from - at); k < t.tiles && from < to; ++k) {
+            const int64_t a = at + paged_before(r, t, k), b = at + paged_before(r, t, k + 1);
+            if (from < a || from >= b) fail("a position outside its tile", n);
+            PagedPiece p;
+            if (paged_piece(r, q, t, k, a, from, std::min(to, b), length, i, &p)) {
+              Tile& x = tiles[{h, s, k}];
+              if (p.begin % r.unit || p.begin < 0 || p.end > p.n || (p.n && p.begin >= p.end)) fail("a piece's keys", n);
+              if (p.end < p.n && p.end % r.unit) fail("a piece's end", n);
+              for (int j = p.begin; j < p.end; ++j) ++x.seen[j];
+              if (p.slot < 0) {
+                ++x.whole;
+                if (p.begin != 0 || p.end != p.n) fail("a part without a slot", n);
+              } else {
+                ++cut;
+                if (p.end - p.begin < std::min(r.least, r.share)) fail("a short piece", n);
+                if (p.slot < 0 || p.slot >= 2 * shares || slots[p.slot]++) fail("a slot twice", n);
+                if (p.begin == 0) {
+                  x.starter = i;
+                  x.wanted = p.pieces;
+                  if (p.slot != 2 * i + 1) fail("a first slot", n);
+                } else if (x.starter < 0 || p.slot != 2 * (x.starter + x.pieces)) {
+                  fail("slots out of order", n);
+                }
+                ++x.pieces;
+              }
+            }
+            from = std::min(to, b);
+          }
+        }
+      if (from < to) fail("a share's end", n);
+    }
+    for (auto& kv_ : tiles) {
+      Tile& x = kv_.second;
+      for (int c : x.seen)
+        if (c != 1) fail("a key not taken once", n);
+      if (x.seen.empty()) ++empty;
+      if (x.whole + (x.pieces > 0) != 1) fail("a tile not done once", n);
+      if (x.pieces && (x.pieces != x.wanted || x.pieces < 2)) fail("pieces miscounted", n);
+    }
+  }
+  std::printf("ok: 4000 batches, %lld pieces, %lld tiles without keys\n", static_cast<long long>(cut), static_cast<long long>(empty));
+  return 0;
+}
