@@ -361,6 +361,29 @@ int t2v_paged_fwd(const void* q, int64_t q_stride, int heads, const int32_t* cu_
                   const t2v_pages* cache, float scale, void* out, float* lse, void* ws, uint64_t ws_bytes,
                   uint64_t* need, void* stream);
 
+/* Stores the keys and values of new tokens in their pages, with the norm and the turn of t2v_norm_rotary for the keys (and, beside them, for
+ * the queries of the same tokens) in the same pass. Of sequence s with Lq tokens, token i is key lengths[s] - Lq + i.
+ *   k, v         device bf16 [tokens, kv_heads, D] of the cache, read only, with strides as in t2v_causal_fwd
+ *   q, q_out     device bf16 [tokens, heads, D], q with a stride, q_out contiguous and written; heads 0: none
+ *   cu_seqlens, cache   as in t2v_paged_fwd (the pages are written); K's and V's rows must not be the same memory
+ *   turn         HOST struct or NULL: keys are stored as they are, and heads must be 0
+ * A token without a place (a key below 0 or beyond the table's width, a page outside the cache) is not stored; padding behind the last
+ * sequence neither, and its q_out is left as it was. Other rows of the pages stay as they are. Pages that two sequences share must
+ * not both get tokens in one row. */
+int t2v_paged_append(const void* k, const void* v, int64_t k_stride, int64_t v_stride, const void* q, int64_t q_stride,
+                     int heads, const int32_t* cu_seqlens, int64_t tokens, const t2v_pages* cache, const t2v_turn* turn,
+                     void* q_out, void* stream);
+
+/* Copies pages src[i] to pages dst[i] (i < n) in each of n_buffers caches: forked sequences that go on in a page which others
+ * share, and pages moved together.
+ *   buffers      HOST array of device pointers, 16-byte aligned: page p of a buffer is page_bytes bytes at p * page_stride
+ *   pages        of each buffer; page_bytes and page_stride (bytes) multiples of 16, page_bytes <= page_stride
+ *   src, dst     HOST int32 [n], in 0 .. pages - 1; a page may be copied to several, but no page is written twice, nor both read and
+ *                written: T2V_ERR_INVALID_ARG
+ * Reads the HOST arrays before it returns. Buffers must not overlap, unless by pages that lie between each other's. */
+int t2v_page_copy(void* const* buffers, int n_buffers, int64_t pages, int64_t page_stride, int64_t page_bytes,
+                  const int32_t* src, const int32_t* dst, int n, void* stream);
+
 /* Thread-local message describing the last non-OK status of this thread. */
 const char* t2v_last_error(void);
 

@@ -10,5 +10,5 @@ from ._lib import (  # noqa: F401
 )
 from .autograd import varlen_attention, varlen_causal_attention  # noqa: F401
 from .norm_rotary import norm_rotary, norm_rotary_apply, norm_rotary_bwd  # noqa: F401
-from .paged import Pages, paged_attn_fwd  # noqa: F401
+from .paged import PagedCache, Pages, page_copy, paged_append, paged_attn_fwd  # noqa: F401
 from .rotary import rotary, rotary_apply, rotary_frequencies  # noqa: F401

@@ -37,7 +37,8 @@ EXPORTS = ("t2v_attn_fwd", "t2v_attn_bwd", "t2v_attn_fwd_qk", "t2v_attn_bwd_qk",
            "t2v_release_cache", "t2v_build_worklist", "t2v_plan_makespan", "t2v_timing_enable", "t2v_kernel_times",
            "t2v_version", "t2v_list_schedule", "t2v_plan_cascades", "t2v_probe_mfma_peak", "t2v_trace_set",
            "t2v_trace_count", "t2v_attn_bwd_noalloc", "t2v_attn_bwd_qk_ws", "t2v_causal_fwd", "t2v_causal_bwd",
-           "t2v_rotary", "t2v_norm_rotary", "t2v_norm_rotary_bwd", "t2v_paged_fwd")
+           "t2v_rotary", "t2v_norm_rotary", "t2v_norm_rotary_bwd", "t2v_paged_fwd", "t2v_paged_append",
+           "t2v_page_copy")
 KERNEL_SLOTS = ("fwd", "bwd_pre", "bwd_dkdv", "bwd_dq")
 HOST_EXPORTS = ("t2v_last_error", "t2v_build_worklist", "t2v_plan_makespan", "t2v_version", "t2v_list_schedule",
                 "t2v_plan_cascades")
@@ -126,6 +127,11 @@ def _declare(lib, full: bool):
         lib.t2v_paged_fwd.restype = ctypes.c_int
         lib.t2v_paged_fwd.argtypes = [_vp, i64, ctypes.c_int, _vp, i64, ctypes.c_int, ctypes.POINTER(PagesStruct), ctypes.c_float,
                                       _vp, _vp, _vp, ctypes.c_uint64, _u64p, _vp]
+        lib.t2v_paged_append.restype = ctypes.c_int
+        lib.t2v_paged_append.argtypes = [_vp, _vp, i64, i64, _vp, i64, ctypes.c_int, _vp, i64, ctypes.POINTER(PagesStruct), turnp,
+                                         _vp, _vp]
+        lib.t2v_page_copy.restype = ctypes.c_int
+        lib.t2v_page_copy.argtypes = [_vp, ctypes.c_int, i64, i64, i64, _vp, _vp, ctypes.c_int, _vp]
         lib.t2v_release_cache.restype = None
         lib.t2v_release_cache.argtypes = []
         lib.t2v_timing_enable.restype = ctypes.c_int

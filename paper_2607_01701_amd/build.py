@@ -29,7 +29,7 @@ CHECKED_FLAGS = ["-DT2V_CHECKED=1"]
 
 HIP_SOURCES = ["t2v_fwd.hip", "t2v_bwd_pre.hip", "t2v_bwd_dkdv.hip", "t2v_bwd_dkdv_wide.hip",
                "t2v_bwd_dq.hip", "t2v_bwd_short.hip", "t2v_causal_fwd.hip", "t2v_causal_dkdv.hip",
-               "t2v_causal_dkdv_wide.hip", "t2v_causal_dq.hip", "t2v_rotary.hip", "t2v_norm_rotary.hip", "t2v_paged_fwd.hip",
+               "t2v_causal_dkdv_wide.hip", "t2v_causal_dq.hip", "t2v_rotary.hip", "t2v_norm_rotary.hip", "t2v_paged_fwd.hip", "t2v_page_copy.hip",
                "t2v_api.hip", "t2v_probe.hip"]
 HOST_SOURCES = ["t2v_host.cpp", "t2v_causal.cpp", "t2v_paged.cpp", "t2v_plan.cpp"]
 

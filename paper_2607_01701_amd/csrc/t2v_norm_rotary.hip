@@ -12,6 +12,7 @@
 #include "../../include/t2vattn.h"
 #include "t2v_device.hpp"
 #include "t2v_host.h"
+#include "t2v_paged_host.h"
 #include "t2v_rotary.hpp"
 
 namespace t2v {
@@ -390,6 +391,140 @@ __global__ __launch_bounds__(kThreads) void norm_weights_kernel(const float* par
     static_cast<bf16*>(o)[d] = static_cast<bf16>(sums[0]);
 }
 
+// ------------------------------------------------------------------ storing in pages
+
+struct AppendArgs {
+  NormArgs n;  // q and k (its out[1] is not used)
+  const bf16* v;
+  int64_t v_stride;
+  bf16 *k_pages, *v_pages;
+  int64_t k_page, k_token, k_head, v_page, v_token, v_head;  // strides in elements
+  const int32_t *cu, *lengths, *table;
+  int64_t table_stride;
+  int nseq, pages, shift, room;
+};
+
+constexpr int kMaxTokens = 2 * kMaxAngles / 64;  // of a workgroup
+
+// Page and row of token i, {-1, 0} if it has none, {-2, 0} behind the last sequence.
+T2V_DEV int2 place_of(const AppendArgs& a, int64_t i) {
+  int lo = 0, hi = a.nseq;  // the last s with cu[s] <= i
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (a.cu[mid] <= i)
+      lo = mid;
+    else
+      hi = mid - 1;
+  }
+  if (lo == a.nseq || a.cu[lo] > i) return make_int2(-2, 0);
+  const int64_t key = a.lengths[lo] - (a.cu[lo + 1] - i);
+  if (key < 0 || key >= a.room || a.lengths[lo] > a.room) return make_int2(-1, 0);
+  const int page = a.table[lo * a.table_stride + (key >> a.shift)];
+  if (static_cast<unsigned>(page) >= static_cast<unsigned>(a.pages)) return make_int2(-1, 0);
+  return make_int2(page, static_cast<int>(key) & ((1 << a.shift) - 1));
+}
+
+// c ? b : a, chosen as a value: a choice of three variables would become a choice of their addresses, and these stay in memory.
+template <typename T>
+T2V_DEV T pick(T a, T b, bool c) {
+  T x = c ? b : a;
+  asm("" : "+v"(x));
+  return x;
+}
+
+// As norm_rotary_kernel, with a token's heads of v after those of q and k.
+template <int D, bool INTERLEAVED, bool VIA_LDS>
+__global__ __launch_bounds__(kThreads) void paged_append_kernel(const AppendArgs p, int tokens_per_block) {
+  const NormArgs& a = p.n;
+  using Lane = RowLane<D, INTERLEAVED, VIA_LDS>;
+  constexpr int L = Lane::L, NG = kThreads / L;
+  __shared__ __attribute__((aligned(16))) float2 cs[kMaxAngles];
+  __shared__ __attribute__((aligned(16))) float wt[2][D];
+  __shared__ int2 place[kMaxTokens];
+  __shared__ float ex[VIA_LDS ? NG * (D + 4) : 1];
+  const int64_t t0 = static_cast<int64_t>(blockIdx.x) * tokens_per_block;
+  const int nt = static_cast<int>(min(static_cast<int64_t>(tokens_per_block), a.tokens - t0));
+  const int hq = a.heads[0], hk = a.heads[1], heads = hq + 2 * hk, total = nt * heads;
+  const int sub = threadIdx.x % L, group = threadIdx.x / L;
+  const Lane at(sub, a.pairs);
+  float* buf = ex + (VIA_LDS ? group * (D + 4) : 0);
+  const int st = NG / heads, sh = NG % heads;
+  auto advance = [&](RowPlace& x) {
+    x.h += sh;
+    const int c = x.h >= heads;
+    x.h -= c ? heads : 0;
+    x.t += st + c;
+  };
+  const gbf16 *q = (const gbf16*)(a.in[0]), *k = (const gbf16*)(a.in[1]), *v = (const gbf16*)(p.v);
+  int64_t qs = a.stride[0], ks = a.stride[1], vs = p.v_stride;
+  gbf16 *qo = (gbf16*)(a.out[0]), *ko = (gbf16*)(p.k_pages), *vo = (gbf16*)(p.v_pages);
+  int64_t kp = p.k_page, kt = p.k_token, kh = p.k_head, vp = p.v_page, vt = p.v_token, vh = p.v_head;
+  // Picked from scalar registers, as above.
+  asm volatile("" : "+s"(q), "+s"(k), "+s"(v), "+s"(qs), "+s"(ks), "+s"(vs), "+s"(qo), "+s"(ko), "+s"(vo));
+  asm volatile("" : "+s"(kp), "+s"(kt), "+s"(kh), "+s"(vp), "+s"(vt), "+s"(vh));
+  auto source = [&](const RowPlace& x) {
+    const bool not_q = x.h >= hq, is_v = x.h >= hq + hk;
+    return pick(pick(q, k, not_q), v, is_v) + (t0 + x.t) * pick(pick(qs, ks, not_q), vs, is_v) +
+           static_cast<int64_t>(x.h - (is_v ? hq + hk : not_q ? hq : 0)) * D;
+  };
+  RowPlace w{group / heads, group % heads};
+  bf16x8 x[kRows], y[kRows];
+  auto load = [&](RowPlace r, int r0) {
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+      if (r0 + i * NG < total) {
+        const gbf16* s = source(r);
+        x[i] = load_vec(s + at.v0);
+        y[i] = load_vec(s + at.v1);
+      }
+      advance(r);
+    }
+  };
+  load(w, group);
+  if (static_cast<int>(threadIdx.x) < nt) place[threadIdx.x] = place_of(p, t0 + threadIdx.x);
+  load_weights<D>(wt, a);
+  load_angles<D>(cs, a, t0, nt, 1.0f);
+  __syncthreads();
+  const bool plain = !a.norm && a.pairs == 0;
+  for (int r0 = group; r0 < total; r0 += kRows * NG) {
+    if (r0 != group) load(w, r0);
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+      const bool not_q = w.h >= hq, is_v = w.h >= hq + hk;
+      int2 to = make_int2(-2, 0);
+      if (r0 + i * NG < total) to = place[w.t];
+      if (to.x >= (not_q ? 0 : -1)) {
+        bf16x8 z0 = x[i], z1 = y[i];
+        if (!is_v && !plain) {
+          float u[kElems];
+          unpack(u, z0, z1);
+          if (a.norm) {
+            float s = 0.0f;
+#pragma unroll
+            for (int e = 0; e < kElems; ++e) s = fmaf(u[e], u[e], s);
+            const float r = rsqrtf(row_sum<L>(s) * (1.0f / D) + a.eps);
+            const float* wr = wt[not_q];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              u[e] = u[e] * r * wr[at.v0 + e];
+              u[8 + e] = u[8 + e] * r * wr[at.v1 + e];
+            }
+          }
+          if (a.pairs > 0) turn_row(u, cs + w.t * (D / 2), a.pairs, sub, at, buf);
+          z0 = packed(u, 0);
+          z1 = packed(u, 8);
+        }
+        gbf16* o = qo + ((t0 + w.t) * hq + w.h) * D;
+        if (not_q)
+          o = pick(ko, vo, is_v) + to.x * pick(kp, vp, is_v) + to.y * pick(kt, vt, is_v) + (w.h - (is_v ? hq + hk : hq)) * pick(kh, vh, is_v);
+        store_vec(o + at.v0, z0);
+        store_vec(o + at.v1, z1);
+      }
+      advance(w);
+    }
+  }
+}
+
 // ------------------------------------------------------------------------ host
 
 int bad(const std::string& what) { return set_error(T2V_ERR_INVALID_ARG, what); }
@@ -599,6 +734,80 @@ int norm_rotary_bwd_impl(const void* q, const void* k, int64_t q_stride, int64_t
   return launched("norm weights kernel");
 }
 
+int paged_append_impl(const void* k, const void* v, int64_t k_stride, int64_t v_stride, const void* q, int64_t q_stride, int heads,
+                      const int32_t* cu_seqlens, int64_t tokens, const t2v_pages* cache, const t2v_turn* turn, void* q_out,
+                      void* stream) {
+  if (int st = check_pages(cache)) return st;
+  const t2v_pages& g = *cache;
+  if (heads < 0) return bad("heads must be >= 0");
+  if (int st = check_heads(tokens, heads, 2 * g.kv_heads, g.head_dim)) return st;
+  AppendArgs p{};
+  NormArgs& a = p.n;
+  bool interleaved = false;
+  int axes = 0;
+  std::vector<Range> in, out;
+  if (turn != nullptr) {
+    if (int st = check_turn(turn, g.head_dim, heads, g.kv_heads, &a, &interleaved, &axes, &in)) return st;
+    a.positions = turn->positions;
+  } else if (heads > 0) {
+    return bad("q is given without a norm or a turn");
+  }
+  if (int st = check_stride(k_stride, g.kv_heads, g.head_dim, "k_stride")) return st;
+  if (int st = check_stride(v_stride, g.kv_heads, g.head_dim, "v_stride")) return st;
+  if (int st = check_stride(q_stride, heads, g.head_dim, "q_stride")) return st;
+  if (tokens == 0 || g.nseq == 0) return T2V_OK;
+  a.tokens = tokens;
+  in.push_back({k, rows_bytes(tokens, k_stride, g.kv_heads, g.head_dim), "k"});
+  in.push_back({v, rows_bytes(tokens, v_stride, g.kv_heads, g.head_dim), "v"});
+  if (heads > 0) {
+    in.push_back({q, rows_bytes(tokens, q_stride, heads, g.head_dim), "q"});
+    out.push_back({q_out, 2 * tokens * heads * g.head_dim, "q_out"});
+  }
+  if (g.pages > 0 && g.k == g.v) return bad("cache.k and cache.v are the same memory");
+  // K's and V's pages may lie between each other, so each is checked against the other tensors.
+  for (int i = 0; i < 2; ++i) {
+    std::vector<Range> o = out;
+    if (g.pages > 0)
+      o.push_back({i ? g.v : g.k, i ? pages_bytes(g, g.v_strides) : pages_bytes(g, g.k_strides), i ? "cache.v" : "cache.k"});
+    if (int st = check_pointers(a, axes, in, o)) return st;
+    if (int st = check_tables_apart(g, cu_seqlens, o)) return st;
+  }
+  a.in[0] = static_cast<const bf16*>(q);
+  a.in[1] = static_cast<const bf16*>(k);
+  a.out[0] = static_cast<bf16*>(q_out);
+  a.stride[0] = q_stride;
+  a.stride[1] = k_stride;
+  a.heads[0] = heads;
+  a.heads[1] = g.kv_heads;
+  p.v = static_cast<const bf16*>(v);
+  p.v_stride = v_stride;
+  p.k_pages = static_cast<bf16*>(g.k);
+  p.v_pages = static_cast<bf16*>(g.v);
+  p.k_page = g.k_strides[0];
+  p.k_token = g.k_strides[1];
+  p.k_head = g.k_strides[2];
+  p.v_page = g.v_strides[0];
+  p.v_token = g.v_strides[1];
+  p.v_head = g.v_strides[2];
+  p.cu = cu_seqlens;
+  p.lengths = g.lengths;
+  p.table = g.table;
+  p.table_stride = g.table_stride;
+  p.nseq = g.nseq;
+  p.pages = static_cast<int>(g.pages);
+  p.shift = __builtin_ctz(g.page_size);
+  p.room = g.width * g.page_size;
+  const int per = tokens_per_block(tokens, heads + 2 * g.kv_heads, g.head_dim);
+  const int64_t blocks = (tokens + per - 1) / per;
+  if (blocks * kThreads > UINT32_MAX)
+    return bad("the call takes " + std::to_string(blocks) + " workgroups of " + std::to_string(per) + " tokens, more than one launch holds");
+  with_form(a, g.head_dim, interleaved, [&](auto d, auto il, auto lds) {
+    hipLaunchKernelGGL((paged_append_kernel<decltype(d)::value, decltype(il)::value, decltype(lds)::value>), dim3(static_cast<int>(blocks)),
+                       dim3(kThreads), 0, static_cast<hipStream_t>(stream), p, per);
+  });
+  return launched("paged append kernel");
+}
+
 }  // namespace
 }  // namespace t2v
 
@@ -618,6 +827,16 @@ extern "C" int t2v_norm_rotary_bwd(const void* q, const void* k, int64_t q_strid
   try {
     return t2v::norm_rotary_bwd_impl(q, k, q_stride, k_stride, dq_out, dk_out, dq_out_stride, dk_out_stride, tokens, heads, kv_heads,
                                      head_dim, turn, dq, dk, dq_weight, dk_weight, ws, ws_bytes, need, stream);
+  } catch (...) {
+    return t2v::set_error(T2V_ERR_OOM, "host allocation failed");
+  }
+}
+
+extern "C" int t2v_paged_append(const void* k, const void* v, int64_t k_stride, int64_t v_stride, const void* q, int64_t q_stride,
+                                int heads, const int32_t* cu_seqlens, int64_t tokens, const t2v_pages* cache, const t2v_turn* turn,
+                                void* q_out, void* stream) {
+  try {
+    return t2v::paged_append_impl(k, v, k_stride, v_stride, q, q_stride, heads, cu_seqlens, tokens, cache, turn, q_out, stream);
   } catch (...) {
     return t2v::set_error(T2V_ERR_OOM, "host allocation failed");
   }

@@ -42,6 +42,8 @@ def _checked(q, k, positions, freqs, layout, sections, mscale, q_weight, k_weigh
         if positions is not None or sections is not None:
             raise ValueError("positions or sections are given without freqs")
         args = None
+    elif positions is None:
+        raise ValueError("freqs are given without positions")
     else:
         args = _arguments(q, k, positions, freqs, layout, sections, mscale)
     return args, _weights(q_weight, k_weight, q, k, eps), eps

@@ -4,7 +4,10 @@ from __future__ import annotations
 
 import ctypes
 
+import numpy as np
+
 from . import _lib
+from .norm_rotary import _aligned_weight, _checked, _turn_struct
 
 
 class Pages:
@@ -79,3 +82,181 @@ def paged_attn_fwd(q, pages: Pages, cu_seqlens, scale: float, max_queries=None, 
     if st != _lib.T2V_OK:
         _lib._check(L, st)
     return out, lse
+
+
+def paged_append(k, v, pages: Pages, cu_seqlens, q=None, positions=None, freqs=None, layout: str = "half", sections=None,
+                 mscale: float = 1.0, q_weight=None, k_weight=None, eps=None, q_out=None, stream=None):
+    """Stores the keys and values k, v [T, Hk, D] of new tokens in their pages: of sequence s with Lq tokens (rows as in paged_attn_fwd), token i is key
+    lengths[s] - Lq + i. With freqs and positions the keys are turned before, with eps normalised (times k_weight), and so are the
+    queries q [T, H, D] of the same tokens, as by norm_rotary_apply, in the same pass; returns those (None without q). A token without a place in
+    the cache is not stored (attention over it gives NaN)."""
+    import torch
+    if k.dim() != 3 or (q is not None and q.dim() != 3):
+        raise ValueError("q and k must be [tokens, heads, head_dim]")
+    T, D = k.shape[0], pages.head_dim
+    shape = (T, pages.kv_heads, D)
+    sk, sv = _lib._check_rows(k, "k", shape), _lib._check_rows(v, "v", shape)
+    _check_cu(cu_seqlens, pages)
+    named = [("pages", pages.k), ("k", k), ("v", v), ("cu_seqlens", cu_seqlens)]
+    turn = None
+    if freqs is not None or eps is not None:
+        checked = _checked(q, k, positions, freqs, layout, sections, mscale, q_weight, k_weight, eps)
+    elif q is not None or positions is not None or sections is not None or q_weight is not None or k_weight is not None:
+        raise ValueError("q, positions, sections or weights are given without a norm (eps) or a turn (freqs)")
+    else:
+        checked = None
+    sq, heads, qp, given = 0, 0, None, ()
+    if q is not None:
+        heads = q.shape[1]
+        sq, qp = _lib._check_rows(q, "q", (T, heads, D)), q.data_ptr()
+        named.append(("q", q))
+        (q_out,), given = _lib._outputs((("q_out", q_out, (T, heads, D), torch.bfloat16),), k.device, stream)
+    elif q_out is not None:
+        raise ValueError("q_out is given without q")
+    for name, t in (("positions", positions), ("q_weight", q_weight), ("k_weight", k_weight)):
+        if t is not None:
+            named.append((name, t))
+    _lib._check_on_device((*named, *given))
+    if checked is not None:
+        with _lib._on(stream):
+            q_weight, k_weight = _aligned_weight(q_weight), _aligned_weight(k_weight)
+        turn = ctypes.byref(_turn_struct(checked, positions, q_weight, k_weight))
+    L = _lib.lib()
+    st = _lib._call_on(k.device, stream, L.t2v_paged_append, k.data_ptr(), v.data_ptr(), sk, sv, qp, sq, heads,
+                       cu_seqlens.data_ptr(), T, pages._ref, turn, None if q_out is None else q_out.data_ptr())
+    if st != _lib.T2V_OK:
+        _lib._check(L, st)
+    return q_out
+
+
+def page_copy(buffers, src, dst, stream=None):
+    """Copies pages src[i] to pages dst[i] in every one of `buffers`: a tensor [pages, ...] on the GPU or a sequence of them, of one shape and
+    strides, each page's memory dense. src, dst: host int32 arrays; no page may be written twice, nor both read and written."""
+    import torch
+    buffers = (buffers,) if isinstance(buffers, torch.Tensor) else tuple(buffers)
+    src, dst = (np.ascontiguousarray(x, dtype=np.int32) for x in (src, dst))
+    if src.ndim != 1 or src.shape != dst.shape:
+        raise ValueError("src and dst must be 1-D arrays of one length")
+    if not buffers:
+        return
+    first = buffers[0]
+    shape, strides, dtype, device = first.shape, first.stride(), first.dtype, first.device
+    if len(shape) < 2 or 0 in shape[1:]:
+        raise ValueError(f"buffers must be [pages, ...] with pages of a size, got {tuple(shape)}")
+    rows = 1
+    for size, step in sorted(zip(shape[1:], strides[1:]), key=lambda x: x[1]):
+        if size > 1 and step != rows:
+            raise ValueError(f"a page's memory must be dense, got strides {strides}")
+        rows *= size
+    item = first.element_size()
+    for b in buffers:
+        if b.shape != shape or b.stride() != strides or b.dtype != dtype or b.device != device:
+            raise ValueError("buffers must have one shape, strides, dtype and device")
+    if not first.is_cuda:
+        raise ValueError("buffers must be CUDA tensors")
+    ptrs = (ctypes.c_void_p * len(buffers))(*[b.data_ptr() for b in buffers])
+    L = _lib.lib()
+    st = _lib._call_on(device, stream, L.t2v_page_copy, ptrs, len(buffers), shape[0], (strides[0] if shape[0] > 1 else rows) * item,
+                       rows * item, src.__array_interface__["data"][0], dst.__array_interface__["data"][0], src.shape[0])
+    if st != _lib.T2V_OK:
+        _lib._check(L, st)
+
+
+class PagedCache:
+    """Keys and values of several layers and many sequences in one paged cache on the GPU. Sequences are numbers, the rows of one table that
+    all layers share; every call below takes all of them, those without new tokens with none:
+
+        cache = PagedCache(layers, pages, kv_heads, head_dim)
+        s = cache.add()
+        cache.extend([s], [prompt_tokens])            # room for its tokens, which count from here on
+        paged_append(k, v, cache.layer(0), cu_seqlens)
+        out, lse = paged_attn_fwd(q, cache.layer(0), cu_seqlens, scale)
+        t = cache.fork(s)                             # shares the pages; the one begun is copied when either goes on
+
+    cu_seqlens (cache.offsets({s: prompt_tokens})) has an entry for every sequence and one more. The bookkeeping is on the host (table:
+    PageTable); its changes and the pages' copies are enqueued on the current stream, which the calls on the cache must follow. A captured step reads
+    lengths and table on the GPU: reserve() room for its tokens, let the graph add them to ``lengths``, and tell grown() afterwards."""
+
+    def __init__(self, layers: int, pages: int, kv_heads: int, head_dim: int, page_size: int = 64, sequences: int = 64, width=None,
+                 device="cuda"):
+        import torch
+        from .page_table import PageTable
+        self.host = PageTable(pages, page_size, sequences, pages if width is None else width)
+        self.data = torch.zeros((layers, 2, pages, page_size, kv_heads, head_dim), dtype=torch.bfloat16, device=device)
+        self.table = torch.full(self.host.table.shape, -1, dtype=torch.int32, device=device)
+        self.lengths = torch.zeros(sequences, dtype=torch.int32, device=device)
+        self._layers = [Pages(x[0], x[1], self.table, self.lengths) for x in self.data]
+        self._buffers = [y for x in self.data for y in x]
+
+    def layer(self, i: int) -> Pages:
+        """Layer i's pages, for paged_append and paged_attn_fwd."""
+        return self._layers[i]
+
+    @property
+    def free_pages(self) -> int:
+        return self.host.free_pages
+
+    def offsets(self, tokens):
+        """cu_seqlens on the GPU for a call in which sequence s has tokens[s] new tokens (a dict, or one count for each sequence)."""
+        counts = np.zeros(self.host.active.size, dtype=np.int32)
+        for s, n in tokens.items() if isinstance(tokens, dict) else enumerate(tokens):
+            counts[s] = n
+        return self._to_device(np.concatenate([[0], np.cumsum(counts)]).astype(np.int32))
+
+    def _to_device(self, x, out=None):
+        import torch
+        host = torch.from_numpy(x).pin_memory()  # a new pinned tensor: its memory is not reused before the copy has run
+        return host.to(self.data.device, non_blocking=True) if out is None else out.copy_(host, non_blocking=True)
+
+    def _host(self):
+        """The bookkeeping, for a change of it."""
+        import torch
+        if self.data.is_cuda and torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("a captured graph cannot hand out or free pages: reserve() room before the capture")
+        return self.host
+
+    def _sync(self, pairs=None, lengths=True):
+        if pairs is not None and pairs[0].size:
+            page_copy(self._buffers, *pairs)
+        self._to_device(self.host.table, self.table)
+        if lengths:
+            self._to_device(self.host.lengths, self.lengths)
+
+    def add(self) -> int:
+        """A new, empty sequence's number."""
+        return self._host().add()
+
+    def extend(self, sequences, tokens) -> None:
+        """Room for so many new tokens in each of the sequences (numbers), which count in their lengths from here on. Raises RuntimeError,
+        and changes nothing, if there are not enough pages."""
+        self._sync(self._host().extend(sequences, tokens))
+
+    def reserve(self, sequences, tokens) -> None:
+        """Room for so many new tokens that a captured step will add to the lengths by itself."""
+        self._sync(self._host().reserve(sequences, tokens), lengths=False)
+
+    def grown(self, sequences, tokens) -> None:
+        """Tells of tokens that were added to the lengths on the GPU."""
+        self._host().grown(sequences, tokens)
+
+    def fork(self, sequence: int) -> int:
+        """A new sequence with the same tokens; both share the pages."""
+        s = self._host().fork(sequence)
+        self._sync()
+        return s
+
+    def free(self, sequence: int) -> None:
+        """Ends a sequence."""
+        self._host().free(sequence)
+        self._sync()
+
+    def truncate(self, sequence: int, tokens: int) -> None:
+        """Takes a sequence back to its first tokens."""
+        self._host().truncate(sequence, tokens)
+        self._sync()
+
+    def compact(self) -> int:
+        """Moves pages so that those in use are the first; returns how many moved."""
+        pairs = self._host().compact()
+        self._sync(pairs)
+        return int(pairs[0].size)
