@@ -328,8 +328,8 @@ int t2v_norm_rotary_bwd(const void* q, const void* k, int64_t q_stride, int64_t 
 typedef struct {
   void* k;                  /* device bf16 [pages, page_size, kv_heads, head_dim], 16-byte aligned */
   void* v;                  /* as k, with strides of its own */
-  int64_t k_strides[3];     /* elements between pages, between a page's tokens, between a token's heads: multiples of 8; a page's */
-  int64_t v_strides[3];     /* rows do not overlap, and pages lie one behind the other (K and V may alternate) */
+  int64_t k_strides[3];     /* elements between pages, between a page's tokens (<= 2^22), between a token's heads: multiples of 8, below */
+  int64_t v_strides[3];     /* 2^31; a page's rows do not overlap, and pages lie one behind the other (K and V may alternate) */
   int64_t pages;            /* 0 .. 2^31 - 1 */
   const int32_t* table;     /* device [nseq, width], rows table_stride entries apart */
   int64_t table_stride;
@@ -347,19 +347,16 @@ typedef struct {
  *   q            device bf16 [tokens, heads, D], read only, q_stride elements between tokens as in t2v_causal_fwd
  *   cu_seqlens   DEVICE int32 [nseq + 1], rows of q: non-decreasing from 0; rows from cu_seqlens[nseq] on are padding, whose results are
  *                left as they were
- *   max_queries  the most queries that a sequence has, or 0 if not known: it saves a launch where it shows that all have few, or that
- *                one sequence has all, and changes results by rounding only
  *   cache        HOST struct, read before the call returns
  *   out, lse     device bf16 [tokens, heads, D], contiguous, and fp32 [heads, tokens], written
- *   ws, need     as in t2v_causal_fwd; need follows from the sizes given here, not from lengths: at most 80 MiB
+ *   ws, need     as in t2v_causal_fwd; need follows from the sizes given here, not from lengths: at most 72 MiB
  * The arrays in device memory cannot be checked before the launch. Whatever they hold, nothing outside the tensors is read or written,
  * and what cannot be right shows: keys in a page outside the cache count as NaN for the queries that see them, a
  * sequence longer than its row of the table gets NaN results. Offsets that decrease give unspecified results. tokens * heads / kv_heads must stay below 2^31.
  * Deterministic, no atomics: how the work is divided follows from offsets, lengths and sizes; a
  * sequence's last bits may depend on the others in the call. T2V_SPLIT and the other settings have no effect here. */
-int t2v_paged_fwd(const void* q, int64_t q_stride, int heads, const int32_t* cu_seqlens, int64_t tokens, int max_queries,
-                  const t2v_pages* cache, float scale, void* out, float* lse, void* ws, uint64_t ws_bytes,
-                  uint64_t* need, void* stream);
+int t2v_paged_fwd(const void* q, int64_t q_stride, int heads, const int32_t* cu_seqlens, int64_t tokens, const t2v_pages* cache,
+                  float scale, void* out, float* lse, void* ws, uint64_t ws_bytes, uint64_t* need, void* stream);
 
 /* Stores the keys and values of new tokens in their pages, with the norm and the turn of t2v_norm_rotary for the keys (and, beside them, for
  * the queries of the same tokens) in the same pass. Of sequence s with Lq tokens, token i is key lengths[s] - Lq + i.

@@ -125,7 +125,7 @@ def _declare(lib, full: bool):
         lib.t2v_norm_rotary_bwd.argtypes = [_vp, _vp, i64, i64, _vp, _vp, i64, i64, i64, ctypes.c_int, ctypes.c_int,
                                             ctypes.c_int, turnp, _vp, _vp, _vp, _vp, _vp, ctypes.c_uint64, _u64p, _vp]
         lib.t2v_paged_fwd.restype = ctypes.c_int
-        lib.t2v_paged_fwd.argtypes = [_vp, i64, ctypes.c_int, _vp, i64, ctypes.c_int, ctypes.POINTER(PagesStruct), ctypes.c_float,
+        lib.t2v_paged_fwd.argtypes = [_vp, i64, ctypes.c_int, _vp, i64, ctypes.POINTER(PagesStruct), ctypes.c_float,
                                       _vp, _vp, _vp, ctypes.c_uint64, _u64p, _vp]
         lib.t2v_paged_append.restype = ctypes.c_int
         lib.t2v_paged_append.argtypes = [_vp, _vp, i64, i64, _vp, i64, ctypes.c_int, _vp, i64, ctypes.POINTER(PagesStruct), turnp,

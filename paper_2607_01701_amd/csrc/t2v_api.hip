@@ -1560,33 +1560,16 @@ int causal_bwd_impl(CausalCall& c, const void* out, const float* lse, const void
 
 // ------------------------------------------------------------------ attention over a paged cache
 
-// The kernels that a call takes, their workgroups and places in the workspace. Where rows of several sequences may be few or many, the
-// kernel of 32-row tiles takes those with few, the other one the rest. Workgroups: as many as the GPU holds at once, or as
-// the call can use at the least share that a workgroup takes.
-int paged_parts(const PagedCall& c, int max_queries, int ncu, PagedPart (&parts)[2], uint64_t* bytes) {
+// Workgroups of a call: as many as the GPU holds at once, or as the call can use at the least share that one takes, whatever the lengths.
+int paged_call_groups(const PagedCall& c) {
   const t2v_pages& g = c.cache;
-  const int64_t group = c.heads / g.kv_heads, room = static_cast<int64_t>(g.width) * g.page_size;
-  int64_t most = c.tokens;  // queries of a sequence, as far as is known
-  if (max_queries > 0) most = std::min<int64_t>(most, max_queries);
-  const bool all_few = (max_queries > 0 || c.tokens <= g.nseq ? (max_queries > 0 ? most : 1) : most) * group <= paged_tile_rows(true);
-  const bool all_many = !all_few && g.nseq == 1;
-  int n = 0;
-  if (!all_many) parts[n++] = {all_few ? kPagedAll : kPagedFew, true, 0, 0};
-  if (!all_few) parts[n++] = {all_many ? kPagedAll : kPagedMany, false, 0, 0};
-  *bytes = 0;
-  for (int i = 0; i < n; ++i) {
-    PagedPart& p = parts[i];
-    const double tiles = static_cast<double>(c.tokens * group / paged_tile_rows(p.few) + g.nseq) * g.kv_heads;
-    const double pieces = tiles * static_cast<double>((room + paged_least_share(p.few) - 1) / paged_least_share(p.few) + 1);
-    p.shares = static_cast<int>(std::min<double>(paged_workgroups(p.few, g.head_dim, ncu), std::max(1.0, pieces)));
-    if (p.shares > kNumXcd) p.shares = p.shares / kNumXcd * kNumXcd;
-    p.at = static_cast<int64_t>(*bytes);
-    *bytes += static_cast<uint64_t>(paged_part_bytes(p, g.head_dim));
-  }
-  return n;
+  const double tiles = (static_cast<double>(c.tokens) * (c.heads / g.kv_heads) / paged_few_rows() + g.nseq) * g.kv_heads;
+  const double pieces = tiles * (static_cast<double>(g.width) * g.page_size / paged_least_share() + 1.0);
+  const int n = static_cast<int>(std::min<double>(paged_groups(g.head_dim, cu_count()), std::max(2.0, pieces)));
+  return n >= 2 * kNumXcd ? n / kNumXcd * kNumXcd : n;
 }
 
-int paged_fwd_impl(PagedCall& c, int max_queries, const t2v_pages* cache, void* ws, uint64_t ws_bytes, uint64_t* need, void* stream) {
+int paged_fwd_impl(PagedCall& c, const t2v_pages* cache, void* ws, uint64_t ws_bytes, uint64_t* need, void* stream) {
   if (need != nullptr) *need = 0;
   if (int st = check_pages(cache)) return st;
   c.cache = *cache;
@@ -1596,14 +1579,13 @@ int paged_fwd_impl(PagedCall& c, int max_queries, const t2v_pages* cache, void* 
     return bad("heads (" + std::to_string(c.heads) + ") must be a multiple of kv_heads (" + std::to_string(g.kv_heads) + ")");
   if (static_cast<int64_t>(c.heads) * g.head_dim > (int64_t(1) << 22)) return bad("heads * head_dim is too large");
   if (!std::isfinite(c.scale)) return bad("scale must be finite");
-  if (max_queries < 0) return bad("max_queries must be >= 0");
   if (c.tokens < 0 || c.tokens * (c.heads / g.kv_heads) > INT32_MAX - 512) return bad("tokens times the heads of a group must be in 0 .. 2^31 - 513");
   if (c.q_stride < static_cast<int64_t>(c.heads) * g.head_dim || c.q_stride % 8 != 0 || c.q_stride > (int64_t(1) << 22))
     return bad("q_stride must be a multiple of 8 between heads * head_dim and 2^22, got " + std::to_string(c.q_stride));
   if (c.tokens == 0 || g.nseq == 0) return T2V_OK;
-  // The kernels count a call's work (at most so much) in 64 bits, a share's number times a share's length included.
+  // The kernels count a call's work in 1 / 256 of a key, exact in a double.
   const double group = c.heads / g.kv_heads, room = static_cast<double>(g.width) * g.page_size;
-  if ((c.tokens * group / paged_tile_rows(true) + g.nseq) * group * (room + 4096.0 + c.tokens) * g.kv_heads > 0x1p52)
+  if (256.0 * (c.tokens * group / paged_few_rows() + g.nseq) * (room + 4096.0 + c.tokens) * g.kv_heads > 0x1p52)
     return bad("the call's largest possible work (queries times the table's width) passes what the kernels count");
   const std::vector<Range> out = {{c.out, tensor_bytes(c.tokens, c.heads, g.head_dim), "out"}, {c.lse, c.tokens * c.heads * 4, "lse"},
                                   {ws, static_cast<int64_t>(ws_bytes), "ws"}};
@@ -1612,28 +1594,21 @@ int paged_fwd_impl(PagedCall& c, int max_queries, const t2v_pages* cache, void* 
                                   {g.v, pages_bytes(g, g.v_strides), "cache.v"}}, out))
     return st;
   if (int st = check_tables_apart(g, c.cu, out)) return st;
-  PagedPart parts[2];
-  uint64_t bytes = 0;
-  const int n = paged_parts(c, max_queries, cu_count(), parts, &bytes);
+  const int groups = paged_call_groups(c);
+  const bool only_few = c.tokens * (c.heads / g.kv_heads) <= paged_few_rows();
+  const auto bytes = static_cast<uint64_t>(paged_workspace(groups, only_few, g.head_dim));
   if (need != nullptr) *need = bytes;
   if (int st = check_workspace(ws_bytes, bytes)) return st;
   const auto s = static_cast<hipStream_t>(stream);
 #if T2V_CHECKED
   if (int st = check_arm()) return st;
 #endif
-  bool cut = false;
-  for (int i = 0; i < n; ++i) {
-    c.trace = tracer().reserve(parts[i].shares);
-    cut |= parts[i].shares > 1;
-    const bool last = i + 1 == n;
-    const hipError_t e = timer().run(kSlotFwd, s, [&] {
-      hipError_t r = launch_paged_fwd(c, parts[i], ws, s);
-      if (r == hipSuccess && last && cut) r = launch_paged_join(c, parts, n, ws, s);
-      return r;
-    });
-    if (e != hipSuccess) return hip_fail(e, "paged forward kernel launch");
-  }
-  return T2V_OK;
+  c.trace = tracer().reserve(groups);
+  const hipError_t e = timer().run(kSlotFwd, s, [&] {
+    const hipError_t r = launch_paged_fwd(c, groups, ws, s);
+    return r == hipSuccess ? launch_paged_join(c, groups, ws, s) : r;
+  });
+  return e == hipSuccess ? T2V_OK : hip_fail(e, "paged forward kernel launch");
 }
 
 // Runs f, turning host exceptions into statuses (none may cross the C ABI).
@@ -1783,12 +1758,11 @@ int t2v_causal_bwd(const void* q, const void* k, const void* v, int64_t q_stride
   });
 }
 
-int t2v_paged_fwd(const void* q, int64_t q_stride, int heads, const int32_t* cu_seqlens, int64_t tokens, int max_queries,
-                  const t2v_pages* cache, float scale, void* out, float* lse, void* ws, uint64_t ws_bytes, uint64_t* need,
-                  void* stream) {
+int t2v_paged_fwd(const void* q, int64_t q_stride, int heads, const int32_t* cu_seqlens, int64_t tokens, const t2v_pages* cache,
+                  float scale, void* out, float* lse, void* ws, uint64_t ws_bytes, uint64_t* need, void* stream) {
   return t2v::guarded([&] {
     t2v::PagedCall c{q, q_stride, heads, cu_seqlens, tokens, {}, scale, out, lse, nullptr};
-    return t2v::checked_call(stream, [&] { return t2v::paged_fwd_impl(c, max_queries, cache, ws, ws_bytes, need, stream); });
+    return t2v::checked_call(stream, [&] { return t2v::paged_fwd_impl(c, cache, ws, ws_bytes, need, stream); });
   });
 }
 

@@ -31,10 +31,15 @@ T2V_DEV float max16(const f32x16& x) {
 template <int D>
 constexpr bool kSoftmaxFirst = D == 128;
 
-// One 32-key step. MASK: this lane's row sees keys 0 .. lim of the step. c > 0.
-template <int D, bool MASK>
+struct Nothing {
+  T2V_DEV void operator()() const {}
+};
+
+// One 32-key step. MASK: this lane's row sees keys 0 .. lim of the step. c > 0. read(): called when all of the tiles' reads have been issued.
+template <int D, bool MASK, typename Read = Nothing>
 T2V_DEV void fwd_step(uint32_t kbase, uint32_t vbase0, uint32_t vbase1, int kb, int lim, float c,
-                      const bf16x8 (&qop)[D / 16], f32x16 (&o)[D / 32], float& m_run, float& l_run, int lane) {
+                      const bf16x8 (&qop)[D / 16], f32x16 (&o)[D / 32], float& m_run, float& l_run, int lane,
+                      Read&& read = Read()) {
   __builtin_amdgcn_iglp_opt(0);
   constexpr int KK = D / 16;
   constexpr int DB = D / 32;
@@ -53,6 +58,7 @@ T2V_DEV void fwd_step(uint32_t kbase, uint32_t vbase0, uint32_t vbase1, int kb, 
   for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
     for (int db = 0; db < DB; ++db) va[hf][db] = read_rows_opnd<D>(vbase0, vbase1, kb + hf * 16, db);
+  read();
   if constexpr (kSoftmaxFirst<D>) __builtin_amdgcn_s_setprio(1);
   if constexpr (MASK) {
 #pragma unroll

@@ -15,8 +15,9 @@ int check_strides(const t2v_pages& c, const int64_t (&st)[3], const char* name) 
   const int64_t page = st[0], token = st[1], head = st[2], d = c.head_dim;
   for (int64_t x : st)
     if (x < 0 || x % 8 != 0) return bad(n + "must be multiples of 8, and not negative");
-  if (token > (int64_t(1) << 22) || head > (int64_t(1) << 40) || page > (int64_t(1) << 40)) return bad(n + "are too large");
   const int64_t tokens = c.page_size, heads = c.kv_heads;
+  if (token > (int64_t(1) << 22) || head > INT32_MAX || page > INT32_MAX || (tokens - 1) * token + (heads - 1) * head > INT32_MAX)
+    return bad(n + "are too large");
   const bool token_major = (heads == 1 || head >= d) && (tokens == 1 || token >= (heads - 1) * head + d);
   const bool head_major = (tokens == 1 || token >= d) && (heads == 1 || head >= (tokens - 1) * token + d);
   if (!token_major && !head_major) return bad(n + "let rows of a page overlap");

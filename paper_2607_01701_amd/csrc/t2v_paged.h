@@ -3,11 +3,17 @@
 // Offsets, lengths and page tables are in device memory, so that a captured call follows them as they grow. A launch has a fixed number
 // of workgroups. Each works out the costs of all sequences by itself and takes an even share of their sum: positions
 // share * length .. on one line on which every tile of packed rows (query, head of the group) of every key head has an interval,
-// key head by key head, sequence by sequence. Sequence s has `rows` packed rows in tiles of `tile`; the interval of tile t is as long as
-// group * (fixed + keys before the sequence's queries) + its last row's number, which is its loop's length in keys and a fixed part, times the
-// group: an arithmetic series, so where a tile begins has a closed form. A boundary between two shares inside a tile cuts its loop at a
-// multiple of `unit` keys, not nearer than `least` to either end; both shares work out the same cut. The pieces of a cut
-// tile leave partial results, joined by a second kernel.
+// sequence by sequence, key head by key head. A position is 1 / 256 of a key. Sequence s has `rows` packed rows in tiles of `tile`; the
+// interval of tile t is as long as a fixed part, the keys before the sequence's queries, and t + 1 tiles' queries, which is (but for
+// rounding) its loop's length: an arithmetic series, so where a tile begins has a closed form. A boundary between two
+// shares inside a tile cuts its loop at a multiple of `unit` keys, not nearer than `least` to either end; both shares work out the
+// same cut. The pieces of a cut tile leave partial results, joined by a second kernel.
+//
+// Sequences with at most `few` packed rows (single tokens), whose loops wait for memory, and those with more, which keep the matrix cores busy,
+// are two lines with tiles and costs of their own. The workgroups are dealt to them by their work, alternating, so that a CU has some of both.
+//
+// Nothing here divides 64-bit numbers, which would take the GPU
+// longer than a short loop: a quotient is estimated in 32 bits and put right.
 #pragma once
 
 #include <cstdint>
@@ -20,18 +26,34 @@
 
 namespace t2v {
 
-// Which sequences a kernel takes: all, or those with at most / more than few rows.
-enum PagedClass { kPagedAll = 0, kPagedFew = 1, kPagedMany = 2 };
+// Which sequences a line takes: those with at most `few` rows, or those with more.
+enum PagedClass { kPagedFew = 0, kPagedMany = 1 };
 
 struct PagedRule {
   int group;   // query heads of a key head
   int tile;    // packed rows of a tile
-  int unit;    // keys, a multiple of 16
+  int span;    // a tile's queries, in positions, rounded up
+  int unit;    // keys, a power of two from 16 on
   int least;   // keys of the shortest piece, a multiple of unit
-  int fixed;   // a tile's cost besides its loop, in keys
+  int fixed;   // a tile's cost besides its loop, in keys, at least 1
   int share;   // keys of the shortest share, at least unit
   int cls, few;
 };
+inline PagedRule paged_rule(int group, int tile, int unit, int least, int fixed, int share, int cls, int few) {
+  return {group, tile, (tile * 256 + group - 1) / group, unit, least, fixed, share, cls, few};
+}
+
+// floor(a / b) of a >= 0 and b > 0, where it is below 2^16.
+T2V_HD int paged_ratio(int64_t a, int64_t b) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  int q = static_cast<int>(static_cast<float>(a) * __builtin_amdgcn_rcpf(static_cast<float>(b)));
+#else
+  int q = static_cast<int>(static_cast<float>(a) / static_cast<float>(b));
+#endif
+  while (q * b > a) --q;
+  while ((q + 1) * b <= a) ++q;
+  return q;
+}
 
 // A sequence as the kernels see it: rows of the packed queries and keys, whatever the device arrays hold.
 struct PagedSeq {
@@ -51,22 +73,24 @@ T2V_HD PagedSeq paged_seq(int cu0, int cu1, int length, int64_t tokens, int room
 
 struct PagedTiles {
   int rows, tiles;
-  int64_t first;  // cost of a tile before its rows: group * (fixed + keys before the queries)
+  int64_t first;  // length of a tile's interval before its queries
+  int64_t over;   // by how much the tiles' queries are more than the sequence's
 };
-// Tiles of a sequence for a kernel (none if another kernel takes it).
+// Tiles of a sequence on a line (none if it is on the other).
 T2V_HD PagedTiles paged_tiles(const PagedRule& r, const PagedSeq& s) {
   PagedTiles t;
   t.rows = s.lq * r.group;
-  const bool mine = r.cls == kPagedAll || (r.cls == kPagedFew) == (t.rows <= r.few);
-  t.tiles = mine ? (t.rows + r.tile - 1) / r.tile : 0;
+  const bool mine = (r.cls == kPagedFew) == (t.rows <= r.few);
+  t.tiles = mine ? static_cast<int>(static_cast<unsigned>(t.rows + r.tile - 1) / static_cast<unsigned>(r.tile)) : 0;
   const int before = s.lk > s.lq ? s.lk - s.lq : 0;
-  t.first = static_cast<int64_t>(r.group) * (r.fixed + before);
+  t.first = (static_cast<int64_t>(r.fixed) + before) * 256;
+  t.over = static_cast<int64_t>(t.tiles) * r.span - static_cast<int64_t>(s.lq) * 256;
   return t;
 }
-// Cost of tiles 0 .. t - 1.
+// Length of the intervals of tiles 0 .. t - 1.
 T2V_HD int64_t paged_before(const PagedRule& r, const PagedTiles& s, int t) {
-  const int64_t full = t * s.first + static_cast<int64_t>(r.tile) * t * (t + 1) / 2;
-  return t < s.tiles ? full : full - (static_cast<int64_t>(t) * r.tile - s.rows);
+  const int64_t full = t * s.first + (static_cast<int64_t>(t) * (t + 1) / 2) * r.span;
+  return t < s.tiles ? full : full - s.over;
 }
 T2V_HD int64_t paged_cost(const PagedRule& r, const PagedTiles& s) { return s.tiles == 0 ? 0 : paged_before(r, s, s.tiles); }
 // Tile that position u of the sequence's interval lies in.
@@ -85,28 +109,60 @@ T2V_HD int paged_tile_at(const PagedRule& r, const PagedTiles& s, int64_t u) {
 T2V_HD int paged_keys(const PagedRule& r, const PagedSeq& s, const PagedTiles& t, int tile) {
   const int64_t end = static_cast<int64_t>(tile + 1) * r.tile;
   const int last = static_cast<int>(end < t.rows ? end : t.rows) - 1;
-  const int64_t n = static_cast<int64_t>(s.lk) - s.lq + last / r.group + 1;
+  const int64_t n = static_cast<int64_t>(s.lk) - s.lq + static_cast<int>(static_cast<unsigned>(last) / static_cast<unsigned>(r.group)) + 1;
   return n < 0 ? 0 : n > s.lk ? s.lk : static_cast<int>(n);
 }
 // Key at which position x of a tile's interval of length cost cuts its loop over n keys.
 T2V_HD int paged_cut(const PagedRule& r, int64_t x, int64_t cost, int n) {
   if (x >= cost) return n;
-  const int64_t y = x - static_cast<int64_t>(r.group) * r.fixed;
-  const int64_t k = y < 0 ? 0 : y / (static_cast<int64_t>(r.group) * r.unit) * r.unit;
+  const int64_t y = (x >> 8) - r.fixed;
+  const int64_t k = y < 0 ? 0 : y & ~static_cast<int64_t>(r.unit - 1);
   return k < r.least ? 0 : k > n - r.least ? n : static_cast<int>(k);
 }
 // The first position that cuts at n.
 T2V_HD int64_t paged_whole(const PagedRule& r, int64_t cost, int n) {
-  int64_t m = n < r.least ? 0 : (n - r.least) / r.unit + 1;
-  if (m * r.unit < r.least) m = r.least / r.unit;
-  const int64_t x = static_cast<int64_t>(r.group) * (r.fixed + m * r.unit);
+  int64_t k = n < r.least ? 0 : ((n - r.least) & ~(r.unit - 1)) + r.unit;
+  if (k < r.least) k = r.least;
+  const int64_t x = (k + r.fixed) * 256;
   return x < cost ? x : cost;
 }
 
-// Even shares of `total`: their length, so that share i takes positions i * length .. (i + 1) * length - 1.
-T2V_HD int64_t paged_share(const PagedRule& r, int64_t total, int shares) {
-  const int64_t even = (total + shares - 1) / shares, least = static_cast<int64_t>(r.group) * r.share;
+// Even shares of `total` for n workgroups: their length, so that share i takes positions i * length .. (i + 1) * length - 1. A little
+// more than even: total / n is off by less than 1.
+T2V_HD int64_t paged_share(const PagedRule& r, int64_t total, int n) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  double inverse = __builtin_amdgcn_rcpf(static_cast<float>(n));
+#else
+  double inverse = 1.0f / static_cast<float>(n);
+#endif
+  inverse *= 2.0 - n * inverse;  // 23 bits, 46, and what a double holds
+  inverse *= 2.0 - n * inverse;
+  const int64_t even = static_cast<int64_t>(static_cast<double>(total) * inverse) + 2, least = static_cast<int64_t>(r.share) * 256;
   return even > least ? even : least;
+}
+
+// How many of `groups` workgroups take the line of many rows, `weight` being the time of a position of few rows against one of many: as their
+// share of the work, but each line that has any gets some. Dies (workgroup b runs on die b % 8) get as many each.
+T2V_HD bool paged_by_die(int groups) { return groups % 8 == 0 && groups >= 16; }
+T2V_HD int paged_many(int groups, int64_t few, int64_t many, float weight) {
+  if (many == 0 || few == 0) return few == 0 && many != 0 ? groups : 0;
+  const int each = paged_by_die(groups) ? 8 : 1, slots = groups / each;
+  const float x = static_cast<float>(many), part = x / (x + weight * static_cast<float>(few));
+  int n = static_cast<int>(part * slots + 0.5f);
+  n = n < 1 ? 1 : n > slots - 1 ? slots - 1 : n;
+  return n * each;
+}
+// Workgroup b's line and share, n_many of `groups` being the line of many rows': alternating within a die, whose shares follow each other.
+struct PagedRole {
+  bool many;
+  int share;
+};
+T2V_HD PagedRole paged_role(int b, int groups, int n_many) {
+  const bool dies = paged_by_die(groups);
+  const int x = dies ? b % 8 : 0, i = dies ? b / 8 : b, per = dies ? groups / 8 : groups, m = dies ? n_many / 8 : n_many;
+  const int before = paged_ratio(i * m, per);
+  const bool many = static_cast<int64_t>(before + 1) * per <= (i + 1) * m;
+  return {many, many ? x * m + before : x * (per - m) + i - before};
 }
 
 // A loop, or a piece of one: keys begin .. end - 1 of a tile of n keys. slot >= 0: a piece, whose partial results go there.
@@ -132,7 +188,7 @@ T2V_HD bool paged_piece(const PagedRule& r, const PagedSeq& s, const PagedTiles&
     p->slot = 2 * share;
   } else if (p->end < p->n) {
     p->slot = 2 * share + 1;
-    p->pieces = static_cast<int>((at + paged_whole(r, cost, p->n) + length - 1) / length) - share;
+    p->pieces = paged_ratio(at + paged_whole(r, cost, p->n) - 1, length) - share + 1;
   }
   return true;
 }

@@ -23,19 +23,24 @@ constexpr int kStage = 64;  // keys of an LDS stage of the kernel of 128 rows
 
 typedef __attribute__((address_space(4))) const int32_t const_i32;  // read with scalar loads
 
+// One tensor's pages: bytes between pages, tokens and heads.
+struct Rows {
+  const char* base;
+  int64_t head;
+  uint32_t page, token;
+};
 struct PagesView {
-  const bf16 *k, *v;
-  int64_t k_page, k_token, k_head, v_page, v_token, v_head;  // strides in elements
+  Rows k, v;
   const_i32* table;
   const_i32* lengths;
   int64_t table_stride;
   int pages, shift, room;
 };
 
-// The first piece of a cut tile, for the join.
+// The first piece of the tile that a workgroup cuts, for the join. Pieces 1, 2, .. are those of the line's next shares.
 struct PagedDesc {
-  int64_t q0;
-  int lq, lk, row0, head, pieces, pad;
+  int64_t q0, first, next;  // first and second piece's place in the partial results, in floats
+  int lq, lk, row0, head, pieces, rows;
 };
 
 struct PagedArgs {
@@ -44,8 +49,9 @@ struct PagedArgs {
   const_i32* cu;
   int64_t tokens;
   PagesView c;
-  PagedRule rule;
-  int nseq, heads, kv_heads, shares;
+  PagedRule few, many;
+  float weight;  // time of a position of few rows against one of many
+  int nseq, heads, kv_heads;
   float scale;  // times log2 e, positive
   unsigned qkeep, qflip;
   bf16* out;
@@ -69,14 +75,42 @@ T2V_DEV int64_t lane_of(int64_t x, int lane) {
   return static_cast<int64_t>((static_cast<uint64_t>(hi) << 32) | lo);
 }
 
+// The kernel's arguments, read again by scalar loads where they are needed: all of them kept in scalar registers would leave too few
+// to the loops.
+typedef __attribute__((address_space(4))) const void const_void;
+T2V_DEV const PagedArgs& arguments() {
+  uint64_t p = (uint64_t)(__builtin_amdgcn_kernarg_segment_ptr());
+  asm volatile("" : "+s"(p));
+  return *(const PagedArgs*)((const_void*)(p));
+}
+
 T2V_DEV PagedSeq seq_at(const PagedArgs& a, int s) {
   return paged_seq(a.cu[s], a.cu[s + 1], a.c.lengths[s], a.tokens, a.c.room);
 }
 
-// This workgroup's share of the line: positions from .. to - 1, the first of which lies in sequence `seq` of key head
-// `head`, whose interval begins at `at`.
+// Sum over a wave's lanes up to this one, by moves between neighbouring lanes and rows of 16.
+T2V_DEV int64_t wave_scan(int64_t x) {
+  auto add = [&](auto ctrl, auto rows) {
+    const uint64_t u = static_cast<uint64_t>(x);
+    const int lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(u), decltype(ctrl)::value, decltype(rows)::value, 0xF, false);
+    const int hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(u >> 32), decltype(ctrl)::value, decltype(rows)::value, 0xF, false);
+    x += static_cast<int64_t>((static_cast<uint64_t>(static_cast<uint32_t>(hi)) << 32) | static_cast<uint32_t>(lo));
+  };
+  using All = std::integral_constant<int, 0xF>;
+  add(std::integral_constant<int, 0x111>{}, All{});                                 // row_shr:1, 2, 4, 8
+  add(std::integral_constant<int, 0x112>{}, All{});
+  add(std::integral_constant<int, 0x114>{}, All{});
+  add(std::integral_constant<int, 0x118>{}, All{});
+  add(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xA>{});    // row_bcast:15 into rows 1 and 3
+  add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xC>{});    // row_bcast:31 into rows 2 and 3
+  return x;
+}
+
+// This workgroup's line and its share of it: positions from .. to - 1, the first of which lies in key head `head` of sequence
+// `seq`, whose interval begins at `at`.
 struct Walk {
-  int share, head, seq;
+  bool many;
+  int share, n_few, head, seq;
   int64_t at, from, to, length;
 };
 
@@ -84,94 +118,105 @@ struct Walk {
 T2V_DEV Walk find_share(const PagedArgs& a, int lane) {
   const int* cu = (const int*)(a.cu);
   const int* lengths = (const int*)(a.c.lengths);
-  Walk w;
-  // Workgroup b runs on die b % 8: neighbouring shares, whose tiles read the same keys, on one die.
-  const int b = blockIdx.x, n = a.shares, per_die = n / 8;
-  w.share = n % 8 == 0 ? (b % 8) * per_die + b / 8 : b;
-  auto cost_of = [&](int s) -> int64_t {
-    if (s >= a.nseq) return 0;
-    return paged_cost(a.rule, paged_tiles(a.rule, paged_seq(cu[s], cu[s + 1], lengths[s], a.tokens, a.c.room)));
-  };
-  int64_t cost = 0, before = 0, sum = 0;
-  auto scan = [&](int s0) {  // cost of sequence s0 + lane, of those before it from s0 on, and of all 64
-    cost = cost_of(s0 + lane);
-    int64_t x = cost;
+  const PagedRule rules[2] = {a.few, a.many};
+  int64_t cost[2], upto[2], sum[2] = {0, 0};  // cost: of one key head
+  auto costs = [&](int s0) {  // of sequence s0 + lane on either line, and with all key heads of those up to it from s0 on
+    const int s = s0 + lane;
+    PagedSeq seq = {0, 0, 0, false};
+    const bool real = s < a.nseq;
+    if (real) seq = paged_seq(cu[s], cu[s + 1], lengths[s], a.tokens, a.c.room);
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int64_t y = __shfl_up(static_cast<long long>(x), d);
-      x += lane >= d ? y : 0;
+    for (int i = 0; i < 2; ++i) {
+      cost[i] = real ? paged_cost(rules[i], paged_tiles(rules[i], seq)) : 0;
+      upto[i] = wave_scan(cost[i] * a.kv_heads);
     }
-    before = x - cost;
-    sum = lane_of(x, 63);
   };
-  int64_t head_cost = 0;
-  int s0 = 0;
-  for (; s0 < a.nseq; s0 += 64) {
-    scan(s0);
-    head_cost += sum;
+  for (int s0 = 0; s0 < a.nseq; s0 += 64) {
+    costs(s0);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) sum[i] += lane_of(upto[i], 63);
   }
-  const int64_t total = head_cost * a.kv_heads;
-  w.length = paged_share(a.rule, total, a.shares);
+  const int groups = gridDim.x, n_many = uniform(paged_many(groups, sum[0], sum[1], a.weight));
+  const PagedRole role = paged_role(blockIdx.x, groups, n_many);
+  const int shares = role.many ? n_many : groups - n_many;
+  const int64_t total = role.many ? sum[1] : sum[0];
+  Walk w;
+  w.many = role.many;
+  w.share = role.share;
+  w.n_few = groups - n_many;
+  w.length = paged_share(role.many ? a.many : a.few, total, shares);
   w.from = w.share * w.length;
   w.to = min(total, w.from + w.length);
   w.head = w.seq = 0;
   w.at = 0;
   if (w.from >= w.to) return w;
-  w.head = uniform(static_cast<int>(w.from / head_cost));
-  int64_t base = w.head * head_cost;
-  s0 = 0;
+  int64_t base = 0;
+  int s0 = 0;
   if (a.nseq > 64) {
     for (;; s0 += 64) {
-      scan(s0);
-      if (w.from < base + sum) break;
-      base += sum;
+      costs(s0);
+      const int64_t all = lane_of(role.many ? upto[1] : upto[0], 63);
+      if (w.from < base + all) break;
+      base += all;
     }
   }
-  const int64_t rest = w.from - base;
-  const unsigned long long hit = __ballot(rest >= before && rest < before + cost);
-  const int at = __builtin_ctzll(hit);
+  const int64_t rest = w.from - base, end = role.many ? upto[1] : upto[0], one = role.many ? cost[1] : cost[0];
+  const int64_t begin = end - one * a.kv_heads;
+  const int at = __builtin_ctzll(__ballot(rest >= begin && rest < end));
+  const int64_t first = lane_of(begin, at), head_cost = lane_of(one, at);
   w.seq = s0 + at;
-  w.at = base + lane_of(before, at);
+  w.head = uniform(paged_ratio(rest - first, head_cost));
+  w.at = base + first + w.head * head_cost;
   return w;
 }
 
-// Runs f(row of the table, sequence, its tiles, head, piece) for every piece of this workgroup's share, and leaves the share's descriptor.
-template <typename F>
-T2V_DEV void for_pieces(const PagedArgs& a, int lane, F&& f) {
-  Walk w = find_share(a, lane);
+// Partial results of a share's two slots: those of the line of few rows come first.
+template <int D>
+T2V_DEV int64_t slot_floats(const Walk& w, int rows) {
+  return (w.many ? static_cast<int64_t>(w.n_few) * 2 * kFewRows * (D + 2) : 0) + static_cast<int64_t>(w.share) * 2 * rows * (D + 2);
+}
+
+// Runs f(sequence's number, sequence, its tiles, head, piece) for every piece of this workgroup's share, and leaves its
+// descriptor.
+template <int D, typename F>
+T2V_DEV void for_pieces(Walk& w, F&& f) {
   bool begun = false;
   while (w.from < w.to) {
+    const PagedArgs& a = arguments();
+    const PagedRule rule = w.many ? a.many : a.few;
     const PagedSeq s = seq_at(a, w.seq);
-    const PagedTiles t = paged_tiles(a.rule, s);
-    const int64_t cost = paged_cost(a.rule, t);
+    const PagedTiles t = paged_tiles(rule, s);
+    const int64_t cost = paged_cost(rule, t);
     if (w.from < w.at + cost) {
-      int tile = paged_tile_at(a.rule, t, w.from - w.at);
+      int tile = paged_tile_at(rule, t, w.from - w.at);
       for (; tile < t.tiles && w.from < w.to; ++tile) {
-        const int64_t at = w.at + paged_before(a.rule, t, tile), end = min(w.to, w.at + paged_before(a.rule, t, tile + 1));
+        const int64_t at = w.at + paged_before(rule, t, tile), end = min(w.to, w.at + paged_before(rule, t, tile + 1));
         PagedPiece p;
-        if (paged_piece(a.rule, s, t, tile, at, w.from, end, w.length, w.share, &p)) {
+        if (paged_piece(rule, s, t, tile, at, w.from, end, w.length, w.share, &p)) {
           if (p.pieces > 1) {
             begun = true;
-            if (threadIdx.x == 0) a.desc[w.share] = {s.q0, s.lq, s.lk, tile * a.rule.tile, w.head, p.pieces, 0};
+            const int64_t place = slot_floats<D>(w, rule.tile), slot = static_cast<int64_t>(rule.tile) * (D + 2);
+            if (threadIdx.x == 0)
+              arguments().desc[blockIdx.x] = {s.q0, place + slot, place + 2 * slot, s.lq, s.lk, tile * rule.tile, w.head, p.pieces, rule.tile};
           }
-          f(a.c.table + w.seq * a.c.table_stride, s, t, w.head, p);
+          f(w.seq, s, t, w.head, p);
         }
         w.from = end;
       }
     }
     w.at += cost;
-    if (++w.seq == a.nseq) {
-      w.seq = 0;
-      ++w.head;
+    if (cost == 0 || ++w.head == a.kv_heads) {
+      w.head = 0;
+      ++w.seq;
     }
   }
-  if (!begun && threadIdx.x == 0) a.desc[w.share].pieces = 0;
+  if (!begun && threadIdx.x == 0) arguments().desc[blockIdx.x].pieces = 0;
 }
 
 // Row r of a tile: where it is in [T, H, D] tensors, and the last key that it sees. Rows behind the last repeat it.
 T2V_DEV LaneRow row_of(const PagedArgs& a, const PagedSeq& s, const PagedTiles& t, int head, int row) {
-  const PackedRow pr = packed_row(min(row, t.rows - 1), a.rule.group);
-  return {row < t.rows, pr.query + s.lk - s.lq, head * a.rule.group + pr.head, s.q0 + pr.query};
+  const PackedRow pr = packed_row(min(row, t.rows - 1), a.few.group);
+  return {row < t.rows, pr.query + s.lk - s.lq, head * a.few.group + pr.head, s.q0 + pr.query};
 }
 
 T2V_DEV void load_queries(const PagedArgs& a, const bf16* p, bool ok, int G, bf16x8* qop, int n) {
@@ -184,81 +229,120 @@ T2V_DEV void load_queries(const PagedArgs& a, const bf16* p, bool ok, int G, bf1
   }
 }
 
-// Sixteen keys from key `key` on, a multiple of 16: their page's number.
-struct Block16 {
-  int key, last;  // the first key that is read, and how many rows follow it (15: all)
-};
-T2V_DEV Block16 block16(int key, int lk) {
-  const int k = min(key, lk - 1);
-  return {k, key < lk ? min(lk - 1 - key, 15) : 0};
-}
-T2V_DEV int page_of(const PagesView& c, const_i32* row, int key, int lk) { return row[block16(key, lk).key >> c.shift]; }
-
-// Address of the block's first key and head (uniform); last: the rows that may be read behind it.
-T2V_DEV const char* block_address(const PagesView& c, const bf16* base, int64_t page, int64_t token, int64_t head_offset, int id,
-                                  const Block16& b, int* last) {
-  const bool ok = static_cast<unsigned>(id) < static_cast<unsigned>(c.pages);
-  *last = ok ? b.last : 0;
-  const int64_t e = id * page + (b.key & ((1 << c.shift) - 1)) * token + head_offset;
-  return ok ? reinterpret_cast<const char*>(base + e) : reinterpret_cast<const char*>(nan_row);
-}
-
-// One tensor's pages, seen by one head.
+// What the loops read of a sequence's pages, for one key head. BIG: pages of 64 keys or more, so that all keys of a
+// step or a stage lie in one; else 16 neighbouring keys do.
 struct HeadPages {
-  const bf16* base;
-  int64_t page, token, head_offset;
+  const_i32* table;
+  const char *k, *v;
+  uint32_t k_page, k_token, v_page, v_token;
+  int pages, shift, lk;
 };
+T2V_DEV HeadPages head_pages(const PagedArgs& a, int seq, int head, int lk) {
+  const PagesView& c = a.c;
+  return {c.table + seq * c.table_stride, c.k.base + head * c.k.head, c.v.base + head * c.v.head, c.k.page, c.k.token, c.v.page,
+          c.v.token, c.pages, c.shift, lk};
+}
+
+// Number of the page that holds key `key` (or the last key, if that comes first).
+T2V_DEV int page_of(const HeadPages& c, int key) { return c.table[min(key, c.lk - 1) >> c.shift]; }
+
+// Where the keys from `key` on lie: addresses of its K and V (uniform), and how many rows behind it may be read. A page outside the cache
+// is the row of NaN, for the key and all behind it.
+struct Block {
+  const char *k, *v;
+  int last;
+};
+T2V_DEV Block block_at(const HeadPages& c, int id, int key) {
+  const int first = min(key, c.lk - 1);
+  const bool ok = static_cast<unsigned>(id) < static_cast<unsigned>(c.pages);
+  const uint32_t row = first & ((1 << c.shift) - 1);
+  const uint64_t page = static_cast<uint32_t>(id);
+  const char* nan = reinterpret_cast<const char*>(nan_row);
+  return {ok ? c.k + (page * c.k_page + row * c.k_token) : nan, ok ? c.v + (page * c.v_page + row * c.v_token) : nan,
+          ok && key < c.lk ? c.lk - 1 - key : 0};
+}
+
+#if T2V_CHECKED
+// Whether row r behind key `key` may be read; a row that may not is replaced by NaN.
+T2V_DEV bool check_key(const HeadPages& c, int key, int r) { return check_row(min(key, c.lk - 1) + r, c.lk); }
+#endif
 
 // ------------------------------------------------------------------ few rows: single tokens
 
-// Copy of 32 keys by one wave into a swizzled tile; instruction j covers RPI rows of one block of 16.
-template <int D>
+// As dma_lds16_s, for bytes that nothing reads again: they need not stay in the caches, which serve 6.6 TB/s of them in place of 6.0.
+T2V_DEV void dma_lds16_once(const void* sbase, uint32_t voff, uint32_t lds) {
+  asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(voff), "s"(uniform_ptr(sbase)), "{m0}"(lds) : "memory");
+}
+
+// Copy of 32 keys by one wave into swizzled tiles of K and V; instruction j covers RPI rows. Its swizzle differs from instruction
+// 0's by a constant.
+template <int D, bool BIG>
 struct StepDma {
   static constexpr int CPR = D / 8, RPI = 64 / CPR, NJ = 32 / RPI;
+  static constexpr int NB = BIG ? 1 : 2, PER = NJ / NB;  // blocks of keys that lie together, and their instructions
   int r0;
   uint32_t chunk0;
   T2V_DEV explicit StepDma(int lane) : r0(lane / CPR), chunk0(static_cast<uint32_t>((lane % CPR) ^ swz<D>(lane / CPR))) {}
-  T2V_DEV void copy(uint32_t lds, const PagesView& c, const HeadPages& p, const int (&ids)[2], int key0, int lk) const {
-    const uint32_t ts = static_cast<uint32_t>(p.token * 2);
+  T2V_DEV uint32_t col(int j) const { return (chunk0 ^ static_cast<uint32_t>(swz<D>(RPI * j))) * 16; }
+  T2V_DEV void find(int (&ids)[NB], const HeadPages& c, int key0) const {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const Block16 b = block16(key0 + 16 * h, lk);
-      int last;
-      const char* base = block_address(c, p.base, p.page, p.token, p.head_offset, ids[h], b, &last);
+    for (int h = 0; h < NB; ++h) ids[h] = page_of(c, key0 + 16 * h);
+  }
+  T2V_DEV void copy(uint32_t k_tile, uint32_t v_tile, const HeadPages& c, const int (&ids)[NB], int key0) const {
+    Block b[NB];
 #pragma unroll
-      for (int i = 0; i < NJ / 2; ++i) {
-        const int j = h * (NJ / 2) + i;
-        const uint32_t col = (chunk0 ^ static_cast<uint32_t>(swz<D>(RPI * j))) * 16;
-        const int r = min(r0 + RPI * i, last);
+    for (int h = 0; h < NB; ++h) b[h] = block_at(c, ids[h], key0 + 16 * h);
+    bool whole = !T2V_CHECKED;
+#pragma unroll
+    for (int h = 0; h < NB; ++h) whole = whole && b[h].last >= RPI * PER - 1;
+    if (whole) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const uint32_t token = t ? c.v_token : c.k_token, tile = t ? v_tile : k_tile, row = static_cast<uint32_t>(r0) * token;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+          dma_lds16_once((t ? b[j / PER].v : b[j / PER].k) + static_cast<uint64_t>(RPI * (j % PER)) * token, row + col(j), tile + j * 1024);
+      }
+      return;
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const uint32_t token = t ? c.v_token : c.k_token, tile = t ? v_tile : k_tile;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const Block& at = b[j / PER];
+        const int r = min(r0 + RPI * (j % PER), at.last);
 #if T2V_CHECKED
-        if (!check_row(b.key + r, lk)) {
-          dma_lds16_s(nan_row, col, lds + j * 1024);
+        if (!check_key(c, key0 + 16 * (j / PER), r)) {
+          dma_lds16_once(nan_row, col(j), tile + j * 1024);
           continue;
         }
 #endif
-        dma_lds16_s(base, static_cast<uint32_t>(r) * ts + col, lds + j * 1024);
+        dma_lds16_once(t ? at.v : at.k, static_cast<uint32_t>(r) * token + col(j), tile + j * 1024);
       }
     }
   }
 };
 
-template <int D>
-__global__ __launch_bounds__(256, D == 64 ? 2 : 1) void paged_few_kernel(const PagedArgs a) {
+// A tile of at most 32 packed rows, which the workgroup's four waves all hold: they take every fourth 32-key step, each through an LDS
+// buffer of its own, which is filled again as soon as its step's operands are in registers; so nothing but its own copies holds a wave
+// up. The waves' sums meet in LDS at the end.
+template <int D, bool BIG>
+T2V_DEV void few_pieces(Walk& w, bf16* lds, float (&sM)[4][kFewRows], float (&sL)[4][kFewRows]) {
+  using Dma = StepDma<D, BIG>;
   constexpr int KK = D / 16, DB = D / 32, R = kFewRows;
-  constexpr int kTile = 32 * D;             // elements of a step's K or V
-  constexpr int kOps = 2 * StepDma<D>::NJ;  // copies of a step
-  __shared__ __attribute__((aligned(1024))) bf16 sKV[4][2][2][kTile];  // [wave][buffer][K, V]
-  __shared__ float sM[4][R], sL[4][R];
-  const unsigned long long trace_t0 = a.trace != nullptr ? trace_clock() : 0ull;
+  constexpr int kTile = 32 * D;  // elements of a step's K or V
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int wave = uniform(tid >> 6);
   const int G = lane >> 5, l32 = lane & 31;
-  const StepDma<D> dma(lane);
-  const uint32_t buf = lds_addr(sKV[wave]);
-  const uint32_t ko = opnd_lane_off<D>(lane);
-  const uint32_t vo0 = rows_lane_off<D>(lane, 0), vo1 = rows_lane_off<D>(lane, 1);
-  for_pieces(a, lane, [&](const_i32* table, const PagedSeq& s, const PagedTiles& t, int head, const PagedPiece& p) {
+  bf16* const buf = lds + wave * (2 * kTile);
+  const Dma dma(lane);
+  const uint32_t k_tile = lds_addr(buf), v_tile = k_tile + 2 * kTile;
+  const uint32_t ko = k_tile + opnd_lane_off<D>(lane);
+  const uint32_t vo0 = v_tile + rows_lane_off<D>(lane, 0), vo1 = v_tile + rows_lane_off<D>(lane, 1);
+  for_pieces<D>(w, [&](int seq, const PagedSeq& s, const PagedTiles& t, int head, const PagedPiece& p) {
+    const PagedArgs& a = arguments();
     const int row0 = p.tile * R;
     const LaneRow me = row_of(a, s, t, head, row0 + l32);
     const int lim_lo = __builtin_amdgcn_readlane(me.lim, 0);
@@ -268,49 +352,44 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void paged_few_kernel(const P
     float m_run = -kInf, l_run = 0.0f;
     const int nsteps = (p.end - p.begin + 31) / 32;
     if (wave < nsteps) {
-      const HeadPages kp{a.c.k, a.c.k_page, a.c.k_token, head * a.c.k_head};
-      const HeadPages vp{a.c.v, a.c.v_page, a.c.v_token, head * a.c.v_head};
-      int ids[2];
-      auto find = [&](int n) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) ids[h] = page_of(a.c, table, p.begin + n * 32 + 16 * h, s.lk);
+      const HeadPages pages = head_pages(a, seq, head, s.lk);
+      const float scale = a.scale;
+      int ids[Dma::NB];
+      auto fetch = [&](int n) {
+        dma.copy(k_tile, v_tile, pages, ids, p.begin + n * 32);
+        if (n + 4 < nsteps) dma.find(ids, pages, p.begin + (n + 4) * 32);
       };
-      auto fetch = [&](int n, uint32_t b) {
-        dma.copy(buf + b * (4 * kTile), a.c, kp, ids, p.begin + n * 32, s.lk);
-        dma.copy(buf + b * (4 * kTile) + 2 * kTile, a.c, vp, ids, p.begin + n * 32, s.lk);
-      };
-      find(wave);
-      fetch(wave, 0);
-      if (wave + 4 < nsteps) find(wave + 4);
+      dma.find(ids, pages, p.begin + wave * 32);
+      fetch(wave);
       bf16x8 qop[KK];
       load_queries(a, a.q + me.token * a.q_stride + static_cast<int64_t>(me.head) * D, me.ok, G, qop, KK);
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) pin(qop[kk]);  // the loads end here, not between counted copies
-      uint32_t b = 0;
-      for (int n = wave; n < nsteps; n += 4, b ^= 1) {
-        // This wave's reads of the buffer that is filled next have returned: their results are used.
-        if (n + 4 < nsteps) {
-          fetch(n + 4, b ^ 1);
-          if (n + 8 < nsteps) find(n + 8);
-          wait_vmcnt<kOps>();
-        } else {
-          wait_vmcnt0();
-        }
+      // Steps that all rows see whole, then the others.
+      int n = wave;
+      auto arrived = [&] {
+        wait_vmcnt0();
         asm volatile("" ::: "memory");
-        const uint32_t tile = buf + b * (4 * kTile);
-        const uint32_t vb = tile + 2 * kTile;
-        const int key0 = p.begin + n * 32;
-        if (key0 + 31 <= lim_lo)
-          fwd_step<D, false>(tile + ko, vb + vo0, vb + vo1, 0, 0, a.scale, qop, o, m_run, l_run, lane);
-        else
-          fwd_step<D, true>(tile + ko, vb + vo0, vb + vo1, 0, me.lim - key0, a.scale, qop, o, m_run, l_run, lane);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // before the next copy over what this step read
+      };
+      auto next = [&] {
+        if (n + 4 < nsteps) {
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this step's operands have left the buffer
+          fetch(n + 4);
+        }
+      };
+      for (; n < nsteps && p.begin + n * 32 + 31 <= lim_lo; n += 4) {
+        arrived();
+        fwd_step<D, false>(ko, vo0, vo1, 0, 0, scale, qop, o, m_run, l_run, lane, next);
+      }
+#pragma unroll 1
+      for (; n < nsteps; n += 4) {
+        arrived();
+        fwd_step<D, true>(ko, vo0, vo1, 0, me.lim - (p.begin + n * 32), scale, qop, o, m_run, l_run, lane);
+        next();  // not before: the step may read its values again
       }
     }
 
     // The waves' sums, unnormalised and each with its own reference, in fp32: wave w's in its buffers.
     const float lt = half_sum(l_run);
-    float* mine = reinterpret_cast<float*>(sKV[wave]);
+    float* mine = reinterpret_cast<float*>(buf);
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -332,21 +411,21 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void paged_few_kernel(const P
     if (row.ok) {
       float m = sM[0][r];
 #pragma unroll
-      for (int w = 1; w < 4; ++w) m = max_nan(m, sM[w][r]);
+      for (int i = 1; i < 4; ++i) m = max_nan(m, sM[i][r]);
       const float ref = m == -kInf ? 0.0f : m;
       float l = 0.0f, x[C];
 #pragma unroll
       for (int e = 0; e < C; ++e) x[e] = 0.0f;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const float f = __builtin_amdgcn_exp2f(sM[w][r] - ref);
-        l = fmaf(f, sL[w][r], l);
-        const float* src = reinterpret_cast<const float*>(sKV[w]) + r * D + col;
+      for (int i = 0; i < 4; ++i) {
+        const float f = __builtin_amdgcn_exp2f(sM[i][r] - ref);
+        l = fmaf(f, sL[i][r], l);
+        const float* src = reinterpret_cast<const float*>(lds + i * (2 * kTile)) + r * D + col;
 #pragma unroll
         for (int e = 0; e < C; ++e) x[e] = fmaf(f, src[e], x[e]);
       }
       if (p.slot >= 0) {
-        float* po = a.partial + static_cast<int64_t>(p.slot) * (R * (D + 2));
+        float* po = a.partial + slot_floats<D>(w, R) + (p.slot & 1) * (R * (D + 2));
 #pragma unroll
         for (int e = 0; e < C; e += 4) *reinterpret_cast<f32x4*>(po + r * D + col + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
         if (col == 0) {
@@ -358,10 +437,10 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void paged_few_kernel(const P
         bf16* op = a.out + (row.token * a.heads + row.head) * D + col;
 #pragma unroll
         for (int e = 0; e < C; e += 8) {
-          bf16x8 w;
+          bf16x8 y;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) w[i] = static_cast<bf16>(x[e + i] * inv);
-          *reinterpret_cast<bf16x8*>(op + e) = w;
+          for (int i = 0; i < 8; ++i) y[i] = static_cast<bf16>(x[e + i] * inv);
+          *reinterpret_cast<bf16x8*>(op + e) = y;
         }
         if (col == 0)
           a.lse[static_cast<int64_t>(row.head) * a.tokens + row.token] = s.bad ? kNan : (m + __builtin_amdgcn_logf(l)) * kLn2;
@@ -369,60 +448,80 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void paged_few_kernel(const P
     }
     __syncthreads();  // before the next piece's copies over the sums
   });
-  if (a.trace != nullptr) trace_end(a.trace, trace_t0, 0, blockIdx.x);
 }
 
 // ------------------------------------------------------------------ many rows: chunks and prompts
 
-// Copy of a stage of 64 keys by a workgroup into a swizzled tile: wave w's instruction j covers RPI rows from row RPI (w + NW j) on,
+// Copy of a stage of 64 keys by a workgroup into swizzled tiles of K and V: wave w's instruction j covers RPI rows from row RPI (w + NW j) on,
 // which lie in one block of 16.
-template <int D, int NT>
+template <int D, int NT, bool BIG>
 struct StageDma {
   static constexpr int CPR = D / 8, RPI = 64 / CPR, NW = NT / 64, NJ = kStage / RPI / NW;
+  static constexpr int NB = BIG ? 1 : NJ;
   static_assert((RPI * NW) % 16 == 0, "a lane's swizzled chunk must not depend on the instruction");
-  int wave, r;  // r: this lane's row of its block
+  int wave, r;  // r: this lane's row of its block of 16, or (BIG) of the stage in instruction 0
   uint32_t col;
   T2V_DEV explicit StageDma(int tid) {
     wave = uniform(tid >> 6);
     const int row = RPI * wave + (tid & 63) / CPR;
-    r = row & 15;
+    r = BIG ? row : row & 15;
     col = static_cast<uint32_t>((((tid & 63) % CPR) ^ swz<D>(row)) * 16);
   }
-  T2V_DEV int block(int j) const { return (RPI * (wave + NW * j)) & ~15; }  // its first key
-  T2V_DEV void find(int (&ids)[NJ], const PagesView& c, const_i32* table, int key0, int lk) const {
+  // First key of what lies together in instruction j.
+  T2V_DEV int block(int j) const { return BIG ? 0 : (RPI * (wave + NW * j)) & ~15; }
+  T2V_DEV void find(int (&ids)[NB], const HeadPages& c, int key0) const {
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) ids[j] = page_of(c, table, key0 + block(j), lk);
+    for (int j = 0; j < NB; ++j) ids[j] = page_of(c, key0 + block(j));
   }
-  T2V_DEV void copy(bf16* tile, const PagesView& c, const HeadPages& p, const int (&ids)[NJ], int key0, int lk) const {
-    const uint32_t ts = static_cast<uint32_t>(p.token * 2);
+  T2V_DEV void copy(bf16* k_tile, bf16* v_tile, const HeadPages& c, const int (&ids)[NB], int key0) const {
+    Block b[NB];
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const Block16 b = block16(key0 + block(j), lk);
-      int last;
-      const char* base = block_address(c, p.base, p.page, p.token, p.head_offset, ids[j], b, &last);
-      const uint32_t lds = lds_addr(tile) + (wave + NW * j) * 1024;
-      const int row = min(r, last);
-#if T2V_CHECKED
-      if (!check_row(b.key + row, lk)) {
-        dma_lds16_s(nan_row, col, lds);
-        continue;
+    for (int j = 0; j < NB; ++j) b[j] = block_at(c, ids[j], key0 + block(j));
+    bool whole = !T2V_CHECKED;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) whole = whole && b[j].last >= (BIG ? kStage : 16) - 1;
+    if (whole) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const uint32_t token = t ? c.v_token : c.k_token, lds = lds_addr(t ? v_tile : k_tile) + wave * 1024;
+        const uint32_t off = static_cast<uint32_t>(r) * token + col;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+          dma_lds16_s((t ? b[BIG ? 0 : j].v : b[BIG ? 0 : j].k) + static_cast<uint64_t>(BIG ? RPI * NW * j : 0) * token, off,
+                      lds + j * NW * 1024);
       }
+      return;
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const uint32_t token = t ? c.v_token : c.k_token, lds = lds_addr(t ? v_tile : k_tile) + wave * 1024;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const Block& at = b[BIG ? 0 : j];
+        const int row = min(r + (BIG ? RPI * NW * j : 0), at.last);
+#if T2V_CHECKED
+        if (!check_key(c, key0 + block(j), row)) {
+          dma_lds16_s(nan_row, col, lds + j * NW * 1024);
+          continue;
+        }
 #endif
-      dma_lds16_s(base, static_cast<uint32_t>(row) * ts + col, lds);
+        dma_lds16_s(t ? at.v : at.k, static_cast<uint32_t>(row) * token + col, lds + j * NW * 1024);
+      }
     }
   }
 };
 
-template <int D>
-__global__ __launch_bounds__(256, 2) void paged_many_kernel(const PagedArgs a) {
+// A tile of 128 packed rows, 32 to a wave; the workgroup stages 64 keys at a time for all of them, the next ones under the
+// products of these.
+template <int D, bool BIG>
+T2V_DEV void many_pieces(Walk& w, bf16* lds) {
   constexpr int KK = D / 16, DB = D / 32, NT = 256, R = kManyRows;
-  using Dma = StageDma<D, NT>;
-  __shared__ __attribute__((aligned(1024))) bf16 sK[2][kStage * D];
-  __shared__ __attribute__((aligned(1024))) bf16 sV[2][kStage * D];
-  const unsigned long long trace_t0 = a.trace != nullptr ? trace_clock() : 0ull;
+  using Dma = StageDma<D, NT, BIG>;
+  auto sK = [&](int b) { return lds + b * (kStage * D); };
+  auto sV = [&](int b) { return lds + (2 + b) * (kStage * D); };
   const int tid = threadIdx.x;
   const int wave = uniform(tid >> 6);
-  for_pieces(a, tid & 63, [&](const_i32* table, const PagedSeq& s, const PagedTiles& t, int head, const PagedPiece& p) {
+  for_pieces<D>(w, [&](int seq, const PagedSeq& s, const PagedTiles& t, int head, const PagedPiece& p) {
     const int lane = lane_again(), G = lane >> 5, l32 = lane & 31;
     const int row0 = p.tile * R + wave * 32;
     const bool wave_active = row0 < t.rows;
@@ -432,16 +531,16 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(const PagedArgs a) {
     float m_run = -kInf, l_run = 0.0f;
     const int ntiles = (p.end - p.begin + kStage - 1) / kStage;
     if (ntiles > 0) {
+      const PagedArgs& a = arguments();
       const LaneRow me = row_of(a, s, t, head, row0 + l32);
       const int lim = me.lim, lim_lo = __builtin_amdgcn_readlane(lim, 0), lim_hi = __builtin_amdgcn_readlane(lim, 31);
-      const HeadPages kp{a.c.k, a.c.k_page, a.c.k_token, head * a.c.k_head};
-      const HeadPages vp{a.c.v, a.c.v_page, a.c.v_token, head * a.c.v_head};
+      const HeadPages pages = head_pages(a, seq, head, s.lk);
+      const float scale = a.scale;
       const Dma dma(tid);
-      int ids[Dma::NJ];
-      dma.find(ids, a.c, table, p.begin, s.lk);
-      dma.copy(sK[0], a.c, kp, ids, p.begin, s.lk);
-      dma.copy(sV[0], a.c, vp, ids, p.begin, s.lk);
-      if (ntiles > 1) dma.find(ids, a.c, table, p.begin + kStage, s.lk);
+      int ids[Dma::NB];
+      dma.find(ids, pages, p.begin);
+      dma.copy(sK(0), sV(0), pages, ids, p.begin);
+      if (ntiles > 1) dma.find(ids, pages, p.begin + kStage);
       bf16x8 qop[KK];
       load_queries(a, a.q + me.token * a.q_stride + static_cast<int64_t>(me.head) * D, me.ok, G, qop, KK);
       const uint32_t ko = opnd_lane_off<D>(lane);
@@ -451,9 +550,8 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(const PagedArgs a) {
       auto prefetch = [&](int tt) {
         if (tt + 1 < ntiles) {
           const int key0 = p.begin + (tt + 1) * kStage;
-          dma.copy(sK[(tt & 1) ^ 1], a.c, kp, ids, key0, s.lk);
-          dma.copy(sV[(tt & 1) ^ 1], a.c, vp, ids, key0, s.lk);
-          if (tt + 2 < ntiles) dma.find(ids, a.c, table, key0 + kStage, s.lk);
+          dma.copy(sK((tt & 1) ^ 1), sV((tt & 1) ^ 1), pages, ids, key0);
+          if (tt + 2 < ntiles) dma.find(ids, pages, key0 + kStage);
         }
       };
       // Stages that all rows of this wave see whole, then the others: every wave passes ntiles barriers.
@@ -462,8 +560,8 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(const PagedArgs a) {
       for (; tt < nfull; ++tt) {
         const int b = tt & 1;
         prefetch(tt);
-        const uint32_t kbase = lds_addr(sK[b]) + ko;
-        const uint32_t vb0 = lds_addr(sV[b]) + vo0, vb1 = lds_addr(sV[b]) + vo1;
+        const uint32_t kbase = lds_addr(sK(b)) + ko;
+        const uint32_t vb0 = lds_addr(sV(b)) + vo0, vb1 = lds_addr(sV(b)) + vo1;
 #pragma unroll
         for (int kb = 0; kb < kStage; kb += 32)
           fwd_step<D, false>(kbase, vb0, vb1, kb, 0, a.scale, qop, o, m_run, l_run, lane);
@@ -475,11 +573,11 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(const PagedArgs a) {
         const int key0 = p.begin + tt * kStage;
         prefetch(tt);
         if (wave_active) {
-          const uint32_t kbase = lds_addr(sK[b]) + ko;
-          const uint32_t vb0 = lds_addr(sV[b]) + vo0, vb1 = lds_addr(sV[b]) + vo1;
+          const uint32_t kbase = lds_addr(sK(b)) + ko;
+          const uint32_t vb0 = lds_addr(sV(b)) + vo0, vb1 = lds_addr(sV(b)) + vo1;
 #pragma unroll 1
           for (int kb = 0; kb < kStage && key0 + kb <= lim_hi; kb += 32)
-            fwd_step<D, true>(kbase, vb0, vb1, kb, lim - key0 - kb, a.scale, qop, o, m_run, l_run, lane);
+            fwd_step<D, true>(kbase, vb0, vb1, kb, lim - key0 - kb, scale, qop, o, m_run, l_run, lane);
         }
         wait_vmcnt0();
         __syncthreads();
@@ -487,11 +585,12 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(const PagedArgs a) {
     }
     if (wave_active) {
       // Worked out again, rather than kept in registers through the loop.
+      const PagedArgs& a = arguments();
       const int lane = lane_again(), G = lane >> 5, l32 = lane & 31;
       const LaneRow me = row_of(a, s, t, head, row0 + l32);
       const float lt = half_sum(l_run);
       if (p.slot >= 0) {  // one piece: unnormalised sums, reference and sum of each row
-        float* po = a.partial + static_cast<int64_t>(p.slot) * (R * (D + 2));
+        float* po = a.partial + slot_floats<D>(w, R) + (p.slot & 1) * (R * (D + 2));
         float* pm = po + R * D;
         const int r = wave * 32 + l32;
         if (me.ok) {
@@ -520,172 +619,156 @@ __global__ __launch_bounds__(256, 2) void paged_many_kernel(const PagedArgs a) {
       }
     }
   });
-  if (a.trace != nullptr) trace_end(a.trace, trace_t0, 0, blockIdx.x);
+}
+
+template <int D, bool BIG>
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void paged_fwd_kernel(const PagedArgs) {
+  __shared__ __attribute__((aligned(1024))) bf16 lds[4 * kStage * D];  // two stages of K and V, or a step of them for each wave
+  __shared__ float sM[4][kFewRows], sL[4][kFewRows];
+  const unsigned long long trace_t0 = arguments().trace != nullptr ? trace_clock() : 0ull;
+  Walk w = find_share(arguments(), threadIdx.x & 63);
+  if (w.many)
+    many_pieces<D, BIG>(w, lds);
+  else
+    few_pieces<D, BIG>(w, lds, sM, sL);
+  if (arguments().trace != nullptr) trace_end(arguments().trace, trace_t0, 0, blockIdx.x);
 }
 
 // ------------------------------------------------------------------ join
 
-// What the join needs of one kernel's part.
-struct JoinPart {
+// Workgroups of a cut tile. Most tiles of few rows leave all but one idle, and the launch of 512 x 8 of them takes 1 us more than of 512 x 4;
+// with two, large tiles take 6 us longer.
+constexpr int kJoinBlocks = 4;
+
+struct JoinArgs {
   const float* partial;
   const PagedDesc* desc;
-  int rows, blocks, first;  // rows of a tile; workgroups of a share; this part's first workgroup
-};
-struct JoinArgs {
-  JoinPart part[2];
-  int parts, heads, group;
+  int blocks, heads, group;  // workgroups of a descriptor
   int64_t tokens;
   bf16* out;
   float* lse;
 };
 
-// Joins the pieces of the tile that a share begins: with the largest reference m of a row, out = sum_p 2^(m_p - m) O_p / l,
+// Joins the pieces of the tile that a workgroup begins: with the largest reference m of a row, out = sum_p 2^(m_p - m) O_p / l,
 // l = sum_p 2^(m_p - m) l_p, in piece order. D / 8 lanes hold a row, eight columns each.
 template <int D>
 __global__ __launch_bounds__(kThreads) void paged_join_kernel(const JoinArgs a) {
   constexpr int LPR = D / 8, RPB = kThreads / LPR;
-  const bool second = a.parts > 1 && static_cast<int>(blockIdx.x) >= a.part[1].first;
-  const JoinPart p = second ? a.part[1] : a.part[0];
-  const int b = blockIdx.x - p.first, share = b / p.blocks;
-  const PagedDesc it = p.desc[share];
+  const PagedDesc it = a.desc[blockIdx.x / a.blocks];
   if (it.pieces == 0) return;
-  const int r = (b % p.blocks) * RPB + threadIdx.x / LPR;  // row of the tile
   const int sub = threadIdx.x % LPR, col = sub * 8;
-  const int row = it.row0 + r;
-  if (row >= it.lq * a.group) return;  // all lanes of a row alike
-  const PackedRow pr = packed_row(row, a.group);
-  const int64_t slot = static_cast<int64_t>(p.rows) * (D + 2);
-  auto piece = [&](int i) { return p.partial + (i == 0 ? 2 * share + 1 : 2 * (share + i)) * slot; };
-  const int mo = p.rows * D + 2 * r, xo = r * D + col;
-  float m = -kInf;
-  for (int i = sub; i < it.pieces; i += LPR) m = max_nan(m, piece(i)[mo]);
+  for (int r = (blockIdx.x % a.blocks) * RPB + threadIdx.x / LPR; r < it.rows; r += a.blocks * RPB) {  // row of the tile
+    const int row = it.row0 + r;
+    if (row >= it.lq * a.group) break;  // all lanes of a row alike
+    const PackedRow pr = packed_row(row, a.group);
+    const int64_t share = static_cast<int64_t>(it.rows) * 2 * (D + 2);
+    auto piece = [&](int i) { return a.partial + (i == 0 ? it.first : it.next + (i - 1) * share); };
+    const int mo = it.rows * D + 2 * r, xo = r * D + col;
+    float m = -kInf;
+    for (int i = sub; i < it.pieces; i += LPR) m = max_nan(m, piece(i)[mo]);
 #pragma unroll
-  for (int off = LPR / 2; off > 0; off >>= 1) m = max_nan(m, __shfl_xor(m, off, LPR));
-  const float ref = m == -kInf ? 0.0f : m;
-  float l = 0.0f;
-  f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f}, y = x;
-  for (int i0 = 0; i0 < it.pieces; i0 += LPR) {
-    const int mine = i0 + sub;
-    const bool has = mine < it.pieces;
-    const float w_mine = has ? __builtin_amdgcn_exp2f(piece(mine)[mo] - ref) : 0.0f;
-    const float l_mine = has ? piece(mine)[mo + 1] : 0.0f;
-    const int n = min(LPR, it.pieces - i0);
-    for (int i = 0; i < n; ++i) {
-      const float w = __shfl(w_mine, i, LPR);
-      l = fmaf(w, __shfl(l_mine, i, LPR), l);
-      const float* src = piece(i0 + i) + xo;
-      const f32x4 u = *reinterpret_cast<const f32x4*>(src);
-      const f32x4 v = *reinterpret_cast<const f32x4*>(src + 4);
+    for (int off = LPR / 2; off > 0; off >>= 1) m = max_nan(m, __shfl_xor(m, off, LPR));
+    const float ref = m == -kInf ? 0.0f : m;
+    float l = 0.0f;
+    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f}, y = x;
+    for (int i0 = 0; i0 < it.pieces; i0 += LPR) {
+      const int mine = i0 + sub;
+      const bool has = mine < it.pieces;
+      const float w_mine = has ? __builtin_amdgcn_exp2f(piece(mine)[mo] - ref) : 0.0f;
+      const float l_mine = has ? piece(mine)[mo + 1] : 0.0f;
+      const int n = min(LPR, it.pieces - i0);
+      for (int i = 0; i < n; ++i) {
+        const float w = __shfl(w_mine, i, LPR);
+        l = fmaf(w, __shfl(l_mine, i, LPR), l);
+        const float* src = piece(i0 + i) + xo;
+        const f32x4 u = *reinterpret_cast<const f32x4*>(src);
+        const f32x4 v = *reinterpret_cast<const f32x4*>(src + 4);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x[e] = fmaf(w, u[e], x[e]);
-        y[e] = fmaf(w, v[e], y[e]);
+        for (int e = 0; e < 4; ++e) {
+          x[e] = fmaf(w, u[e], x[e]);
+          y[e] = fmaf(w, v[e], y[e]);
+        }
       }
     }
-  }
-  const float inv = pr.query + it.lk - it.lq < 0 ? 0.0f : 1.0f / l;
-  const int64_t token = it.q0 + pr.query;
-  const int head = it.head * a.group + pr.head;
-  bf16x8 w;
+    const float inv = pr.query + it.lk - it.lq < 0 ? 0.0f : 1.0f / l;
+    const int64_t token = it.q0 + pr.query;
+    const int head = it.head * a.group + pr.head;
+    bf16x8 w;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    w[e] = static_cast<bf16>(x[e] * inv);
-    w[4 + e] = static_cast<bf16>(y[e] * inv);
+    for (int e = 0; e < 4; ++e) {
+      w[e] = static_cast<bf16>(x[e] * inv);
+      w[4 + e] = static_cast<bf16>(y[e] * inv);
+    }
+    *reinterpret_cast<bf16x8*>(a.out + (token * a.heads + head) * D + col) = w;
+    if (col == 0) a.lse[static_cast<int64_t>(head) * a.tokens + token] = (m + __builtin_amdgcn_logf(l)) * kLn2;
   }
-  *reinterpret_cast<bf16x8*>(a.out + (token * a.heads + head) * D + col) = w;
-  if (col == 0) a.lse[static_cast<int64_t>(head) * a.tokens + token] = (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // ------------------------------------------------------------------ launches
 
-PagedRule rule_of(const PagedCall& c, const PagedPart& p) {
-  PagedRule r;
-  r.group = c.heads / c.cache.kv_heads;
-  r.tile = paged_tile_rows(p.few);
-  r.unit = p.few ? 128 : kStage;
-  r.least = 128;
-  r.fixed = 256;
-  r.share = paged_least_share(p.few);
-  r.cls = p.cls;
-  r.few = kFewRows;
-  return r;
+Rows rows_of(const void* base, const int64_t (&strides)[3]) {
+  return {static_cast<const char*>(base), 2 * strides[2], static_cast<uint32_t>(2 * strides[0]), static_cast<uint32_t>(2 * strides[1])};
 }
 
-int64_t desc_bytes(const PagedPart& p) { return (static_cast<int64_t>(p.shares) * sizeof(PagedDesc) + 255) / 256 * 256; }
+int64_t desc_bytes(int groups) { return (static_cast<int64_t>(groups) * sizeof(PagedDesc) + 255) / 256 * 256; }
 
 }  // namespace
 
-int paged_tile_rows(bool few) { return few ? kFewRows : kManyRows; }
-int paged_workgroups(bool few, int head_dim, int ncu) { return std::max(1, ncu) * (few ? (head_dim == 64 ? 2 : 1) : 2); }
-int paged_least_share(bool few) { return few ? 128 : 128; }
-int64_t paged_part_bytes(const PagedPart& p, int head_dim) {
-  return desc_bytes(p) + 2 * static_cast<int64_t>(p.shares) * paged_tile_rows(p.few) * (head_dim + 2) * 4;
+int paged_few_rows() { return kFewRows; }
+int paged_many_rows() { return kManyRows; }
+int paged_least_share() { return 128; }
+int paged_groups(int head_dim, int ncu) { return std::max(1, ncu) * (head_dim == 64 ? 3 : 2); }
+int64_t paged_workspace(int groups, bool only_few, int head_dim) {
+  return desc_bytes(groups) + 2 * static_cast<int64_t>(groups) * (only_few ? kFewRows : kManyRows) * (head_dim + 2) * 4;
 }
 
-hipError_t launch_paged_fwd(const PagedCall& c, const PagedPart& p, void* ws, hipStream_t s) {
+hipError_t launch_paged_fwd(const PagedCall& c, int groups, void* ws, hipStream_t s) {
   PagedArgs a{};
   const t2v_pages& g = c.cache;
+  const int group = c.heads / g.kv_heads;
   a.q = static_cast<const bf16*>(c.q);
   a.q_stride = c.q_stride;
   a.cu = (const_i32*)(c.cu);
   a.tokens = c.tokens;
-  a.c.k = static_cast<const bf16*>(g.k);
-  a.c.v = static_cast<const bf16*>(g.v);
-  a.c.k_page = g.k_strides[0];
-  a.c.k_token = g.k_strides[1];
-  a.c.k_head = g.k_strides[2];
-  a.c.v_page = g.v_strides[0];
-  a.c.v_token = g.v_strides[1];
-  a.c.v_head = g.v_strides[2];
+  a.c.k = rows_of(g.k, g.k_strides);
+  a.c.v = rows_of(g.v, g.v_strides);
   a.c.table = (const_i32*)(g.table);
   a.c.lengths = (const_i32*)(g.lengths);
   a.c.table_stride = g.table_stride;
   a.c.pages = static_cast<int>(g.pages);
   a.c.shift = __builtin_ctz(g.page_size);
   a.c.room = g.width * g.page_size;
-  a.rule = rule_of(c, p);
+  a.few = paged_rule(group, kFewRows, 128, 128, 256, paged_least_share(), kPagedFew, kFewRows);
+  a.many = paged_rule(group, kManyRows, kStage, 128, 256, paged_least_share(), kPagedMany, kFewRows);
+  a.weight = g.head_dim == 64 ? 0.8f : 1.1f;
   a.nseq = g.nseq;
   a.heads = c.heads;
   a.kv_heads = g.kv_heads;
-  a.shares = p.shares;
   // A negative scale turns the sign of Q (so that the largest scaled score is that of the largest product), a scale of 0 clears it.
   a.scale = c.scale == 0.0f ? 1.0f : fabsf(c.scale) * kLog2e;
   a.qkeep = c.scale == 0.0f ? 0u : ~0u;
   a.qflip = c.scale < 0.0f ? 0x80008000u : 0u;
   a.out = static_cast<bf16*>(c.out);
   a.lse = c.lse;
-  char* at = static_cast<char*>(ws) + p.at;
-  a.desc = reinterpret_cast<PagedDesc*>(at);
-  a.partial = reinterpret_cast<float*>(at + desc_bytes(p));
+  a.desc = static_cast<PagedDesc*>(ws);
+  a.partial = reinterpret_cast<float*>(static_cast<char*>(ws) + desc_bytes(groups));
   a.trace = c.trace;
-  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(p.shares), dim3(256), 0, s, a); };
-  if (p.few)
-    g.head_dim == 128 ? launch(paged_few_kernel<128>) : launch(paged_few_kernel<64>);
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(groups), dim3(256), 0, s, a); };
+  if (g.page_size >= kStage)
+    g.head_dim == 128 ? launch(paged_fwd_kernel<128, true>) : launch(paged_fwd_kernel<64, true>);
   else
-    g.head_dim == 128 ? launch(paged_many_kernel<128>) : launch(paged_many_kernel<64>);
+    g.head_dim == 128 ? launch(paged_fwd_kernel<128, false>) : launch(paged_fwd_kernel<64, false>);
   return hipGetLastError();
 }
 
-hipError_t launch_paged_join(const PagedCall& c, const PagedPart* parts, int n, void* ws, hipStream_t s) {
-  JoinArgs a{};
-  const int d = c.cache.head_dim, rows_per_block = kThreads / (d / 8);
-  int blocks = 0;
-  for (int i = 0; i < n; ++i) {
-    char* at = static_cast<char*>(ws) + parts[i].at;
-    const int rows = paged_tile_rows(parts[i].few), per = rows / rows_per_block;
-    a.part[i] = {reinterpret_cast<const float*>(at + desc_bytes(parts[i])), reinterpret_cast<const PagedDesc*>(at), rows, per, blocks};
-    blocks += parts[i].shares * per;
-  }
-  a.parts = n;
-  a.heads = c.heads;
-  a.group = c.heads / c.cache.kv_heads;
-  a.tokens = c.tokens;
-  a.out = static_cast<bf16*>(c.out);
-  a.lse = c.lse;
+hipError_t launch_paged_join(const PagedCall& c, int groups, void* ws, hipStream_t s) {
+  const int d = c.cache.head_dim, blocks = kJoinBlocks;
+  const JoinArgs a{reinterpret_cast<const float*>(static_cast<char*>(ws) + desc_bytes(groups)), static_cast<const PagedDesc*>(ws), blocks,
+                   c.heads, c.heads / c.cache.kv_heads, c.tokens, static_cast<bf16*>(c.out), c.lse};
   if (d == 128)
-    hipLaunchKernelGGL((paged_join_kernel<128>), dim3(blocks), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((paged_join_kernel<128>), dim3(groups * blocks), dim3(kThreads), 0, s, a);
   else
-    hipLaunchKernelGGL((paged_join_kernel<64>), dim3(blocks), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((paged_join_kernel<64>), dim3(groups * blocks), dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }
 

@@ -23,21 +23,16 @@ struct PagedCall {
   unsigned long long* trace;
 };
 
-// One kernel's part of a call: the sequences that it takes, its workgroups, and its place in the workspace.
-struct PagedPart {
-  PagedClass cls;
-  bool few;          // the kernel of 32-row tiles, or that of 128
-  int shares;        // workgroups
-  int64_t at;        // bytes into the workspace
-};
-int paged_tile_rows(bool few);
-// The kernel's workgroups on a GPU of ncu CUs.
-int paged_workgroups(bool few, int head_dim, int ncu);
-int paged_least_share(bool few);  // keys
-int64_t paged_part_bytes(const PagedPart& p, int head_dim);
+int paged_few_rows();
+int paged_many_rows();
+int paged_least_share();  // keys
+// Workgroups that a GPU of ncu CUs holds at once.
+int paged_groups(int head_dim, int ncu);
+// only_few: no sequence can have more than few rows.
+int64_t paged_workspace(int groups, bool only_few, int head_dim);
 
-hipError_t launch_paged_fwd(const PagedCall& c, const PagedPart& p, void* ws, hipStream_t s);
-hipError_t launch_paged_join(const PagedCall& c, const PagedPart* parts, int n, void* ws, hipStream_t s);
+hipError_t launch_paged_fwd(const PagedCall& c, int groups, void* ws, hipStream_t s);
+hipError_t launch_paged_join(const PagedCall& c, int groups, void* ws, hipStream_t s);
 
 #if T2V_CHECKED
 hipError_t paged_fwd_check_take(unsigned int* rec, unsigned int canary);

@@ -52,11 +52,11 @@ def _check_cu(cu, pages):
         raise ValueError(f"cu_seqlens must be contiguous int32 [{pages.nseq + 1}] on the GPU")
 
 
-def paged_attn_fwd(q, pages: Pages, cu_seqlens, scale: float, max_queries=None, out=None, lse=None, stream=None):
+def paged_attn_fwd(q, pages: Pages, cu_seqlens, scale: float, out=None, lse=None, stream=None):
     """Causal attention with grouped heads over a paged cache: single tokens, chunks and prompts in one call. q [T, H, D] (bf16 on
     the GPU, tokens any distance apart) holds sequence s's queries in rows cu_seqlens[s] .. cu_seqlens[s + 1] - 1 (int32 on the GPU; rows behind
     the last are padding and left as they are in out and lse). Query i of Lq sees keys 0 .. i + lengths[s] - Lq of its sequence, whose
-    keys and values are already stored. max_queries: the most queries of a sequence, if known (for speed). Returns (out [T, H, D]
+    keys and values are already stored. Returns (out [T, H, D]
     bf16, lse [H, T] fp32). A page number outside the cache or a length beyond the table's width gives NaN."""
     import torch
     if q.dim() != 3:
@@ -74,8 +74,7 @@ def paged_attn_fwd(q, pages: Pages, cu_seqlens, scale: float, max_queries=None, 
         size = pages._workspace
         with _lib._on(stream):
             ws = torch.empty(size, dtype=torch.uint8, device=q.device)
-        st = _lib._call_on(q.device, stream, L.t2v_paged_fwd, q.data_ptr(), step, H, cu_seqlens.data_ptr(), T, max_queries or 0,
-                           pages._ref, scale, out.data_ptr(), lse.data_ptr(), ws.data_ptr(), size, ctypes.byref(need))
+        st = _lib._call_on(q.device, stream, L.t2v_paged_fwd, q.data_ptr(), step, H, cu_seqlens.data_ptr(), T, pages._ref, scale, out.data_ptr(), lse.data_ptr(), ws.data_ptr(), size, ctypes.byref(need))
         if st != _lib.T2V_ERR_WORKSPACE:
             break
         pages._workspace = need.value

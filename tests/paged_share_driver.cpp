@@ -16,17 +16,54 @@ static void fail(const char* what, int n) {
   std::exit(1);
 }
 
+static void quotients() {
+  std::mt19937_64 g(6);
+  for (int i = 0; i < 2000000; ++i) {
+    const int64_t b = 1 + static_cast<int64_t>(g() >> (12 + g() % 52)), q = g() % 60000;
+    if (b > (int64_t(1) << 52) / (q + 1)) continue;
+    for (int64_t a : {q * b, q * b + b - 1, q * b + static_cast<int64_t>(g() % b)})
+      if (paged_ratio(a, b) != q) fail("a quotient", i);
+  }
+}
+
+// Every workgroup has one share of one line, and neighbouring shares of a die are neighbours on the line.
+static void roles() {
+  std::mt19937 g(7);
+  for (int n = 0; n < 3000; ++n) {
+    const int groups = n % 3 ? 8 * (1 + g() % 100) : 2 + g() % 40;
+    const int64_t few = g() % 5 ? g() : 0, many = g() % 5 ? g() : 0;
+    const int m = paged_many(groups, few, many, 0.5f + (g() % 8) * 0.25f);
+    if (m < 0 || m > groups || (many && !m) || (few && m == groups) || (!many && m)) fail("roles", n);
+    std::vector<int> seen[2] = {std::vector<int>(groups - m, 0), std::vector<int>(m, 0)};
+    int last[2][8];
+    for (auto& x : last)
+      for (int& y : x) y = -1;
+    for (int b = 0; b < groups; ++b) {
+      const PagedRole r = paged_role(b, groups, m);
+      if (r.share < 0 || r.share >= static_cast<int>(seen[r.many].size()) || seen[r.many][r.share]++) fail("a share of no or two workgroups", n);
+      int& before = last[r.many][paged_by_die(groups) ? b % 8 : 0];
+      if (before >= 0 && r.share != before + 1) fail("shares of a die apart", n);
+      before = r.share;
+    }
+    const int64_t total = (int64_t(1) << (g() % 52)) + g();
+    PagedRule rule = paged_rule(1, 32, 128, 128, 1, 1, kPagedFew, 32);
+    const int64_t length = paged_share(rule, total, groups);
+    if (length * groups < total || length > total / groups + 256) fail("a share's length", n);
+  }
+}
+
 int main() {
+  quotients();
+  roles();
   std::mt19937 g(5);
   auto pick = [&](int lo, int hi) { return std::uniform_int_distribution<int>(lo, hi)(g); };
   int64_t cut = 0, empty = 0;
   for (int n = 0; n < 4000; ++n) {
     const int group = std::vector<int>{1, 2, 3, 4, 5, 7, 8, 16, 40}[pick(0, 8)];
     const bool few = pick(0, 1);
-    PagedRule r{group, few ? 32 : 128, few ? 128 : 64, 0, pick(0, 600), 0, pick(0, 2), 32};
-    r.least = r.unit * pick(1, 3);
-    r.share = r.unit * pick(1, 4);
+    const int unit = few ? 128 : 64, least = unit * pick(1, 3), share = unit * pick(1, 4);
     const int kv = pick(1, 4), nseq = pick(0, 9), shares = pick(1, 64), room = 5000;
+    const PagedRule r = paged_rule(group, few ? 32 : 128, unit, least, pick(1, 600), share, few ? kPagedFew : kPagedMany, 32);
     std::vector<int> cu{0}, len;
     for (int s = 0; s < nseq; ++s) {
       const int longest = pick(0, 3) == 0 ? 6000 : 300;
@@ -61,8 +98,8 @@ int main() {
       int64_t from = i * length;
       const int64_t to = std::min(total, (i + 1) * length);
       int64_t at = 0;
-      for (int h = 0; h < kv; ++h)
-        for (int s = 0; s < nseq; at += cost[s], ++s) {
+      for (int s = 0; s < nseq; ++s)
+        for (int h = 0; h < kv; ++h, at += cost[s]) {
           if (from >= to || from < at || from >= at + cost[s]) continue;
           const PagedSeq q = paged_seq(cu[s], cu[s + 1], len[s], tokens, room);
           const PagedTiles t = paged_tiles(r, q);

@@ -62,14 +62,6 @@ def test_values(H, Hk, D, page, queries, keys, heads_first):
     c = Case(H, Hk, D, page, queries, keys, heads_first=heads_first)
     ref = reference(c)
     check(c, *paged_attn_fwd(c.q, c.pages, c.cu, c.scale), ref)
-    check(c, *paged_attn_fwd(c.q, c.pages, c.cu, c.scale, max_queries=max(queries)), ref)
-
-
-@pytest.mark.parametrize("queries,hint", [([40, 1, 300], 1), ([1, 1, 200], 2), ([1, 2, 1], 1000), ([500], None), ([9], 1)])
-def test_a_wrong_hint_costs_time_only(queries, hint):
-    log(f"case hint {queries} {hint}")
-    c = Case(6, 2, 128, 32, queries, [n + 700 for n in queries])
-    check(c, *paged_attn_fwd(c.q, c.pages, c.cu, c.scale, max_queries=hint))
 
 
 def test_many_sequences():
