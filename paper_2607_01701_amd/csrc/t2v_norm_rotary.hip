@@ -2,8 +2,15 @@
 // head's D elements; and the backward pass, with dn = R^T dy and x^ = x r: dx = r (w dn - x^ mean(w dn x^)), dw = sum dn x^.
 //
 // A row (token, head) is held by L = D / 16 lanes, 16 elements each in two 16-byte vectors that hold both elements of
-// eight pairs, so that the turn stays within a lane and the norm's sum takes log2 L steps between neighbouring lanes. Pairs (j, j + n) with n no multiple
-// of 8 have no such vectors: there a row goes through LDS in 32 bits (VIA_LDS).
+// eight pairs, so that the turn stays within a lane and the norm's sums take log2 L steps between neighbouring lanes; the lanes of a row read
+// two runs of consecutive bytes. Pairs (j, j + n) with n no multiple of 8 have no such vectors: there a row goes through LDS in 32 bits
+// (VIA_LDS). Sines and cosines are worked out once a token and shared by its heads through LDS, after the first loads.
+//
+// Bound by memory, each element being read and written once (backward: two read, one written): 116,904 tokens of 24 + 24 heads of 128
+// forward 476 us, 6.0 TB/s, backward 867 us, 5.0 TB/s; 20,280 tokens of 24 + 8 heads 57 us, 5.8 TB/s; through LDS (14,750 tokens of 30 + 10
+// heads of 64, 36 dimensions turned) 37 and 50 us. Forward, many short workgroups with one row a lane in flight are fastest: with two rows
+// 514 us of the 490 that it takes without the marks of set_once, with 2 tokens a workgroup in place of 1 525, with 8 555. Backward, 512
+// workgroups that go through their tokens, which leaves few sums for the weights, lose nothing (512 to 32,768 of them: 846 to 870 us).
 #include <algorithm>
 #include <cmath>
 #include <string>
@@ -20,10 +27,11 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kElems = 16;        // of a lane
-constexpr int kRows = 4;          // in flight per lane, forward
+constexpr int kRows = 1;          // in flight per lane, forward
+constexpr int kLeastRows128 = 48; // of a workgroup at head_dim 128, four times as many at 64
 constexpr int kRowsBack = 2;      // backward
 constexpr int kMaxAngles = 2048;  // of a workgroup's tokens (16 KB of LDS)
-constexpr int kMaxBackBlocks = 1024;
+constexpr int kMaxBackBlocks = 512;
 
 struct NormArgs {
   const bf16* in[2];    // q, k
@@ -41,6 +49,7 @@ struct NormArgs {
   int pairs;
   float mscale;
   float* partial;  // backward: [blocks, 2, D]
+  int read_once, write_once;  // forward: inputs and outputs that the caches need not keep
   RotaryAngles angles;
 };
 
@@ -48,6 +57,31 @@ typedef __attribute__((address_space(1))) bf16 gbf16;
 typedef __attribute__((address_space(1))) u32x4 gu32x4;
 T2V_DEV bf16x8 load_vec(const gbf16* p) { return __builtin_bit_cast(bf16x8, *(const gu32x4*)(p)); }
 T2V_DEV void store_vec(gbf16* p, const bf16x8& x) { *(gu32x4*)(p) = __builtin_bit_cast(u32x4, x); }
+
+// A lane's two vectors; once: bytes that the caches need not keep. (The empty assembly keeps the compiler from making one access, without
+// the mark, of the two.)
+T2V_DEV void load_row(bf16x8& x, bf16x8& y, const gbf16* p, const gbf16* q, int once) {
+  if (once) {
+    asm volatile("");
+    x = __builtin_bit_cast(bf16x8, __builtin_nontemporal_load((const gu32x4*)(p)));
+    y = __builtin_bit_cast(bf16x8, __builtin_nontemporal_load((const gu32x4*)(q)));
+    asm volatile("");
+  } else {
+    x = load_vec(p);
+    y = load_vec(q);
+  }
+}
+T2V_DEV void store_row(gbf16* p, gbf16* q, const bf16x8& x, const bf16x8& y, int once) {
+  if (once) {
+    asm volatile("");
+    __builtin_nontemporal_store(__builtin_bit_cast(u32x4, x), (gu32x4*)(p));
+    __builtin_nontemporal_store(__builtin_bit_cast(u32x4, y), (gu32x4*)(q));
+    asm volatile("");
+  } else {
+    store_vec(p, x);
+    store_vec(q, y);
+  }
+}
 
 // Sum over the L neighbouring lanes of a row, in every one of them.
 template <int L>
@@ -67,16 +101,15 @@ template <int D, bool INTERLEAVED, bool VIA_LDS>
 struct RowLane {
   static constexpr int L = D / kElems;
   int v0, v1;
+  // Pair e of the eight that the lane turns. (Those of dimensions that are copied are no pair's; their numbers are not below `pairs`.)
+  T2V_DEV static int pair(int sub, int e) { return INTERLEAVED ? 4 * sub + (e < 4 ? e : D / 4 + e - 4) : 8 * sub + e; }
   T2V_DEV RowLane(int sub, int pairs) {
-    if constexpr (VIA_LDS) {
+    if constexpr (VIA_LDS || INTERLEAVED) {
       v0 = 8 * sub;
       v1 = D / 2 + 8 * sub;
-    } else if constexpr (INTERLEAVED) {
-      v0 = 16 * sub;
-      v1 = v0 + 8;
-    } else {  // pairs is a multiple of 8: lanes hold pairs 8 sub .. 8 sub + 7, or what follows the turned dimensions
-      v0 = 8 * sub < pairs ? 8 * sub : 16 * sub;
-      v1 = v0 + (8 * sub < pairs ? pairs : 8);
+    } else {  // pairs is a multiple of 8: lanes hold pairs 8 sub .. 8 sub + 7, or share what follows the turned dimensions
+      v0 = 8 * sub < pairs ? 8 * sub : 8 * sub + pairs;
+      v1 = v0 + (8 * sub < pairs ? pairs : D / 2 - pairs);
     }
   }
 };
@@ -114,8 +147,9 @@ T2V_DEV void turn_row(float (&u)[kElems], const float2* row, int pairs, int sub,
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float2 k = row[8 * sub + e];
-    const bool turned = 8 * sub + e < pairs;  // chosen, not multiplied by 1 and 0: the others may hold an infinity
+    const int p = at.pair(sub, e);
+    const float2 k = row[p];
+    const bool turned = p < pairs;  // chosen, not multiplied by 1 and 0: the others may hold an infinity
     const float c = fmaf(a[e], k.x, -(b[e] * k.y)), d = fmaf(a[e], k.y, b[e] * k.x);
     a[e] = turned ? c : a[e];
     b[e] = turned ? d : b[e];
@@ -226,8 +260,7 @@ __global__ __launch_bounds__(kThreads) void norm_rotary_kernel(const NormArgs a,
     for (int i = 0; i < kRows; ++i) {
       if (r0 + i * NG < total) {
         const gbf16* s = source(p);
-        x[i] = load_vec(s + at.v0);
-        y[i] = load_vec(s + at.v1);
+        load_row(x[i], y[i], s + at.v0, s + at.v1, a.read_once);
       }
       advance(p);
     }
@@ -257,8 +290,7 @@ __global__ __launch_bounds__(kThreads) void norm_rotary_kernel(const NormArgs a,
         }
         if (a.pairs > 0) turn_row(u, cs + w.t * (D / 2), a.pairs, sub, at, buf);
         gbf16* o = target(w);
-        store_vec(o + at.v0, packed(u, 0));
-        store_vec(o + at.v1, packed(u, 8));
+        store_row(o + at.v0, o + at.v1, packed(u, 0), packed(u, 8), a.write_once);
       }
       advance(w);
     }
@@ -474,8 +506,7 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(const AppendArgs
     for (int i = 0; i < kRows; ++i) {
       if (r0 + i * NG < total) {
         const gbf16* s = source(r);
-        x[i] = load_vec(s + at.v0);
-        y[i] = load_vec(s + at.v1);
+        load_row(x[i], y[i], s + at.v0, s + at.v1, a.read_once);
       }
       advance(r);
     }
@@ -517,8 +548,7 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(const AppendArgs
         gbf16* o = qo + ((t0 + w.t) * hq + w.h) * D;
         if (not_q)
           o = pick(ko, vo, is_v) + to.x * pick(kp, vp, is_v) + to.y * pick(kt, vt, is_v) + (w.h - (is_v ? hq + hk : hq)) * pick(kh, vh, is_v);
-        store_vec(o + at.v0, z0);
-        store_vec(o + at.v1, z1);
+        store_row(o + at.v0, o + at.v1, z0, z1, a.write_once);
       }
       advance(w);
     }
@@ -610,11 +640,26 @@ int check_pointers(const NormArgs& a, int axes, const std::vector<Range>& in, co
   return T2V_OK;
 }
 
-// Tokens of a workgroup: as many as give each lane its kRows rows, as long as there are two workgroups a CU, and no more than
-// the table of angles holds.
+// Tokens of a workgroup: the fewest with kLeast rows of which a quarter at most is missing in the last round of the groups of lanes, as long as
+// there are two workgroups a CU, and no more than the table of angles holds.
 int tokens_per_block(int64_t tokens, int heads, int head_dim) {
-  const int64_t per = std::min<int64_t>(kRows * (kThreads * kElems / head_dim) / heads, tokens / 512);
-  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(per, 2 * kMaxAngles / head_dim)));
+  const int groups = kThreads * kElems / head_dim, least = kLeastRows128 * 128 * 128 / (head_dim * head_dim);
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(tokens / 512, 2 * kMaxAngles / head_dim));
+  for (int per = 1; per < most; ++per) {
+    const int rows = per * heads, rounds = (rows + groups - 1) / groups * groups;
+    if (rows >= least && 4 * rows >= 3 * rounds) return per;
+  }
+  return static_cast<int>(most);
+}
+
+// What the caches need not keep, by the bytes that a call writes (it reads as many) against the 256 MB that lie before the memory. Where both fit:
+// nothing (14,750 tokens, 75 MB: 36 us, 38 to 39 with either hint on reads). Where only the outputs fit: the inputs, so that the outputs wait there for the
+// attention (20,280 tokens, 24 + 8 heads, 166 MB: 57 us against 64; stored in pages, 210 MB: 78 against 90). Else both
+// (116,904 tokens, 1.4 GB: 474 us against 490).
+void set_once(NormArgs* a, int64_t out_bytes) {
+  constexpr int64_t kCache = 256 << 20;
+  a->read_once = 2 * out_bytes > kCache;
+  a->write_once = out_bytes > kCache;
 }
 
 int launched(const char* what) {
@@ -651,6 +696,7 @@ int norm_rotary_impl(const void* q, const void* k, int64_t q_stride, int64_t k_s
   a.positions = turn->positions;
   a.tokens = tokens;
   if (int st = check_pointers(a, axes, in, out)) return st;
+  set_once(&a, 2 * tokens * (heads + static_cast<int64_t>(kv_heads)) * head_dim);
   const int per = tokens_per_block(tokens, heads + kv_heads, head_dim);
   const int64_t blocks = (tokens + per - 1) / per;
   if (blocks * kThreads > UINT32_MAX)  // a launch counts its threads in 32 bits
@@ -709,10 +755,11 @@ int norm_rotary_bwd_impl(const void* q, const void* k, int64_t q_stride, int64_t
   a.positions = turn->positions;
   a.tokens = tokens;
   if (int st = check_pointers(a, tokens > 0 ? axes : 0, in, out)) return st;
-  // Chunks as in the forward pass, as many to a workgroup as leave kMaxBackBlocks of them.
-  const int chunk = tokens_per_block(tokens, heads + kv_heads, head_dim);
-  const int64_t chunks = (tokens + chunk - 1) / chunk, each = std::max<int64_t>(1, (chunks + kMaxBackBlocks - 1) / kMaxBackBlocks);
-  const int blocks = static_cast<int>((chunks + each - 1) / each);
+  // As many workgroups as the GPU holds at once, if they get rows enough to have two in flight in every lane.
+  const int64_t rows = kRowsBack * (kThreads * kElems / head_dim), least = (rows + heads + kv_heads - 1) / (heads + kv_heads);
+  const int64_t each = std::max<int64_t>((tokens + kMaxBackBlocks - 1) / kMaxBackBlocks, std::min<int64_t>(least, (tokens + 255) / 256));
+  const int blocks = tokens == 0 ? 0 : static_cast<int>((tokens + each - 1) / each);
+  const int chunk = static_cast<int>(std::min<int64_t>(each, 2 * kMaxAngles / head_dim));
   const uint64_t bytes = weights ? static_cast<uint64_t>(blocks) * 2 * head_dim * sizeof(float) : 0;
   if (need != nullptr) *need = bytes;
   if (ws_bytes < bytes)
@@ -722,7 +769,7 @@ int norm_rotary_bwd_impl(const void* q, const void* k, int64_t q_stride, int64_t
   if (blocks > 0) {
     with_form(a, head_dim, interleaved, [&](auto d, auto il, auto lds) {
       hipLaunchKernelGGL((norm_rotary_bwd_kernel<decltype(d)::value, decltype(il)::value, decltype(lds)::value>), dim3(blocks),
-                         dim3(kThreads), 0, s, a, static_cast<int>(each * chunk), chunk);
+                         dim3(kThreads), 0, s, a, static_cast<int>(each), chunk);
     });
     if (int st = launched("norm and rotary backward kernel")) return st;
   }
@@ -797,6 +844,7 @@ int paged_append_impl(const void* k, const void* v, int64_t k_stride, int64_t v_
   p.pages = static_cast<int>(g.pages);
   p.shift = __builtin_ctz(g.page_size);
   p.room = g.width * g.page_size;
+  set_once(&a, 2 * tokens * (heads + 2 * static_cast<int64_t>(g.kv_heads)) * g.head_dim);
   const int per = tokens_per_block(tokens, heads + 2 * g.kv_heads, g.head_dim);
   const int64_t blocks = (tokens + per - 1) / per;
   if (blocks * kThreads > UINT32_MAX)
