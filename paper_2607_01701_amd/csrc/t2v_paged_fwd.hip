@@ -564,7 +564,7 @@ T2V_DEV void many_pieces(Walk& w, bf16* lds) {
         const uint32_t vb0 = lds_addr(sV(b)) + vo0, vb1 = lds_addr(sV(b)) + vo1;
 #pragma unroll
         for (int kb = 0; kb < kStage; kb += 32)
-          fwd_step<D, false>(kbase, vb0, vb1, kb, 0, a.scale, qop, o, m_run, l_run, lane);
+          fwd_step<D, false>(kbase, vb0, vb1, kb, 0, scale, qop, o, m_run, l_run, lane);
         wait_vmcnt0();
         __syncthreads();
       }

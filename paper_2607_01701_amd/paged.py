@@ -52,6 +52,14 @@ def _check_cu(cu, pages):
         raise ValueError(f"cu_seqlens must be contiguous int32 [{pages.nseq + 1}] on the GPU")
 
 
+def _same_device(device, *named):
+    for name, t in named:
+        if t.device != device:
+            if not t.is_cuda:
+                raise ValueError(f"{name} must be a CUDA tensor")
+            raise ValueError(f"{name} is on {t.device}, the pages on {device}")
+
+
 def paged_attn_fwd(q, pages: Pages, cu_seqlens, scale: float, out=None, lse=None, stream=None):
     """Causal attention with grouped heads over a paged cache: single tokens, chunks and prompts in one call. q [T, H, D] (bf16 on
     the GPU, tokens any distance apart) holds sequence s's queries in rows cu_seqlens[s] .. cu_seqlens[s + 1] - 1 (int32 on the GPU; rows behind
@@ -66,18 +74,26 @@ def paged_attn_fwd(q, pages: Pages, cu_seqlens, scale: float, out=None, lse=None
         raise ValueError(f"q has head_dim {D}, the pages {pages.head_dim}")
     step = _lib._check_rows(q, "q", (T, H, D))
     _check_cu(cu_seqlens, pages)
-    named = [("k", pages.k), ("q", q), ("cu_seqlens", cu_seqlens)]
-    (out, lse), given = _lib._outputs((("out", out, (T, H, D), torch.bfloat16), ("lse", lse, (H, T), torch.float32)), q.device, stream)
-    _lib._check_on_device((*named, *given))
-    L, need = _lib.lib(), ctypes.c_uint64()
-    for _ in range(2):
-        size = pages._workspace
+    device = pages.device
+    _same_device(device, ("q", q), ("cu_seqlens", cu_seqlens))
+    size = pages._workspace
+    if out is None and lse is None and stream is None:
+        out = torch.empty((T, H, D), dtype=torch.bfloat16, device=device)
+        lse = torch.empty((H, T), dtype=torch.float32, device=device)
+        ws = torch.empty(size, dtype=torch.uint8, device=device)
+    else:
+        (out, lse), given = _lib._outputs((("out", out, (T, H, D), torch.bfloat16), ("lse", lse, (H, T), torch.float32)), device, stream)
+        _same_device(device, *given)
         with _lib._on(stream):
-            ws = torch.empty(size, dtype=torch.uint8, device=q.device)
-        st = _lib._call_on(q.device, stream, L.t2v_paged_fwd, q.data_ptr(), step, H, cu_seqlens.data_ptr(), T, pages._ref, scale, out.data_ptr(), lse.data_ptr(), ws.data_ptr(), size, ctypes.byref(need))
-        if st != _lib.T2V_ERR_WORKSPACE:
-            break
-        pages._workspace = need.value
+            ws = torch.empty(size, dtype=torch.uint8, device=device)
+    L, need = _lib.lib(), ctypes.c_uint64()
+    args = (q.data_ptr(), step, H, cu_seqlens.data_ptr(), T, pages._ref, scale, out.data_ptr(), lse.data_ptr())
+    st = _lib._call_on(device, stream, L.t2v_paged_fwd, *args, ws.data_ptr(), size, ctypes.byref(need))
+    if st == _lib.T2V_ERR_WORKSPACE:
+        size = pages._workspace = need.value  # more than any call so far
+        with _lib._on(stream):
+            ws = torch.empty(size, dtype=torch.uint8, device=device)
+        st = _lib._call_on(device, stream, L.t2v_paged_fwd, *args, ws.data_ptr(), size, ctypes.byref(need))
     if st != _lib.T2V_OK:
         _lib._check(L, st)
     return out, lse
@@ -96,7 +112,8 @@ def paged_append(k, v, pages: Pages, cu_seqlens, q=None, positions=None, freqs=N
     shape = (T, pages.kv_heads, D)
     sk, sv = _lib._check_rows(k, "k", shape), _lib._check_rows(v, "v", shape)
     _check_cu(cu_seqlens, pages)
-    named = [("pages", pages.k), ("k", k), ("v", v), ("cu_seqlens", cu_seqlens)]
+    device = pages.device
+    named = [("k", k), ("v", v), ("cu_seqlens", cu_seqlens)]
     turn = None
     if freqs is not None or eps is not None:
         checked = _checked(q, k, positions, freqs, layout, sections, mscale, q_weight, k_weight, eps)
@@ -109,19 +126,23 @@ def paged_append(k, v, pages: Pages, cu_seqlens, q=None, positions=None, freqs=N
         heads = q.shape[1]
         sq, qp = _lib._check_rows(q, "q", (T, heads, D)), q.data_ptr()
         named.append(("q", q))
-        (q_out,), given = _lib._outputs((("q_out", q_out, (T, heads, D), torch.bfloat16),), k.device, stream)
+        if q_out is None and stream is None:
+            q_out = torch.empty((T, heads, D), dtype=torch.bfloat16, device=device)
+        else:
+            (q_out,), given = _lib._outputs((("q_out", q_out, (T, heads, D), torch.bfloat16),), device, stream)
     elif q_out is not None:
         raise ValueError("q_out is given without q")
     for name, t in (("positions", positions), ("q_weight", q_weight), ("k_weight", k_weight)):
         if t is not None:
             named.append((name, t))
-    _lib._check_on_device((*named, *given))
+    _same_device(device, *named, *given)
     if checked is not None:
-        with _lib._on(stream):
-            q_weight, k_weight = _aligned_weight(q_weight), _aligned_weight(k_weight)
+        if q_weight is not None or k_weight is not None:
+            with _lib._on(stream):
+                q_weight, k_weight = _aligned_weight(q_weight), _aligned_weight(k_weight)
         turn = ctypes.byref(_turn_struct(checked, positions, q_weight, k_weight))
     L = _lib.lib()
-    st = _lib._call_on(k.device, stream, L.t2v_paged_append, k.data_ptr(), v.data_ptr(), sk, sv, qp, sq, heads,
+    st = _lib._call_on(device, stream, L.t2v_paged_append, k.data_ptr(), v.data_ptr(), sk, sv, qp, sq, heads,
                        cu_seqlens.data_ptr(), T, pages._ref, turn, None if q_out is None else q_out.data_ptr())
     if st != _lib.T2V_OK:
         _lib._check(L, st)

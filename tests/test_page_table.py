@@ -274,6 +274,7 @@ def pages(monkeypatch):
     monkeypatch.setattr(_lib, "_check_on_device", lambda named: None)
     p = t2v.Pages(_t(4, 16, 2, 128), _t(4, 16, 2, 128), _t(3, 5, dtype=torch.int32), _t(3, dtype=torch.int32))
     monkeypatch.undo()
+    p.device = torch.device("cuda", 0)  # as pages have
     return p
 
 
