@@ -1583,9 +1583,9 @@ int paged_fwd_impl(PagedCall& c, const t2v_pages* cache, void* ws, uint64_t ws_b
   if (c.q_stride < static_cast<int64_t>(c.heads) * g.head_dim || c.q_stride % 8 != 0 || c.q_stride > (int64_t(1) << 22))
     return bad("q_stride must be a multiple of 8 between heads * head_dim and 2^22, got " + std::to_string(c.q_stride));
   if (c.tokens == 0 || g.nseq == 0) return T2V_OK;
-  // The kernels count a call's work in 1 / 256 of a key, exact in a double.
+  // The kernels count a call's work in 1 / 256 of a key.
   const double group = c.heads / g.kv_heads, room = static_cast<double>(g.width) * g.page_size;
-  if (256.0 * (c.tokens * group / paged_few_rows() + g.nseq) * (room + 4096.0 + c.tokens) * g.kv_heads > 0x1p52)
+  if (256.0 * (c.tokens * group / paged_few_rows() + g.nseq) * (room + 4096.0 + c.tokens) * g.kv_heads > static_cast<double>(kPagedMost))
     return bad("the call's largest possible work (queries times the table's width) passes what the kernels count");
   const std::vector<Range> out = {{c.out, tensor_bytes(c.tokens, c.heads, g.head_dim), "out"}, {c.lse, c.tokens * c.heads * 4, "lse"},
                                   {ws, static_cast<int64_t>(ws_bytes), "ws"}};

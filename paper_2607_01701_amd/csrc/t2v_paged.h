@@ -26,6 +26,15 @@
 
 namespace t2v {
 
+// The longest line. (Positions are exact in a double, and sums of 64 sequences' in 64 bits.) A call whose sequences can reach it is refused;
+// where offsets decrease, they may all the same, as each has the queries that others have too: then no work is done.
+constexpr int64_t kPagedMost = int64_t(1) << 52;
+T2V_HD int64_t paged_add(int64_t sum, int64_t more) {
+  const int64_t x = sum + more;
+  return x > kPagedMost ? kPagedMost + 1 : x;
+}
+T2V_HD int64_t paged_line(int64_t sum, int64_t other) { return sum > kPagedMost || other > kPagedMost ? 0 : sum; }
+
 // Which sequences a line takes: those with at most `few` rows, or those with more.
 enum PagedClass { kPagedFew = 0, kPagedMany = 1 };
 

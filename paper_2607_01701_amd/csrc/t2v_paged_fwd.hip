@@ -110,11 +110,12 @@ T2V_DEV int64_t wave_scan(int64_t x) {
 // `seq`, whose interval begins at `at`.
 struct Walk {
   bool many;
-  int share, n_few, head, seq;
+  int share, shares, n_few, head, seq;
   int64_t at, from, to, length;
 };
 
-// Each wave works it out by itself: costs of 64 sequences at a time, their sums over the lanes, and a search.
+// Each wave works it out by itself: costs of 64 sequences at a time, their sums over the lanes, and a search. (Offsets or lengths that
+// something changes meanwhile may be found nowhere: then this workgroup does no work.)
 T2V_DEV Walk find_share(const PagedArgs& a, int lane) {
   const int* cu = (const int*)(a.cu);
   const int* lengths = (const int*)(a.c.lengths);
@@ -134,15 +135,16 @@ T2V_DEV Walk find_share(const PagedArgs& a, int lane) {
   for (int s0 = 0; s0 < a.nseq; s0 += 64) {
     costs(s0);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) sum[i] += lane_of(upto[i], 63);
+    for (int i = 0; i < 2; ++i) sum[i] = paged_add(sum[i], lane_of(upto[i], 63));
   }
   const int groups = gridDim.x, n_many = uniform(paged_many(groups, sum[0], sum[1], a.weight));
   const PagedRole role = paged_role(blockIdx.x, groups, n_many);
   const int shares = role.many ? n_many : groups - n_many;
-  const int64_t total = role.many ? sum[1] : sum[0];
+  const int64_t total = role.many ? paged_line(sum[1], sum[0]) : paged_line(sum[0], sum[1]);
   Walk w;
   w.many = role.many;
   w.share = role.share;
+  w.shares = shares;
   w.n_few = groups - n_many;
   w.length = paged_share(role.many ? a.many : a.few, total, shares);
   w.from = w.share * w.length;
@@ -153,7 +155,7 @@ T2V_DEV Walk find_share(const PagedArgs& a, int lane) {
   int64_t base = 0;
   int s0 = 0;
   if (a.nseq > 64) {
-    for (;; s0 += 64) {
+    for (; s0 < a.nseq; s0 += 64) {
       costs(s0);
       const int64_t all = lane_of(role.many ? upto[1] : upto[0], 63);
       if (w.from < base + all) break;
@@ -162,7 +164,12 @@ T2V_DEV Walk find_share(const PagedArgs& a, int lane) {
   }
   const int64_t rest = w.from - base, end = role.many ? upto[1] : upto[0], one = role.many ? cost[1] : cost[0];
   const int64_t begin = end - one * a.kv_heads;
-  const int at = __builtin_ctzll(__ballot(rest >= begin && rest < end));
+  const uint64_t found = __ballot(rest >= begin && rest < end);
+  if (found == 0) {
+    w.to = w.from;
+    return w;
+  }
+  const int at = __builtin_ctzll(found);
   const int64_t first = lane_of(begin, at), head_cost = lane_of(one, at);
   w.seq = s0 + at;
   w.head = uniform(paged_ratio(rest - first, head_cost));
@@ -181,7 +188,7 @@ T2V_DEV int64_t slot_floats(const Walk& w, int rows) {
 template <int D, typename F>
 T2V_DEV void for_pieces(Walk& w, F&& f) {
   bool begun = false;
-  while (w.from < w.to) {
+  while (w.from < w.to && w.seq < arguments().nseq) {
     const PagedArgs& a = arguments();
     const PagedRule rule = w.many ? a.many : a.few;
     const PagedSeq s = seq_at(a, w.seq);
@@ -197,7 +204,7 @@ T2V_DEV void for_pieces(Walk& w, F&& f) {
             begun = true;
             const int64_t place = slot_floats<D>(w, rule.tile), slot = static_cast<int64_t>(rule.tile) * (D + 2);
             if (threadIdx.x == 0)
-              arguments().desc[blockIdx.x] = {s.q0, place + slot, place + 2 * slot, s.lq, s.lk, tile * rule.tile, w.head, p.pieces, rule.tile};
+              arguments().desc[blockIdx.x] = {s.q0, place + slot, place + 2 * slot, s.lq, s.lk, tile * rule.tile, w.head, min(p.pieces, w.shares - w.share), rule.tile};
           }
           f(w.seq, s, t, w.head, p);
         }
@@ -216,7 +223,7 @@ T2V_DEV void for_pieces(Walk& w, F&& f) {
 // Row r of a tile: where it is in [T, H, D] tensors, and the last key that it sees. Rows behind the last repeat it.
 T2V_DEV LaneRow row_of(const PagedArgs& a, const PagedSeq& s, const PagedTiles& t, int head, int row) {
   const PackedRow pr = packed_row(min(row, t.rows - 1), a.few.group);
-  return {row < t.rows, pr.query + s.lk - s.lq, head * a.few.group + pr.head, s.q0 + pr.query};
+  return {row < t.rows, pr.query + (s.lk - s.lq), head * a.few.group + pr.head, s.q0 + pr.query};
 }
 
 T2V_DEV void load_queries(const PagedArgs& a, const bf16* p, bool ok, int G, bf16x8* qop, int n) {
@@ -690,7 +697,7 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(const JoinArgs a) 
         }
       }
     }
-    const float inv = pr.query + it.lk - it.lq < 0 ? 0.0f : 1.0f / l;
+    const float inv = pr.query + (it.lk - it.lq) < 0 ? 0.0f : 1.0f / l;
     const int64_t token = it.q0 + pr.query;
     const int head = it.head * a.group + pr.head;
     bf16x8 w;

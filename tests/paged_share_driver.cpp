@@ -52,8 +52,30 @@ static void roles() {
   }
 }
 
+// Offsets that decrease give many sequences the queries of one: the line's length stays within what is counted, or there is no work.
+static void long_lines() {
+  const PagedRule few = paged_rule(16, 32, 128, 128, 256, 128, kPagedFew, 32), many = paged_rule(16, 128, 64, 128, 256, 128, kPagedMany, 32);
+  // Every second sequence has 1,024 tiles of a little more than 2^30 keys, 2^48 positions: 16 of them pass 2^52.
+  for (const int nseq : {1, 2, 100, 1 << 12, 1 << 20}) {
+    int64_t sum[2] = {0, 0};
+    for (int s0 = 0; s0 < nseq; s0 += 64) {
+      int64_t more[2] = {0, 0};
+      for (int s = s0; s < std::min(nseq, s0 + 64); ++s) {
+        const PagedSeq q = paged_seq(s % 2 ? 8192 : 0, s % 2 ? 0 : 8192, 1 << 30, 8192, 1 << 30);
+        more[0] += paged_cost(few, paged_tiles(few, q));
+        more[1] += paged_cost(many, paged_tiles(many, q));
+      }
+      for (int i = 0; i < 2; ++i) sum[i] = paged_add(sum[i], more[i]);
+    }
+    const int64_t total = paged_line(sum[1], sum[0]), length = paged_share(many, total, 512);
+    if (total < 0 || total > kPagedMost || (total == 0) != ((nseq + 1) / 2 >= 16) || length * 512 < total) fail("a line's length", nseq);
+    if (paged_line(sum[0], sum[1]) != 0) fail("work on an empty line", nseq);
+  }
+}
+
 int main() {
   quotients();
+  long_lines();
   roles();
   std::mt19937 g(5);
   auto pick = [&](int lo, int hi) { return std::uniform_int_distribution<int>(lo, hi)(g); };

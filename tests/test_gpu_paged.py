@@ -168,6 +168,20 @@ def test_offsets_that_no_batch_has_touch_nothing_outside():
         assert (buf[:32] == 7.0).all() and (buf[32 + c.T:] == 7.0).all()
 
 
+def test_offsets_that_multiply_the_work_end_without_any():
+    log("case many long sequences with the queries of one")
+    n, T, width = 4096, 8192, 16384
+    k = torch.ones(1, 65536, 1, 64, dtype=torch.bfloat16, device="cuda")
+    pages = Pages(k, k.clone(), torch.zeros(n, width, dtype=torch.int32, device="cuda"), torch.full((n,), 2 ** 30, dtype=torch.int32, device="cuda"))
+    cu = torch.zeros(n + 1, dtype=torch.int32, device="cuda")
+    cu[1::2] = T
+    q = torch.zeros(T, 16, 64, dtype=torch.bfloat16, device="cuda")
+    out = torch.full_like(q, 7.0)
+    paged_attn_fwd(q, pages, cu, 0.1, out=out)
+    torch.cuda.synchronize()
+    assert (out == 7.0).all()
+
+
 def test_no_queries_no_sequences():
     c = Case(4, 2, 64, 16, [0, 0], [30, 20])
     out, lse = paged_attn_fwd(c.q, c.pages, c.cu, c.scale)
