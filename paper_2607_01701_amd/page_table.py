@@ -18,6 +18,7 @@ class PageTable:
         self.table = np.full((sequences, width), -1, dtype=np.int32)
         self.lengths = np.zeros(sequences, dtype=np.int32)
         self.counts = np.zeros(sequences, dtype=np.int32)  # pages of each sequence: those of its tokens, and reserved ones
+        self.room = np.zeros(sequences, dtype=np.int64)  # tokens that may follow each sequence's: reserved, and in pages of its own
         self.active = np.zeros(sequences, dtype=bool)
         self.refs = np.zeros(pages, dtype=np.int32)
         self._free = list(range(pages - 1, -1, -1))
@@ -48,7 +49,8 @@ class PageTable:
 
     def reserve(self, sequences, tokens):
         """Makes room for so many more tokens in each sequence without adding them; returns the pages to copy first (src, dst): those
-        that the next tokens go to and that others share. Raises without a change if pages or the table do not suffice."""
+        that the next tokens go to and that others share. The room lasts until the sequence is forked or truncated: its next tokens may go
+        to a page that others share then. Raises without a change if pages or the table do not suffice."""
         rows, more = self._rows(sequences, tokens)
         new = self.lengths[rows].astype(np.int64) + more
         want = -(-new // self.page_size)
@@ -81,6 +83,7 @@ class PageTable:
             for _ in range(n):
                 self.table[s, self.counts[s]] = self._take()
                 self.counts[s] += 1
+        self.room[rows] = np.maximum(self.room[rows], more)
         return np.array(src, dtype=np.int32), np.array(dst, dtype=np.int32)
 
     def _take(self) -> int:
@@ -97,10 +100,10 @@ class PageTable:
     def grown(self, sequences, tokens) -> None:
         """Tokens that were added in room reserved before."""
         rows, more = self._rows(sequences, tokens)
-        new = self.lengths[rows].astype(np.int64) + more
-        if (new > self.counts[rows].astype(np.int64) * self.page_size).any():
-            raise ValueError("more tokens than were reserved")
-        self.lengths[rows] = new
+        if (more > self.room[rows]).any():
+            raise ValueError("more tokens than were reserved (a fork or truncation ends the room)")
+        self.room[rows] -= more
+        self.lengths[rows] += more.astype(np.int32)
 
     def fork(self, sequence: int) -> int:
         """A new sequence with the same tokens, whose pages both share."""
@@ -110,6 +113,7 @@ class PageTable:
         self.table[t, :n] = self.table[s, :n]
         self.refs[self.table[s, :n]] += 1
         self.counts[t], self.lengths[t] = n, self.lengths[s]
+        self.room[s] = 0
         return t
 
     def free(self, sequence: int) -> None:
@@ -133,6 +137,7 @@ class PageTable:
         self._free.extend(int(p) for p in pages[::-1] if self.refs[p] == 0)
         self.table[s, keep:self.counts[s]] = -1
         self.counts[s] = keep
+        self.room[s] = 0
 
     def compact(self):
         """Moves pages so that those in use are the first ones; returns the copies (src, dst) that carry them out."""

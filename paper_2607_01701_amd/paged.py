@@ -195,7 +195,8 @@ class PagedCache:
 
     cu_seqlens (cache.offsets({s: prompt_tokens})) has an entry for every sequence and one more. The bookkeeping is on the host (table:
     PageTable); its changes and the pages' copies are enqueued on the current stream, which the calls on the cache must follow. A captured step reads
-    lengths and table on the GPU: reserve() room for its tokens, let the graph add them to ``lengths``, and tell grown() afterwards."""
+    lengths and table on the GPU: reserve() room for its tokens, let the graph add them to ``lengths``, and tell grown() afterwards, before any
+    other change. A fork or truncation of a sequence ends its room: reserve() again before the next replay."""
 
     def __init__(self, layers: int, pages: int, kv_heads: int, head_dim: int, page_size: int = 64, sequences: int = 64, width=None,
                  device="cuda"):
@@ -207,6 +208,8 @@ class PagedCache:
         self.lengths = torch.zeros(sequences, dtype=torch.int32, device=device)
         self._layers = [Pages(x[0], x[1], self.table, self.lengths) for x in self.data]
         self._buffers = [y for x in self.data for y in x]
+        self._sent = self.host.table.copy()  # what the GPU's table holds
+        self._width = 0  # columns of it that may hold pages
 
     def layer(self, i: int) -> Pages:
         """Layer i's pages, for paged_append and paged_attn_fwd."""
@@ -218,10 +221,15 @@ class PagedCache:
 
     def offsets(self, tokens):
         """cu_seqlens on the GPU for a call in which sequence s has tokens[s] new tokens (a dict, or one count for each sequence)."""
-        counts = np.zeros(self.host.active.size, dtype=np.int32)
+        counts = np.zeros(self._host().active.size, dtype=np.int64)
         for s, n in tokens.items() if isinstance(tokens, dict) else enumerate(tokens):
+            if not 0 <= s < counts.size or n < 0:
+                raise ValueError(f"{n} tokens of sequence {s}, of {counts.size}")
             counts[s] = n
-        return self._to_device(np.concatenate([[0], np.cumsum(counts)]).astype(np.int32))
+        cu = np.concatenate([[0], np.cumsum(counts)])
+        if cu[-1] >= 2 ** 31:
+            raise ValueError(f"{cu[-1]} tokens are too many for one call")
+        return self._to_device(cu.astype(np.int32))
 
     def _to_device(self, x, out=None):
         import torch
@@ -232,13 +240,18 @@ class PagedCache:
         """The bookkeeping, for a change of it."""
         import torch
         if self.data.is_cuda and torch.cuda.is_current_stream_capturing():
-            raise RuntimeError("a captured graph cannot hand out or free pages: reserve() room before the capture")
+            raise RuntimeError("a captured graph cannot hand out or free pages, nor take offsets: reserve() room and make them before the capture")
         return self.host
 
     def _sync(self, pairs=None, lengths=True):
         if pairs is not None and pairs[0].size:
             page_copy(self._buffers, *pairs)
-        self._to_device(self.host.table, self.table)
+        width = max(self._width, int(self.host.counts.max()))
+        now, sent = self.host.table[:, :width], self._sent[:, :width]
+        if not np.array_equal(now, sent):
+            self._to_device(np.ascontiguousarray(now), self.table[:, :width])
+            sent[:] = now
+        self._width = int(self.host.counts.max())
         if lengths:
             self._to_device(self.host.lengths, self.lengths)
 

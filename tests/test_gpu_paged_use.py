@@ -321,6 +321,8 @@ def test_a_captured_block_writes_an_answer():
         y = step()
         with pytest.raises(RuntimeError, match="captured"):
             cache.extend([0], [1])
+        with pytest.raises(RuntimeError, match="captured"):
+            cache.offsets([1, 1])
     texts = list(prompts)
     for i in range(40):
         x.copy_(torch.randn(2, 96, generator=g))
@@ -332,6 +334,28 @@ def test_a_captured_block_writes_an_answer():
     cache.grown([0, 1], 40)
     torch.cuda.synchronize()
     assert torch.equal(cache.lengths.cpu(), torch.from_numpy(cache.host.lengths))
+
+
+def test_cache_offsets_and_tables_on_the_gpu():
+    log("case offsets and tables")
+    cache = PagedCache(1, 40, 1, 64, page_size=16, sequences=3, width=20)
+    assert cache.offsets({2: 5, 0: 3}).tolist() == [0, 3, 3, 8] and cache.offsets([1, 2]).tolist() == [0, 1, 3, 3]
+    for bad in ({3: 1}, {-1: 1}, {0: -1}, [1, 1, 1, 1], {0: 2 ** 31 - 1, 1: 1}):
+        with pytest.raises(ValueError, match="tokens"):
+            cache.offsets(bad)
+    r = np.random.default_rng(2)
+    a, b = cache.add(), cache.add()
+    for step in range(40):  # longer, shorter, none
+        s = (a, b)[step % 2]
+        do = r.integers(0, 3)
+        if do == 0:
+            cache.truncate(s, int(r.integers(0, cache.host.lengths[s] + 1)))
+        elif do == 1 and cache.host.lengths[s] < 200:
+            cache.extend([s], [int(r.integers(0, 90))])
+        else:
+            cache.compact()
+        assert torch.equal(cache.table.cpu(), torch.from_numpy(cache.host.table))
+        assert torch.equal(cache.lengths.cpu(), torch.from_numpy(cache.host.lengths))
 
 
 def test_the_definition_end_to_end():

@@ -129,6 +129,29 @@ def test_page_table_refusals(do, err, msg):
     assert t.lengths.tolist() == [8, 0, 0, 0] and t.free_pages == 4
 
 
+def test_forks_and_truncations_end_reserved_room():
+    m = Memory(10, 16, 4, 8)
+    s = m.t.add()
+    m.copy(m.t.extend([s], [20]))
+    m.write(s, 0, range(20))
+    m.copy(m.t.reserve([s], 9))
+    m.t.grown([s], 4)
+    m.write(s, 20, range(20, 24))
+    with pytest.raises(ValueError, match="reserved"):
+        m.t.grown([s], 6)
+    f = m.t.fork(s)  # the next tokens of s would go to a page that f has
+    for x in (s, f):
+        with pytest.raises(ValueError, match="reserved"):
+            m.t.grown([x], 1)
+    src, _ = m.t.reserve([s], 2)
+    assert src.tolist() == [int(m.t.table[f, 1])]
+    m.t.grown([s], 1)
+    m.t.truncate(s, 10)
+    with pytest.raises(ValueError, match="reserved"):
+        m.t.grown([s], 1)
+    assert m.t.lengths[[s, f]].tolist() == [10, 24]
+
+
 # ------------------------------------------------------------------------ the calls
 
 
