@@ -643,9 +643,10 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void paged_fwd_kernel(const P
 
 // ------------------------------------------------------------------ join
 
-// Workgroups of a cut tile. Most tiles of few rows leave all but one idle, and the launch of 512 x 8 of them takes 1 us more than of 512 x 4;
-// with two, large tiles take 6 us longer.
+// Workgroups of a cut tile of many rows, in calls whose sequences have more than 32 packed rows each in the mean; else one, as most
+// tiles have few.
 constexpr int kJoinBlocks = 4;
+constexpr int kJoinAhead = 4;  // pieces of a row in flight
 
 struct JoinArgs {
   const float* partial;
@@ -657,56 +658,81 @@ struct JoinArgs {
 };
 
 // Joins the pieces of the tile that a workgroup begins: with the largest reference m of a row, out = sum_p 2^(m_p - m) O_p / l,
-// l = sum_p 2^(m_p - m) l_p, in piece order. D / 8 lanes hold a row, eight columns each.
+// l = sum_p 2^(m_p - m) l_p, in piece order. D / 8 lanes hold a row, eight columns each. Of a tile with fewer rows than a workgroup holds, several groups
+// of lanes take parts of the pieces, whose sums meet in LDS, in order.
 template <int D>
 __global__ __launch_bounds__(kThreads) void paged_join_kernel(const JoinArgs a) {
   constexpr int LPR = D / 8, RPB = kThreads / LPR;
+  __shared__ __attribute__((aligned(16))) float part_x[RPB][D];
+  __shared__ float part_l[RPB];
   const PagedDesc it = a.desc[blockIdx.x / a.blocks];
   if (it.pieces == 0) return;
-  const int sub = threadIdx.x % LPR, col = sub * 8;
-  for (int r = (blockIdx.x % a.blocks) * RPB + threadIdx.x / LPR; r < it.rows; r += a.blocks * RPB) {  // row of the tile
-    const int row = it.row0 + r;
-    if (row >= it.lq * a.group) break;  // all lanes of a row alike
-    const PackedRow pr = packed_row(row, a.group);
-    const int64_t share = static_cast<int64_t>(it.rows) * 2 * (D + 2);
-    auto piece = [&](int i) { return a.partial + (i == 0 ? it.first : it.next + (i - 1) * share); };
+  const int sub = threadIdx.x % LPR, col = sub * 8, group = threadIdx.x / LPR, block = blockIdx.x % a.blocks;
+  const int64_t share = static_cast<int64_t>(it.rows) * 2 * (D + 2);
+  auto piece = [&](int i) { return a.partial + (i == 0 ? it.first : it.next + (i - 1) * share); };
+  const int rows = min(it.rows, it.lq * a.group - it.row0);
+  int parts = 1;
+  while (2 * parts * rows <= RPB) parts *= 2;
+  const int per_part = (it.pieces + parts - 1) / parts, held = RPB / parts;  // rows at a time
+  if (parts > 1 && block > 0) return;
+  for (int r0 = parts > 1 ? 0 : block * RPB; r0 < rows; r0 += a.blocks * RPB) {  // all threads alike
+    const int r = r0 + group % held, part = group / held;
+    const bool real = r < rows;
+    const int begin = part * per_part, end = real ? min(begin + per_part, it.pieces) : begin;
     const int mo = it.rows * D + 2 * r, xo = r * D + col;
     float m = -kInf;
-    for (int i = sub; i < it.pieces; i += LPR) m = max_nan(m, piece(i)[mo]);
+    for (int i = real ? sub : it.pieces; i < it.pieces; i += LPR) m = max_nan(m, piece(i)[mo]);
 #pragma unroll
     for (int off = LPR / 2; off > 0; off >>= 1) m = max_nan(m, __shfl_xor(m, off, LPR));
     const float ref = m == -kInf ? 0.0f : m;
     float l = 0.0f;
     f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f}, y = x;
-    for (int i0 = 0; i0 < it.pieces; i0 += LPR) {
-      const int mine = i0 + sub;
-      const bool has = mine < it.pieces;
-      const float w_mine = has ? __builtin_amdgcn_exp2f(piece(mine)[mo] - ref) : 0.0f;
-      const float l_mine = has ? piece(mine)[mo + 1] : 0.0f;
-      const int n = min(LPR, it.pieces - i0);
-      for (int i = 0; i < n; ++i) {
-        const float w = __shfl(w_mine, i, LPR);
-        l = fmaf(w, __shfl(l_mine, i, LPR), l);
-        const float* src = piece(i0 + i) + xo;
-        const f32x4 u = *reinterpret_cast<const f32x4*>(src);
-        const f32x4 v = *reinterpret_cast<const f32x4*>(src + 4);
+    for (int i0 = begin; i0 < end; i0 += kJoinAhead) {
+      f32x4 u[kJoinAhead], v[kJoinAhead];
+      float w[kJoinAhead], lw[kJoinAhead];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[e] = fmaf(w, u[e], x[e]);
-          y[e] = fmaf(w, v[e], y[e]);
+      for (int e = 0; e < kJoinAhead; ++e) {
+        const float* src = piece(min(i0 + e, end - 1));
+        u[e] = *reinterpret_cast<const f32x4*>(src + xo);
+        v[e] = *reinterpret_cast<const f32x4*>(src + xo + 4);
+        w[e] = src[mo];
+        lw[e] = src[mo + 1];
+      }
+#pragma unroll
+      for (int e = 0; e < kJoinAhead; ++e) {
+        if (i0 + e >= end) break;
+        const float f = __builtin_amdgcn_exp2f(w[e] - ref);
+        l = fmaf(f, lw[e], l);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          x[c] = fmaf(f, u[e][c], x[c]);
+          y[c] = fmaf(f, v[e][c], y[c]);
         }
       }
     }
+    if (parts > 1) {
+      *reinterpret_cast<f32x4*>(&part_x[group][col]) = x;
+      *reinterpret_cast<f32x4*>(&part_x[group][col + 4]) = y;
+      if (sub == 0) part_l[group] = l;
+      __syncthreads();
+      for (int g = group + held; part == 0 && g < RPB; g += held) {
+        l += part_l[g];
+        x += *reinterpret_cast<const f32x4*>(&part_x[g][col]);
+        y += *reinterpret_cast<const f32x4*>(&part_x[g][col + 4]);
+      }
+    }
+    if (!real || part > 0) continue;
+    const PackedRow pr = packed_row(it.row0 + r, a.group);
     const float inv = pr.query + (it.lk - it.lq) < 0 ? 0.0f : 1.0f / l;
     const int64_t token = it.q0 + pr.query;
     const int head = it.head * a.group + pr.head;
-    bf16x8 w;
+    bf16x8 o;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      w[e] = static_cast<bf16>(x[e] * inv);
-      w[4 + e] = static_cast<bf16>(y[e] * inv);
+      o[e] = static_cast<bf16>(x[e] * inv);
+      o[4 + e] = static_cast<bf16>(y[e] * inv);
     }
-    *reinterpret_cast<bf16x8*>(a.out + (token * a.heads + head) * D + col) = w;
+    *reinterpret_cast<bf16x8*>(a.out + (token * a.heads + head) * D + col) = o;
     if (col == 0) a.lse[static_cast<int64_t>(head) * a.tokens + token] = (m + __builtin_amdgcn_logf(l)) * kLn2;
   }
 }
@@ -769,9 +795,10 @@ hipError_t launch_paged_fwd(const PagedCall& c, int groups, void* ws, hipStream_
 }
 
 hipError_t launch_paged_join(const PagedCall& c, int groups, void* ws, hipStream_t s) {
-  const int d = c.cache.head_dim, blocks = kJoinBlocks;
+  const int d = c.cache.head_dim, group = c.heads / c.cache.kv_heads;
+  const int blocks = c.tokens * group <= static_cast<int64_t>(c.cache.nseq) * kFewRows ? 1 : kJoinBlocks;
   const JoinArgs a{reinterpret_cast<const float*>(static_cast<char*>(ws) + desc_bytes(groups)), static_cast<const PagedDesc*>(ws), blocks,
-                   c.heads, c.heads / c.cache.kv_heads, c.tokens, static_cast<bf16*>(c.out), c.lse};
+                   c.heads, group, c.tokens, static_cast<bf16*>(c.out), c.lse};
   if (d == 128)
     hipLaunchKernelGGL((paged_join_kernel<128>), dim3(groups * blocks), dim3(kThreads), 0, s, a);
   else
