@@ -50,7 +50,6 @@ SCHED = {
     "t2v_bwd_dkdv.hip": ["-mllvm", "-amdgpu-sched-strategy=iterative-ilp"],
     "t2v_bwd_dq.hip": ["-mllvm", "-amdgpu-sched-strategy=max-ilp"],
     "t2v_causal_fwd.hip": ["-mllvm", "-amdgpu-sched-strategy=max-ilp"],
-    "t2v_paged_fwd.hip": ["-mllvm", "-amdgpu-sched-strategy=max-ilp"],
 }
 
 

@@ -19,6 +19,9 @@ namespace {
 
 constexpr int kFewRows = 32, kManyRows = 128;
 constexpr float kNan = __builtin_nanf("");
+// Time of a position of few rows against one of many. Four mixtures of tokens and chunks at head_dim 128, of 0.8, 0.95, 1.1, 1.25, 1.4 and 1.6: in the mean
+// 3, 1, 7, 7, 14 and 23% slower than the best for each; five at 64, of 0.5, 0.65, 0.8, 0.95 and 1.1: 4, 6, 4, 1 and 2%.
+constexpr float kFewWeight = 0.95f;
 constexpr int kStage = 64;  // keys of an LDS stage of the kernel of 128 rows
 
 typedef __attribute__((address_space(4))) const int32_t const_i32;  // read with scalar loads
@@ -518,6 +521,14 @@ struct StageDma {
   }
 };
 
+// Stage of a piece that comes first, where `clock` keys of the share have been gone through: key k has its turn at clock k modulo the share's
+// keys (or the tile's, if it has fewer).
+T2V_DEV int first_stage(const Walk& w, const PagedPiece& p, unsigned clock) {
+  const unsigned n = p.n, begin = p.begin, period = w.length >> 8 < p.n ? static_cast<unsigned>(w.length >> 8) : n, at = clock % period;
+  const unsigned key = at + (begin <= at ? 0 : (begin - at + period - 1) / period * period);
+  return key < static_cast<unsigned>(p.end) ? static_cast<int>(key - begin) / kStage : 0;
+}
+
 // A tile of 128 packed rows, 32 to a wave; the workgroup stages 64 keys at a time for all of them, the next ones under the
 // products of these.
 template <int D, bool BIG>
@@ -528,6 +539,7 @@ T2V_DEV void many_pieces(Walk& w, bf16* lds) {
   auto sV = [&](int b) { return lds + (2 + b) * (kStage * D); };
   const int tid = threadIdx.x;
   const int wave = uniform(tid >> 6);
+  unsigned clock = 0;  // keys of the pieces so far, rounded up to stages
   for_pieces<D>(w, [&](int seq, const PagedSeq& s, const PagedTiles& t, int head, const PagedPiece& p) {
     const int lane = lane_again(), G = lane >> 5, l32 = lane & 31;
     const int row0 = p.tile * R + wave * 32;
@@ -544,50 +556,55 @@ T2V_DEV void many_pieces(Walk& w, bf16* lds) {
       const HeadPages pages = head_pages(a, seq, head, s.lk);
       const float scale = a.scale;
       const Dma dma(tid);
+      // The stages are gone through from `first` on and around, for a key to have its turn at the same time in all of a die's workgroups, whose
+      // pieces begin at other keys: what one reads from memory the others find in the die's L2 then.
+      const int first = first_stage(w, p, clock);
+      clock += ntiles * kStage;
+      auto key_at = [&](int j) { return p.begin + (first + j < ntiles ? first + j : first + j - ntiles) * kStage; };
       int ids[Dma::NB];
-      dma.find(ids, pages, p.begin);
-      dma.copy(sK(0), sV(0), pages, ids, p.begin);
-      if (ntiles > 1) dma.find(ids, pages, p.begin + kStage);
+      dma.find(ids, pages, key_at(0));
+      dma.copy(sK(0), sV(0), pages, ids, key_at(0));
+      if (ntiles > 1) dma.find(ids, pages, key_at(1));
       bf16x8 qop[KK];
       load_queries(a, a.q + me.token * a.q_stride + static_cast<int64_t>(me.head) * D, me.ok, G, qop, KK);
       const uint32_t ko = opnd_lane_off<D>(lane);
       const uint32_t vo0 = rows_lane_off<D>(lane, 0), vo1 = rows_lane_off<D>(lane, 1);
       wait_vmcnt0();
       __syncthreads();
-      auto prefetch = [&](int tt) {
-        if (tt + 1 < ntiles) {
-          const int key0 = p.begin + (tt + 1) * kStage;
-          dma.copy(sK((tt & 1) ^ 1), sV((tt & 1) ^ 1), pages, ids, key0);
-          if (tt + 2 < ntiles) dma.find(ids, pages, key0 + kStage);
+      auto prefetch = [&](int j) {
+        if (j + 1 < ntiles) {
+          dma.copy(sK((j & 1) ^ 1), sV((j & 1) ^ 1), pages, ids, key_at(j + 1));
+          if (j + 2 < ntiles) dma.find(ids, pages, key_at(j + 2));
         }
       };
-      // Stages that all rows of this wave see whole, then the others: every wave passes ntiles barriers.
-      const int nfull = wave_active ? min(max(lim_lo + 1 - p.begin, 0) / kStage, ntiles) : 0;
-      int tt = 0;
-      for (; tt < nfull; ++tt) {
-        const int b = tt & 1;
-        prefetch(tt);
-        const uint32_t kbase = lds_addr(sK(b)) + ko;
-        const uint32_t vb0 = lds_addr(sV(b)) + vo0, vb1 = lds_addr(sV(b)) + vo1;
-#pragma unroll
-        for (int kb = 0; kb < kStage; kb += 32)
-          fwd_step<D, false>(kbase, vb0, vb1, kb, 0, scale, qop, o, m_run, l_run, lane);
-        wait_vmcnt0();
-        __syncthreads();
-      }
-      for (; tt < ntiles; ++tt) {
-        const int b = tt & 1;
-        const int key0 = p.begin + tt * kStage;
-        prefetch(tt);
-        if (wave_active) {
+      // Stages that all rows of this wave see whole (before key `full`), and the others, the tile's last: every wave passes ntiles barriers.
+      const int full = wave_active ? p.begin + min(max(lim_lo + 1 - p.begin, 0) / kStage, ntiles) * kStage : p.begin;
+      for (int j = 0; j < ntiles;) {
+        for (; j < ntiles && key_at(j) < full; ++j) {
+          const int b = j & 1;
+          prefetch(j);
           const uint32_t kbase = lds_addr(sK(b)) + ko;
           const uint32_t vb0 = lds_addr(sV(b)) + vo0, vb1 = lds_addr(sV(b)) + vo1;
-#pragma unroll 1
-          for (int kb = 0; kb < kStage && key0 + kb <= lim_hi; kb += 32)
-            fwd_step<D, true>(kbase, vb0, vb1, kb, lim - key0 - kb, scale, qop, o, m_run, l_run, lane);
+#pragma unroll
+          for (int kb = 0; kb < kStage; kb += 32)
+            fwd_step<D, false>(kbase, vb0, vb1, kb, 0, scale, qop, o, m_run, l_run, lane);
+          wait_vmcnt0();
+          __syncthreads();
         }
-        wait_vmcnt0();
-        __syncthreads();
+        for (; j < ntiles && key_at(j) >= full; ++j) {
+          const int b = j & 1;
+          const int key0 = key_at(j);
+          prefetch(j);
+          if (wave_active) {
+            const uint32_t kbase = lds_addr(sK(b)) + ko;
+            const uint32_t vb0 = lds_addr(sV(b)) + vo0, vb1 = lds_addr(sV(b)) + vo1;
+#pragma unroll 1
+            for (int kb = 0; kb < kStage && key0 + kb <= lim_hi; kb += 32)
+              fwd_step<D, true>(kbase, vb0, vb1, kb, lim - key0 - kb, scale, qop, o, m_run, l_run, lane);
+          }
+          wait_vmcnt0();
+          __syncthreads();
+        }
       }
     }
     if (wave_active) {
@@ -773,7 +790,7 @@ hipError_t launch_paged_fwd(const PagedCall& c, int groups, void* ws, hipStream_
   a.c.room = g.width * g.page_size;
   a.few = paged_rule(group, kFewRows, 128, 128, 256, paged_least_share(), kPagedFew, kFewRows);
   a.many = paged_rule(group, kManyRows, kStage, 128, 256, paged_least_share(), kPagedMany, kFewRows);
-  a.weight = g.head_dim == 64 ? 0.8f : 1.1f;
+  a.weight = kFewWeight;
   a.nseq = g.nseq;
   a.heads = c.heads;
   a.kv_heads = g.kv_heads;
