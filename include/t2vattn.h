@@ -1,8 +1,9 @@
 /*
  * libt2vattn: bidirectional multi-head self-attention, forward and backward,
  * over packed variable-length token sequences, for AMD MI355X (gfx950); and causal
- * attention with grouped heads over such sequences (t2v_causal_fwd, t2v_causal_bwd)
- * with rotary positions for its queries and keys (t2v_rotary), described where they are declared.
+ * attention with grouped heads over such sequences (t2v_causal_fwd, t2v_causal_bwd) or over a paged
+ * cache of their keys and values (t2v_paged_fwd, t2v_paged_append, t2v_page_copy), with rotary positions (t2v_rotary)
+ * and norms (t2v_norm_rotary, t2v_norm_rotary_bwd) for its queries and keys, described where they are declared.
  *
  * The operation (paper Section III, Observation 2): every clip is one sequence
  * of 3D latent patches, and each token attends to every token of its own clip
@@ -66,7 +67,8 @@
  * workspace, which a second kernel joins in order. The 256- and 128-row shapes of the forward and dQ kernels give
  * bitwise-equal results where nothing is cut; the forward form for at most 32 rows and the two dK/dV forms at head_dim 128
  * agree with the others to rounding. The shape follows from all sequences of a call, so a sequence's last bits may
- * depend on which others it is packed with.
+ * depend on which others it is packed with. Calls on a paged cache read their offsets, lengths and tables on the GPU: they use
+ * neither work lists nor the cache of them, and their kernels divide the work themselves.
  *
  * Environment. T2V_ORDER=natural schedules tiles in pack order instead of longest clip
  * first (for ablations); T2V_QTILE=wide or narrow forces the forward / dQ tile shape,
@@ -75,7 +77,7 @@
  * forward and dK/dV kernels on a persistent grid (as many workgroups as the GPU holds at once,
  * each striding over the work list; bitwise-equal results, measured ~1% slower, so off by
  * default; causal kernels have no such form). T2V_ORDER, T2V_QTILE, T2V_KVTILE and T2V_SPLIT apply to causal calls
- * too. T2V_LOG=1 prints one
+ * too, and not to those on a paged cache. T2V_LOG=1 prints one
  * line to stderr per new work list: its items, the host's predicted list-scheduling
  * makespan and its lower bound, and the loop split if any. T2V_TEST_FAIL_ALLOC=1 makes
  * building a new work list fail with T2V_ERR_OOM, for testing that path.
@@ -101,7 +103,8 @@
  * t2v_last_error() names the work item, or the kernel, workgroup and row. Calls into it are
  * serialised. T2V_CHECK_CANARY=n takes n rows off every bound the kernels check, so correct
  * kernels report their clips' last rows: a way to see that the checks report. Its results
- * equal the unchecked library's bitwise. (t2v_rotary copies no rows into LDS and is the same in both.)
+ * equal the unchecked library's bitwise. (t2v_rotary, t2v_norm_rotary, its backward, t2v_paged_append and t2v_page_copy copy no rows into LDS and
+ * are the same in both; t2v_paged_fwd checks the keys that it copies against their sequence.)
  */
 #ifndef T2VATTN_H
 #define T2VATTN_H
@@ -289,7 +292,7 @@ int t2v_rotary(const void* q, const void* k, int64_t q_stride, int64_t k_stride,
 /* Norms of the heads of q and k, and rotary positions after them, in one pass:
  *   n = w x / sqrt(mean(x^2) + eps)   over the head_dim elements x of a token's head, w the weights of its tensor;
  *   the first 2 n_pairs dimensions of n are then turned and multiplied by mscale as in t2v_rotary, the others are n's.
- * All in 32 bits, rounded once. */
+ * All in 32 bits, rounded once: the sum of squares of a head whose elements pass 2^60 overflows, and gives zeros. */
 typedef struct {
   const int32_t* positions;   /* the turn: as t2v_rotary's arguments; n_sections 0: none (the other five are not read) */
   const double* freqs;
@@ -352,7 +355,8 @@ typedef struct {
  *   ws, need     as in t2v_causal_fwd; need follows from the sizes given here, not from lengths: at most 72 MiB
  * The arrays in device memory cannot be checked before the launch. Whatever they hold, nothing outside the tensors is read or written,
  * and what cannot be right shows: keys in a page outside the cache count as NaN for the queries that see them, a
- * sequence longer than its row of the table gets NaN results. Offsets that decrease give unspecified results. tokens * heads / kv_heads must stay below 2^31.
+ * sequence longer than its row of the table gets NaN results. Offsets that decrease give unspecified results. tokens * heads / kv_heads must stay below 2^31,
+ * and 256 kv_heads (tokens heads / (32 kv_heads) + nseq) (width page_size + 4096 + tokens) below 2^52 (the largest possible work).
  * Deterministic, no atomics: how the work is divided follows from offsets, lengths and sizes; a
  * sequence's last bits may depend on the others in the call. T2V_SPLIT and the other settings have no effect here. */
 int t2v_paged_fwd(const void* q, int64_t q_stride, int heads, const int32_t* cu_seqlens, int64_t tokens, const t2v_pages* cache,
@@ -440,7 +444,7 @@ int t2v_plan_cascades(int n_cascades, const int32_t* pred_ptr, const int32_t* pr
  * events, returns the summed elapsed milliseconds and the launch count of each kernel since
  * the previous read (slots: 0 forward, 1 backward Delta, 2 backward dK/dV, 3 backward dQ; the
  * one-pass backward with its reduce counts as 2, once per batch of heads; causal kernels with their
- * joins count alike, rotary launches are not timed),
+ * joins count alike, and attention over a paged cache with its join as 0; rotary, norm, append and page copy launches are not timed),
  * and forgets them. Enabling or disabling also forgets. Calls overlapping with launches on
  * other host threads are serialised by a mutex.
  *   ms_out     host double[4];  counts_out host int[4] */
@@ -450,7 +454,7 @@ int t2v_kernel_times(double* ms_out, int* counts_out);
 /* Per-workgroup trace, for measurement: the single-GPU analogue of the per-rank balance
  * metric of the case study (Section V-E), i.e. per-CU busy time and its coefficient of
  * variation. While armed, every forward, dK/dV and dQ kernel launch takes the next n_items
- * records of dev_records, one per workgroup in work-list order, each four uint64:
+ * records of dev_records, one per workgroup in work-list order (paged: in the order of their numbers), each four uint64:
  * {CU id, start, end, kernel slot}; CU id = (XCC_ID << 16) | bits 8..15 of HW_ID, start
  * and end on the constant 100 MHz device clock, slot 0 forward, 2 dK/dV or one-pass, 3 dQ. A launch
  * whose records do not fit runs untraced and is counted as overflowed. Tracing does not

@@ -1,5 +1,6 @@
 """libt2vattn: packed variable-length attention (bidirectional, and causal with grouped heads; forward and
-backward) and rotary positions for AMD MI355X (gfx950), behind a C ABI (include/t2vattn.h).
+backward), causal attention over a paged cache of keys and values, norms and rotary positions for AMD MI355X (gfx950), behind a C ABI
+(include/t2vattn.h).
 
 The binding below only marshals arguments; all computation is in the HIP library.
 """

@@ -12,8 +12,7 @@
 // Sequences with at most `few` packed rows (single tokens), whose loops wait for memory, and those with more, which keep the matrix cores busy,
 // are two lines with tiles and costs of their own. The workgroups are dealt to them by their work, so that a CU has some of both.
 //
-// Nothing here divides 64-bit numbers, which would take the GPU
-// longer than a short loop: a quotient is estimated in 32 bits and put right.
+// Nothing here divides 64-bit numbers, which would take the GPU longer than a short loop: a quotient is estimated in 32 bits and put right.
 #pragma once
 
 #include <cstdint>

@@ -6,6 +6,16 @@
 // by the kernels themselves (t2v_paged.h): each of a fixed number of workgroups takes an even share of all loops.
 //
 // A page number outside the cache is replaced by a row of NaN, so that it shows in the queries that see it and nothing is read.
+//
+// What bounds it. Few rows (single tokens): memory. 32 tokens over 31 to 20,280 keys, 40 heads over 8 of 128, 813 MB: 139 us, 5.8 TB/s; a
+// token over 100,000 keys, 24 heads over 8: 70 us; both and the join's 5. Copies to LDS reach 6.0 TB/s, and 6.6 marked as not to be kept (nt), which each
+// key is here: without the mark 17 and 10 us more. One token over 1,280 keys takes 9 us, a chain of dependent reads (offsets, page numbers, keys).
+// Many rows (chunks, prompts): the matrix cores. 768, 257 and 512 queries over 20,280, 4,097 and 9,999 keys, 12 heads over 4 of 128: 136 us, 970
+// TFLOP/s, and 11 for the join of 42 MB of partial sums; a prompt of 6,912 tokens, 24 heads over 8, 338 us in all, where the kernel of whole offsets on
+// the host (t2v_causal_fwd.hip), which deals tiles longest first and cuts fewer, takes 320; of 20,280 tokens 2,445 against 2,175, as
+// there the workgroups of a die read other parts of more keys than its L2 holds.
+// Mixtures run both at once, two workgroups a CU at head_dim 128 and three at 64, as many as registers and LDS let: 30 tokens beside chunks
+// of 512 and 300, 804 MB: 146 us (as two launches, one after the other, 202).
 #include <algorithm>
 
 #include "t2v_causal_fwd_step.hpp"
@@ -661,9 +671,9 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void paged_fwd_kernel(const P
 // ------------------------------------------------------------------ join
 
 // Workgroups of a cut tile of many rows, in calls whose sequences have more than 32 packed rows each in the mean; else one, as most
-// tiles have few.
+// tiles have few: 32 tokens 6.3 us with four, 4.7 with one; the chunks above 29 with one, 11 with four, 10 with eight.
 constexpr int kJoinBlocks = 4;
-constexpr int kJoinAhead = 4;  // pieces of a row in flight
+constexpr int kJoinAhead = 4;  // pieces of a row in flight (a token over 100,000 keys: 5.6 us; one after the other, by 16 lanes, 24; eight: 5.2, mixtures 10 for 7)
 
 struct JoinArgs {
   const float* partial;
@@ -788,6 +798,9 @@ hipError_t launch_paged_fwd(const PagedCall& c, int groups, void* ws, hipStream_
   a.c.pages = static_cast<int>(g.pages);
   a.c.shift = __builtin_ctz(g.page_size);
   a.c.room = g.width * g.page_size;
+  // Cuts are at multiples of the four waves' steps, or of a stage. A tile's fixed part is 256 keys: with 64, 32 tokens over 31 to 20,280 keys take 159 us
+  // for 153 (graphs replayed), with 1,024 158, and 60 beside a chunk of 700, 30 heads of 64 over 10, 168 for 160. Shares have 128 keys at least: with 512, 64
+  // tokens over 300 take 26 us for 23, and longer ones as long.
   a.few = paged_rule(group, kFewRows, 128, 128, 256, paged_least_share(), kPagedFew, kFewRows);
   a.many = paged_rule(group, kManyRows, kStage, 128, 256, paged_least_share(), kPagedMany, kFewRows);
   a.weight = kFewWeight;
