@@ -1,8 +1,8 @@
 // Work of attention over a paged cache, divided on the GPU: what host and device code share (no HIP needed).
 //
 // Offsets, lengths and page tables are in device memory, so that a captured call follows them as they grow. A launch has a fixed number
-// of workgroups. Each works out the costs of all sequences by itself and takes an even share of their sum: positions
-// share * length .. on one line on which every tile of packed rows (query, head of the group) of every key head has an interval,
+// of workgroups. Each works out the costs of all sequences by itself and takes an even share of their sum: an interval
+// of one line on which every tile of packed rows (query, head of the group) of every key head has an interval,
 // sequence by sequence, key head by key head. A position is 1 / 256 of a key. Sequence s has `rows` packed rows in tiles of `tile`; the
 // interval of tile t is as long as a fixed part, the keys before the sequence's queries, and t + 1 tiles' queries, which is (but for
 // rounding) its loop's length: an arithmetic series, so where a tile begins has a closed form. A boundary between two
@@ -135,20 +135,6 @@ T2V_HD int64_t paged_whole(const PagedRule& r, int64_t cost, int n) {
   return x < cost ? x : cost;
 }
 
-// Even shares of `total` for n workgroups: their length, so that share i takes positions i * length .. (i + 1) * length - 1. A little
-// more than even: total / n is off by less than 1.
-T2V_HD int64_t paged_share(const PagedRule& r, int64_t total, int n) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  double inverse = __builtin_amdgcn_rcpf(static_cast<float>(n));
-#else
-  double inverse = 1.0f / static_cast<float>(n);
-#endif
-  inverse *= 2.0 - n * inverse;  // 23 bits, 46, and what a double holds
-  inverse *= 2.0 - n * inverse;
-  const int64_t even = static_cast<int64_t>(static_cast<double>(total) * inverse) + 2, least = static_cast<int64_t>(r.share) * 256;
-  return even > least ? even : least;
-}
-
 // How many of `groups` workgroups take the line of many rows, `weight` being the time of a position of few rows against one of many: as their
 // share of the work, but each line that has any gets some. Dies (workgroup b runs on die b % 8) get as many each.
 T2V_HD bool paged_by_die(int groups) { return groups % 8 == 0 && groups >= 16; }
@@ -160,18 +146,44 @@ T2V_HD int paged_many(int groups, int64_t few, int64_t many, float weight) {
   n = n < 1 ? 1 : n > slots - 1 ? slots - 1 : n;
   return n * each;
 }
-// Workgroup b's line and share, n_many of `groups` being the line of many rows': a die's first ones, which begin one to a CU, so that few CUs have
-// two; shares of a die follow each other. (Dealt alternately, two of them met on a CU where their distance divided a die's CUs: 60 tokens beside a
-// chunk of 200, 40 heads over 8: 290 us against 229; the die's last ones: 249.)
+// Workgroup b's line and its place among those of its die (x) that take it, n_many of `groups` being the line of many rows': a die's first ones, which
+// begin one to a CU, so that few CUs have two. (Dealt alternately, two of them met on a CU where their distance divided a die's CUs: 60
+// tokens beside a chunk of 200, 40 heads over 8: 290 us against 229; the die's last ones: 249.)
 struct PagedRole {
   bool many;
-  int share;
+  int x, i;
 };
 T2V_HD PagedRole paged_role(int b, int groups, int n_many) {
   const bool dies = paged_by_die(groups);
-  const int x = dies ? b % 8 : 0, i = dies ? b / 8 : b, per = dies ? groups / 8 : groups, m = dies ? n_many / 8 : n_many;
-  const bool many = i < m;
-  return {many, many ? x * m + i : x * (per - m) + i - m};
+  const int x = dies ? b % 8 : 0, i = dies ? b / 8 : b, m = dies ? n_many / 8 : n_many;
+  return {i < m, x, i < m ? i : i - m};
+}
+
+// Shares of a line, `each` for each of the dies, one after the other; share i takes positions i * length .. (i + 1) * length - 1.
+struct PagedShares {
+  int dies, each;
+  int64_t length;
+};
+// Even shares of `total` for the n workgroups of `groups` that take the line, a little more than even (total / n is off by less than 1), but none shorter
+// than the rule's: where that leaves workgroups without one, every die has as many (a token over 2,000 keys, 24 heads over 8, in a
+// table for 64,000: 14 us; on the first two dies 17).
+T2V_HD PagedShares paged_shares(const PagedRule& r, int64_t total, int n, int groups) {
+  PagedShares s;
+  s.dies = paged_by_die(groups) ? 8 : 1;
+  s.each = n / s.dies;
+  const int64_t least = static_cast<int64_t>(r.share) * 256, keys = total / 256 / s.dies + 1;  // keys: of a die
+  if (keys < static_cast<int64_t>(s.each) * r.share) s.each = static_cast<int>((static_cast<unsigned>(keys) + r.share - 1) / static_cast<unsigned>(r.share));
+  const int shares = s.dies * s.each;
+#if defined(__HIP_DEVICE_COMPILE__)
+  double inverse = __builtin_amdgcn_rcpf(static_cast<float>(shares));
+#else
+  double inverse = 1.0f / static_cast<float>(shares);
+#endif
+  inverse *= 2.0 - shares * inverse;  // 23 bits, 46, and what a double holds
+  inverse *= 2.0 - shares * inverse;
+  s.length = static_cast<int64_t>(static_cast<double>(total) * inverse) + 2;
+  if (s.length < least) s.length = least;
+  return s;
 }
 
 // A loop, or a piece of one: keys begin .. end - 1 of a tile of n keys. slot >= 0: a piece, whose partial results go there.

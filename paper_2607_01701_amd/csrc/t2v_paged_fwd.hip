@@ -125,6 +125,7 @@ struct Walk {
   bool many;
   int share, shares, n_few, head, seq;
   int64_t at, from, to, length;
+  int period;  // keys of a share, 2^31 - 1 at most
 };
 
 // Each wave works it out by itself: costs of 64 sequences at a time, their sums over the lanes, and a search. (Offsets or lengths that
@@ -152,16 +153,17 @@ T2V_DEV Walk find_share(const PagedArgs& a, int lane) {
   }
   const int groups = gridDim.x, n_many = uniform(paged_many(groups, sum[0], sum[1], a.weight));
   const PagedRole role = paged_role(blockIdx.x, groups, n_many);
-  const int shares = role.many ? n_many : groups - n_many;
   const int64_t total = role.many ? paged_line(sum[1], sum[0]) : paged_line(sum[0], sum[1]);
   Walk w;
   w.many = role.many;
-  w.share = role.share;
-  w.shares = shares;
   w.n_few = groups - n_many;
-  w.length = paged_share(role.many ? a.many : a.few, total, shares);
+  const PagedShares shares = paged_shares(role.many ? a.many : a.few, total, role.many ? n_many : groups - n_many, groups);
+  w.share = role.x * shares.each + role.i;
+  w.shares = shares.dies * shares.each;
+  w.length = shares.length;
+  w.period = static_cast<int>(min(shares.length, (static_cast<int64_t>(1) << 39) - 1) >> 8);
   w.from = w.share * w.length;
-  w.to = min(total, w.from + w.length);
+  w.to = role.i < shares.each ? min(total, w.from + w.length) : w.from;
   w.head = w.seq = 0;
   w.at = 0;
   if (w.from >= w.to) return w;
@@ -534,7 +536,7 @@ struct StageDma {
 // Stage of a piece that comes first, where `clock` keys of the share have been gone through: key k has its turn at clock k modulo the share's
 // keys (or the tile's, if it has fewer).
 T2V_DEV int first_stage(const Walk& w, const PagedPiece& p, unsigned clock) {
-  const unsigned n = p.n, begin = p.begin, period = w.length >> 8 < p.n ? static_cast<unsigned>(w.length >> 8) : n, at = clock % period;
+  const unsigned begin = p.begin, period = min(w.period, p.n), at = clock % period;
   const unsigned key = at + (begin <= at ? 0 : (begin - at + period - 1) / period * period);
   return key < static_cast<unsigned>(p.end) ? static_cast<int>(key - begin) / kStage : 0;
 }

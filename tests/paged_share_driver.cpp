@@ -26,7 +26,7 @@ static void quotients() {
   }
 }
 
-// Every workgroup has one share of one line, and neighbouring shares of a die are neighbours on the line.
+// Every workgroup has one place on one line; a line's shares cover it, and none is too short.
 static void roles() {
   std::mt19937 g(7);
   for (int n = 0; n < 3000; ++n) {
@@ -34,21 +34,22 @@ static void roles() {
     const int64_t few = g() % 5 ? g() : 0, many = g() % 5 ? g() : 0;
     const int m = paged_many(groups, few, many, 0.5f + (g() % 8) * 0.25f);
     if (m < 0 || m > groups || (many && !m) || (few && m == groups) || (!many && m)) fail("roles", n);
-    std::vector<int> seen[2] = {std::vector<int>(groups - m, 0), std::vector<int>(m, 0)};
-    int last[2][8];
-    for (auto& x : last)
-      for (int& y : x) y = -1;
+    std::vector<std::vector<int>> seen[2];
+    for (auto& x : seen) x.assign(8, std::vector<int>(groups, 0));
     for (int b = 0; b < groups; ++b) {
       const PagedRole r = paged_role(b, groups, m);
-      if (r.share < 0 || r.share >= static_cast<int>(seen[r.many].size()) || seen[r.many][r.share]++) fail("a share of no or two workgroups", n);
-      int& before = last[r.many][paged_by_die(groups) ? b % 8 : 0];
-      if (before >= 0 && r.share != before + 1) fail("shares of a die apart", n);
-      before = r.share;
+      const int dies = paged_by_die(groups) ? 8 : 1, each = (r.many ? m : groups - m) / dies;
+      if (r.x < 0 || r.x >= dies || r.i < 0 || r.i >= each || seen[r.many][r.x][r.i]++) fail("a place of no or two workgroups", n);
+      if (dies == 8 && r.x != b % 8) fail("a place on another die", n);
     }
     const int64_t total = (int64_t(1) << (g() % 52)) + g();
-    PagedRule rule = paged_rule(1, 32, 128, 128, 1, 1, kPagedFew, 32);
-    const int64_t length = paged_share(rule, total, groups);
-    if (length * groups < total || length > total / groups + 256) fail("a share's length", n);
+    const PagedRule rule = paged_rule(1, 32, 128, 128, 1, 1 + g() % 300, kPagedFew, 32);
+    const int taken = m ? m : groups;
+    const PagedShares s = paged_shares(rule, total, taken, groups);
+    const int64_t count = int64_t(s.dies) * s.each, least = int64_t(rule.share) * 256;
+    if (s.each < 1 || count > taken || s.length * count < total || s.length < least) fail("shares of a line", n);
+    if (s.length > std::max(least, total / count + 256)) fail("a share's length", n);
+    if (count < taken && s.length > least + total / count / rule.share) fail("workgroups without a share", n);
   }
 }
 
@@ -67,8 +68,9 @@ static void long_lines() {
       }
       for (int i = 0; i < 2; ++i) sum[i] = paged_add(sum[i], more[i]);
     }
-    const int64_t total = paged_line(sum[1], sum[0]), length = paged_share(many, total, 512);
-    if (total < 0 || total > kPagedMost || (total == 0) != ((nseq + 1) / 2 >= 16) || length * 512 < total) fail("a line's length", nseq);
+    const int64_t total = paged_line(sum[1], sum[0]);
+    const PagedShares shares = paged_shares(many, total, 512, 512);
+    if (total < 0 || total > kPagedMost || (total == 0) != ((nseq + 1) / 2 >= 16) || 512 * shares.length < total) fail("a line's length", nseq);
     if (paged_line(sum[0], sum[1]) != 0) fail("work on an empty line", nseq);
   }
 }
@@ -113,10 +115,12 @@ int main() {
           if (paged_before(r, t, i + 1) <= paged_before(r, t, i)) fail("a tile without an interval", n);
         }
     }
-    const int64_t total = per_head * kv, length = paged_share(r, total, shares);
-    if (length * shares < total) fail("shares too short", n);
+    const int64_t total = per_head * kv;
+    const PagedShares line = paged_shares(r, total, shares, shares);
+    const int64_t length = line.length;
+    if (line.dies * line.each * length < total) fail("shares too short", n);
     std::vector<char> slots(2 * shares, 0);
-    for (int i = 0; i < shares; ++i) {
+    for (int i = 0; i < line.dies * line.each; ++i) {
       int64_t from = i * length;
       const int64_t to = std::min(total, (i + 1) * length);
       int64_t at = 0;
