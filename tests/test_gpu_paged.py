@@ -64,6 +64,16 @@ def test_values(H, Hk, D, page, queries, keys, heads_first):
     check(c, *paged_attn_fwd(c.q, c.pages, c.cu, c.scale), ref)
 
 
+@pytest.mark.parametrize("H,Hk,D,page,queries,keys", [
+    (3, 1, 128, 64, [1], [20000]), (1, 1, 64, 16, [1], [9000]), (32, 1, 128, 64, [1], [9000]), (5, 1, 64, 64, [3], [12000]),  # tiles of many pieces
+    (24, 8, 128, 64, [1], [300]), (8, 2, 64, 16, [1] * 3, [129, 500, 40]), (12, 4, 128, 64, [64], [500]), (6, 2, 128, 32, [1, 40], [700, 300]),
+])
+def test_wide_tables_and_many_pieces(H, Hk, D, page, queries, keys):
+    log(f"case {H} {Hk} {D} {page} {queries} {keys}")
+    c = Case(H, Hk, D, page, queries, keys, width=3000)  # room for far more than there is: few workgroups get a share
+    check(c, *paged_attn_fwd(c.q, c.pages, c.cu, c.scale))
+
+
 def test_many_sequences():
     log("case many sequences")
     r = np.random.default_rng(0)
