@@ -37,7 +37,11 @@ class PageTable:
         return s
 
     def _rows(self, sequences, tokens):
-        rows, more = np.atleast_1d(np.asarray(sequences, dtype=np.int64)), np.asarray(tokens, dtype=np.int64)
+        rows, more = np.atleast_1d(np.asarray(sequences)), np.asarray(tokens)
+        for x in (rows, more):
+            if x.size and (x.dtype.kind not in "iu" or x.max() >= 2 ** 31):
+                raise ValueError("sequences and tokens must be whole numbers below 2^31")
+        rows, more = rows.astype(np.int64), more.astype(np.int64)
         more = np.broadcast_to(more, rows.shape)
         if rows.ndim != 1 or np.unique(rows).size != rows.size:
             raise ValueError("sequences must be a list of different numbers")

@@ -149,12 +149,20 @@ def paged_append(k, v, pages: Pages, cu_seqlens, q=None, positions=None, freqs=N
     return q_out
 
 
+def _numbers(x):
+    """Page numbers as a contiguous int32 array."""
+    x = np.asarray(x)
+    if x.dtype != np.int32 and x.size and (x.dtype.kind not in "iu" or x.min() < -2 ** 31 or x.max() >= 2 ** 31):
+        raise ValueError(f"src and dst must be page numbers, got {x.dtype} of another kind or range")
+    return np.ascontiguousarray(x, dtype=np.int32)
+
+
 def page_copy(buffers, src, dst, stream=None):
     """Copies pages src[i] to pages dst[i] in every one of `buffers`: a tensor [pages, ...] on the GPU or a sequence of them, of one shape and
     strides, each page's memory dense. src, dst: host int32 arrays; no page may be written twice, nor both read and written."""
     import torch
     buffers = (buffers,) if isinstance(buffers, torch.Tensor) else tuple(buffers)
-    src, dst = (np.ascontiguousarray(x, dtype=np.int32) for x in (src, dst))
+    src, dst = _numbers(src), _numbers(dst)
     if src.ndim != 1 or src.shape != dst.shape:
         raise ValueError("src and dst must be 1-D arrays of one length")
     if not buffers:

@@ -114,7 +114,9 @@ def test_forks_share_full_pages_and_copy_the_begun_one():
 @pytest.mark.parametrize("do,err,msg", [
     (lambda t: t.extend([0, 0], [1, 1]), ValueError, "different"), (lambda t: t.extend([3], [1]), ValueError, "not in use"),
     (lambda t: t.extend([9], [1]), ValueError, "not in use"), (lambda t: t.extend([-1], [1]), ValueError, "not in use"),
-    (lambda t: t.extend([0], [-1]), ValueError, ">= 0"), (lambda t: t.extend([0], [1000]), RuntimeError, "passes its"),
+    (lambda t: t.extend([0], [-1]), ValueError, ">= 0"), (lambda t: t.extend([0], [1.5]), ValueError, "whole"),
+    (lambda t: t.extend([0.0], [1]), ValueError, "whole"), (lambda t: t.extend([0], [2 ** 31]), ValueError, "whole"),
+    (lambda t: t.extend([0], [1000]), RuntimeError, "passes its"),
     (lambda t: t.extend([0], [90]), RuntimeError, "pages are needed"), (lambda t: t.grown([0], [16]), ValueError, "reserved"),
     (lambda t: t.fork(2), ValueError, "not in use"), (lambda t: t.free(2), ValueError, "not in use"),
     (lambda t: t.truncate(0, 9), ValueError, "tokens"), (lambda t: PageTable(4, 24, 1, 1), ValueError, "power of two"),
@@ -266,6 +268,14 @@ def test_page_copy_of_nothing():
 
 def _t(*shape, dtype=torch.bfloat16):
     return torch.zeros(shape, dtype=dtype)
+
+
+@pytest.mark.parametrize("kw", [{"src": np.array([2 ** 32])}, {"dst": [1.0]}, {"src": [True]}, {"dst": np.array([-2 ** 31 - 1])}])
+def test_page_copy_takes_no_other_numbers(kw):
+    a = dict(src=[1], dst=[2])
+    a.update(kw)
+    with pytest.raises(ValueError, match="page numbers"):
+        t2v.page_copy(_t(4, 16, 8), a["src"], a["dst"])
 
 
 @pytest.mark.parametrize("kw,msg", [
