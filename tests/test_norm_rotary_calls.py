@@ -11,6 +11,8 @@ import paper_2607_01701_amd as t2v
 from oracle import norm_rotary as oracle
 from paper_2607_01701_amd import _lib
 
+from test_autograd_calls import HOOKS, calls  # noqa: F401
+
 A, MB = 0x100000, 1 << 20
 INV, UNS, WS = _lib.T2V_ERR_INVALID_ARG, _lib.T2V_ERR_UNSUPPORTED, _lib.T2V_ERR_WORKSPACE
 
@@ -129,3 +131,58 @@ def test_autograd_refusals():
         t2v.norm_rotary_bwd(_t(9, 6, 64), None, _t(9, 6, 64), None, _t(9, dtype=torch.int32), np.ones(8), eps=None)
     with pytest.raises(ValueError, match="both be given"):
         t2v.norm_rotary_bwd(_t(9, 6, 64), None, None, None, _t(9, dtype=torch.int32), np.ones(8))
+
+
+# ------------------------------------------------------------------------ what autograd passes on
+
+
+def leaves():
+    w = torch.zeros(50, 8, 64, dtype=torch.bfloat16).requires_grad_(True)
+    return w, w[:, :6], w[:, 6:], *(torch.ones(64, dtype=torch.bfloat16).requires_grad_(True) for _ in range(2))
+
+
+def turned(q, k, wq, wk):
+    return t2v.norm_rotary(q, k, torch.zeros(50, dtype=torch.int32), np.ones(32), wq, wk)
+
+
+@pytest.mark.parametrize("hooks", HOOKS, ids=["none", "pack", "unpack"])
+def test_backward_describes_the_tensors_that_it_passes(calls, hooks):
+    """Saved-tensor hooks may give dense copies of slices; gradients may be spread out or start anywhere."""
+    w, q, k, wq, wk = leaves()
+    seen = {x.data_ptr(): x for x in (q, k)}
+
+    def unpacked(x):
+        y = hooks[1](x)
+        seen[y.data_ptr()] = y
+        return y
+
+    if hooks is None:
+        a, b = turned(q, k, wq, wk)
+    else:
+        with torch.autograd.graph.saved_tensors_hooks(hooks[0], unpacked):
+            a, b = turned(q, k, wq, wk)
+    da = torch.zeros(1, dtype=torch.bfloat16).expand(a.shape)
+    db = torch.zeros(b.numel() + 1, dtype=torch.bfloat16)[1:].view(b.shape)
+    torch.autograd.grad((a, b), (w, wq, wk), (da, db))
+    args = [x for n, x in calls.made if n == "t2v_norm_rotary_bwd"][-1]
+    for p, step in zip(args[0:2], args[2:4]):
+        assert step == seen[p].stride(0) and p % 16 == 0
+    assert all(p % 16 == 0 and p for p in args[4:6]) and args[6:8] == (6 * 64, 2 * 64)
+
+
+@pytest.mark.parametrize("eager,refused", [(0, True), (7, False), (None, False)], ids=["default stream", "side stream", "no eager graph"])
+def test_captured_backward_beside_an_eager_graph(calls, monkeypatch, eager, refused):
+    w, q, k, wq, wk = leaves()
+    current = [eager or 0]
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: current[0], raising=False)
+    alive = turned(q, k, wq, wk) if eager is not None else None
+    current[0] = 9
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    out = turned(q, k, wq, wk)
+    g = tuple(torch.zeros_like(x) for x in out)
+    if refused:
+        with pytest.raises(RuntimeError, match="default stream"):
+            torch.autograd.grad(out, (wq, wk), g)
+        del alive, out
+        out = turned(q, k, wq, wk)
+    torch.autograd.grad(out, (wq, wk), g)
