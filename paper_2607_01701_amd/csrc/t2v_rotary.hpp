@@ -32,10 +32,11 @@ T2V_DEV float2 angle_of(const RotaryAngles& a, int j, int p) {
   return make_float2(c, s);
 }
 
-// f radians in 2^-64 turns, modulo a turn. long double holds 64 bits of the quotient.
+// f radians in 2^-64 turns, modulo a turn. long double holds 64 bits of the quotient. (Usual frequencies are less than a turn: without floor, which takes
+// 0.1 us in long double, 64 pairs take 0.5 us for 6.9.)
 inline unsigned long long turn_of(double f) {
   const long double turns = static_cast<long double>(f) * 0.159154943091895335768883763372514362L;  // 1 / (2 pi)
-  const long double frac = turns - std::floor(turns);
+  const long double frac = turns >= 0.0L && turns < 1.0L ? turns : turns - std::floor(turns);
   const long double scaled = frac * 18446744073709551616.0L;
   return scaled >= 18446744073709551615.0L ? ~0ull : static_cast<unsigned long long>(scaled + 0.5L);
 }
