@@ -157,16 +157,8 @@ def _numbers(x):
     return np.ascontiguousarray(x, dtype=np.int32)
 
 
-def page_copy(buffers, src, dst, stream=None):
-    """Copies pages src[i] to pages dst[i] in every one of `buffers`: a tensor [pages, ...] on the GPU or a sequence of them, of one shape and
-    strides, each page's memory dense. src, dst: host int32 arrays; no page may be written twice, nor both read and written."""
-    import torch
-    buffers = (buffers,) if isinstance(buffers, torch.Tensor) else tuple(buffers)
-    src, dst = _numbers(src), _numbers(dst)
-    if src.ndim != 1 or src.shape != dst.shape:
-        raise ValueError("src and dst must be 1-D arrays of one length")
-    if not buffers:
-        return
+def _buffers(buffers):
+    """What t2v_page_copy takes of the buffers, checked: device, addresses, their number, pages, strides and sizes in bytes."""
     first = buffers[0]
     shape, strides, dtype, device = first.shape, first.stride(), first.dtype, first.device
     if len(shape) < 2 or 0 in shape[1:]:
@@ -183,9 +175,26 @@ def page_copy(buffers, src, dst, stream=None):
     if not first.is_cuda:
         raise ValueError("buffers must be CUDA tensors")
     ptrs = (ctypes.c_void_p * len(buffers))(*[b.data_ptr() for b in buffers])
+    return device, ptrs, len(buffers), shape[0], (strides[0] if shape[0] > 1 else rows) * item, rows * item
+
+
+def page_copy(buffers, src, dst, stream=None):
+    """Copies pages src[i] to pages dst[i] in every one of `buffers`: a tensor [pages, ...] on the GPU or a sequence of them, of one shape and
+    strides, each page's memory dense. src, dst: host int32 arrays; no page may be written twice, nor both read and written."""
+    import torch
+    buffers = (buffers,) if isinstance(buffers, torch.Tensor) else tuple(buffers)
+    src, dst = _numbers(src), _numbers(dst)
+    if src.ndim != 1 or src.shape != dst.shape:
+        raise ValueError("src and dst must be 1-D arrays of one length")
+    if buffers:
+        _copy(_buffers(buffers), src, dst, stream)
+
+
+def _copy(buffers, src, dst, stream=None):
+    device, *rest = buffers
     L = _lib.lib()
-    st = _lib._call_on(device, stream, L.t2v_page_copy, ptrs, len(buffers), shape[0], (strides[0] if shape[0] > 1 else rows) * item,
-                       rows * item, src.__array_interface__["data"][0], dst.__array_interface__["data"][0], src.shape[0])
+    st = _lib._call_on(device, stream, L.t2v_page_copy, *rest, src.__array_interface__["data"][0], dst.__array_interface__["data"][0],
+                       src.shape[0])
     if st != _lib.T2V_OK:
         _lib._check(L, st)
 
@@ -215,7 +224,7 @@ class PagedCache:
         self.table = torch.full(self.host.table.shape, -1, dtype=torch.int32, device=device)
         self.lengths = torch.zeros(sequences, dtype=torch.int32, device=device)
         self._layers = [Pages(x[0], x[1], self.table, self.lengths) for x in self.data]
-        self._buffers = [y for x in self.data for y in x]
+        self._buffers = _buffers([y for x in self.data for y in x]) if layers else None
         self._sent = self.host.table.copy()  # what the GPU's table holds
         self._width = 0  # columns of it that may hold pages
 
@@ -252,8 +261,8 @@ class PagedCache:
         return self.host
 
     def _sync(self, pairs=None, lengths=True):
-        if pairs is not None and pairs[0].size:
-            page_copy(self._buffers, *pairs)
+        if pairs is not None and pairs[0].size and self._buffers is not None:
+            _copy(self._buffers, *pairs)
         width = max(self._width, int(self.host.counts.max()))
         now, sent = self.host.table[:, :width], self._sent[:, :width]
         if not np.array_equal(now, sent):
