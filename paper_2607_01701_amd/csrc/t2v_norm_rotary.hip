@@ -7,10 +7,11 @@
 // (VIA_LDS). Sines and cosines are worked out once a token and shared by its heads through LDS, after the first loads.
 //
 // Bound by memory, each element being read and written once (backward: two read, one written): 116,904 tokens of 24 + 24 heads of 128
-// forward 476 us, 6.0 TB/s, backward 867 us, 5.0 TB/s; 20,280 tokens of 24 + 8 heads 57 us, 5.8 TB/s; through LDS (14,750 tokens of 30 + 10
+// forward 476 us, 6.0 TB/s, backward 819 us, 5.3 TB/s; 20,280 tokens of 24 + 8 heads 57 us, 5.8 TB/s; through LDS (14,750 tokens of 30 + 10
 // heads of 64, 36 dimensions turned) 37 and 50 us. Forward, many short workgroups with one row a lane in flight are fastest: with two rows
 // 514 us of the 490 that it takes without the marks of set_once, with 2 tokens a workgroup in place of 1 525, with 8 555. Backward, 512
-// workgroups that go through their tokens, which leaves few sums for the weights, lose nothing (512 to 32,768 of them: 846 to 870 us).
+// workgroups, which leave few sums for the weights, lose nothing (512 to 32,768 of them with tokens of their own: 846 to 870 us), and marks gain
+// nothing (860 to 889).
 #include <algorithm>
 #include <cmath>
 #include <string>
@@ -32,6 +33,7 @@ constexpr int kLeastRows128 = 48; // of a workgroup at head_dim 128, four times 
 constexpr int kRowsBack = 2;      // backward
 constexpr int kMaxAngles = 2048;  // of a workgroup's tokens (16 KB of LDS)
 constexpr int kMaxBackBlocks = 512;
+constexpr int kChunkBack = 8;     // tokens
 
 struct NormArgs {
   const bf16* in[2];    // q, k
@@ -297,17 +299,15 @@ __global__ __launch_bounds__(kThreads) void norm_rotary_kernel(const NormArgs a,
   }
 }
 
-// A workgroup takes `per_block` tokens, `chunk` at a time (their angles fill its table), q's heads and then k's, and
+// A workgroup takes `chunk` tokens at a time (their angles are in its table), every gridDim-th such chunk, q's heads and then k's, and
 // leaves its sums for the weights in partial[block].
 template <int D, bool INTERLEAVED, bool VIA_LDS>
-__global__ __launch_bounds__(kThreads) void norm_rotary_bwd_kernel(const NormArgs a, int per_block, int chunk) {
+__global__ __launch_bounds__(kThreads) void norm_rotary_bwd_kernel(const NormArgs a, int chunk) {
   using Lane = RowLane<D, INTERLEAVED, VIA_LDS>;
   constexpr int L = Lane::L, NG = kThreads / L;
   __shared__ __attribute__((aligned(16))) float2 cs[kMaxAngles];
   __shared__ __attribute__((aligned(16))) float wt[2][D];
   __shared__ float ex[VIA_LDS ? NG * (D + 4) : 1];
-  const int64_t first = static_cast<int64_t>(blockIdx.x) * per_block;
-  const int64_t last = min(first + per_block, a.tokens);
   const int sub = threadIdx.x % L, group = threadIdx.x / L;
   const Lane at(sub, a.pairs);
   float* buf = ex + (VIA_LDS ? group * (D + 4) : 0);
@@ -317,8 +317,8 @@ __global__ __launch_bounds__(kThreads) void norm_rotary_bwd_kernel(const NormArg
   for (int i = 0; i < 2; ++i)
 #pragma unroll
     for (int e = 0; e < kElems; ++e) dw[i][e] = 0.0f;
-  for (int64_t t0 = first; t0 < last; t0 += chunk) {
-    const int nt = static_cast<int>(min(static_cast<int64_t>(chunk), last - t0));
+  for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * chunk; t0 < a.tokens; t0 += static_cast<int64_t>(gridDim.x) * chunk) {
+    const int nt = static_cast<int>(min(static_cast<int64_t>(chunk), a.tokens - t0));
     __syncthreads();
     load_angles<D>(cs, a, t0, nt, -1.0f);
     __syncthreads();
@@ -759,7 +759,9 @@ int norm_rotary_bwd_impl(const void* q, const void* k, int64_t q_stride, int64_t
   const int64_t rows = kRowsBack * (kThreads * kElems / head_dim), least = (rows + heads + kv_heads - 1) / (heads + kv_heads);
   const int64_t each = std::max<int64_t>((tokens + kMaxBackBlocks - 1) / kMaxBackBlocks, std::min<int64_t>(least, (tokens + 255) / 256));
   const int blocks = tokens == 0 ? 0 : static_cast<int>((tokens + each - 1) / each);
-  const int chunk = static_cast<int>(std::min<int64_t>(each, 2 * kMaxAngles / head_dim));
+  // One chunk, if the table holds it; else short ones in turn, so that the workgroups go through memory side by side: 116,904 tokens of 24 + 24 heads 819 us, each
+  // through a part of its own 872; 60,000 of 30 + 10 heads of 64 182 and 194. (Chunks of 32: 855 and 191, of 5: 799 and 209.)
+  const int chunk = each <= 2 * kMaxAngles / head_dim ? static_cast<int>(each) : kChunkBack;
   const uint64_t bytes = weights ? static_cast<uint64_t>(blocks) * 2 * head_dim * sizeof(float) : 0;
   if (need != nullptr) *need = bytes;
   if (ws_bytes < bytes)
@@ -769,7 +771,7 @@ int norm_rotary_bwd_impl(const void* q, const void* k, int64_t q_stride, int64_t
   if (blocks > 0) {
     with_form(a, head_dim, interleaved, [&](auto d, auto il, auto lds) {
       hipLaunchKernelGGL((norm_rotary_bwd_kernel<decltype(d)::value, decltype(il)::value, decltype(lds)::value>), dim3(blocks),
-                         dim3(kThreads), 0, s, a, static_cast<int>(each), chunk);
+                         dim3(kThreads), 0, s, a, chunk);
     });
     if (int st = launched("norm and rotary backward kernel")) return st;
   }

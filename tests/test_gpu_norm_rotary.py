@@ -60,6 +60,12 @@ CASES = [  # tokens, H, Hk, D, sections, first position
 ]
 
 
+@pytest.mark.parametrize("T,H,Hk,D,sections,layout", [(16501, 2, 1, 128, (64,), "interleaved"), (33003, 1, 2, 64, (18,), "half"), (20483, 1, 1, 128, (30, 9), "half")])
+def test_many_tokens(T, H, Hk, D, sections, layout):
+    """More than the backward's workgroups go through at once."""
+    test_values_and_gradients(T, H, Hk, D, sections, 5, layout, torch.float32)
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32, None], ids=["bf16", "fp32", "none"])
 @pytest.mark.parametrize("layout", ["half", "interleaved"])
 @pytest.mark.parametrize("T,H,Hk,D,sections,start", CASES)
