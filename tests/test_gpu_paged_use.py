@@ -159,6 +159,16 @@ def test_page_copy_of_strided_pages_and_many_buffers():
     assert torch.equal(heads, ref)
 
 
+def test_page_copy_of_more_than_the_caches_hold():
+    log("case copy 290 MB")
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x = torch.randint(-2 ** 31, 2 ** 31 - 1, (2, 1700, 32771, 4), dtype=torch.int32, device="cuda", generator=g)[:, :, :8195]  # a part's end in a page, a gap between pages
+    ref = x.clone()
+    ref[:, 550:1100] = ref[:, 1100:1650] = ref[:, :550]
+    page_copy([x[0], x[1]], np.arange(1100) % 550, np.arange(550, 1650))
+    assert torch.equal(x, ref)
+
+
 def test_page_copy_beyond_32_bit_offsets():
     log("case copy large")
     x = torch.zeros(40_000, 64 * 8 * 128, dtype=torch.bfloat16, device="cuda")
