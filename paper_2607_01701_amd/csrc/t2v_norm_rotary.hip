@@ -654,7 +654,8 @@ int tokens_per_block(int64_t tokens, int heads, int head_dim) {
 
 // What the caches need not keep, by the bytes that a call writes (it reads as many) against the 256 MB that lie before the memory. Where both fit:
 // nothing (14,750 tokens, 75 MB: 36 us, 38 to 39 with either hint on reads). Where only the outputs fit: the inputs, so that the outputs wait there for the
-// attention (20,280 tokens, 24 + 8 heads, 166 MB: 57 us against 64; stored in pages, 210 MB: 78 against 90). Else both
+// attention (20,280 tokens, 24 + 8 heads, 166 MB: 57 us against 64; stored in pages, 210 MB: 77 against 90; with the outputs marked too
+// 84, or 81 for 90 where no call writes the memory of another). Else both
 // (116,904 tokens, 1.4 GB: 474 us against 490).
 void set_once(NormArgs* a, int64_t out_bytes) {
   constexpr int64_t kCache = 256 << 20;
