@@ -35,8 +35,9 @@ struct Nothing {
   T2V_DEV void operator()() const {}
 };
 
-// One 32-key step. MASK: this lane's row sees keys 0 .. lim of the step. c > 0. read(): called when all of the tiles' reads have been issued.
-template <int D, bool MASK, typename Read = Nothing>
+// One 32-key step. MASK: this lane's row sees keys 0 .. lim of the step. REST: what rounding P to bf16 for its product takes is multiplied too. c > 0.
+// read(): called when all of the tiles' reads have been issued.
+template <int D, bool MASK, bool REST = MASK, typename Read = Nothing>
 T2V_DEV void fwd_step(uint32_t kbase, uint32_t vbase0, uint32_t vbase1, int kb, int lim, float c,
                       const bf16x8 (&qop)[D / 16], f32x16 (&o)[D / 32], float& m_run, float& l_run, int lane,
                       Read&& read = Read()) {
@@ -87,7 +88,9 @@ T2V_DEV void fwd_step(uint32_t kbase, uint32_t vbase0, uint32_t vbase1, int kb, 
   l_run += sum16(s);
   // P in bf16 for its product; the row sum above took it in 32 bits. In masked steps, which hold all keys of a sequence's
   // first rows, the rest is multiplied too: those rows' few large weights make up half of a gradient's norm,
-  // and the steps are few (errors against 64 bits at 256 tokens, of their norm: out 2.3e-3 -> 1.9e-3).
+  // and the steps are few (errors against 64 bits at 256 tokens, of their norm: out 2.3e-3 -> 1.9e-3). So it is for single tokens over pages, whose
+  // kernel waits for memory (32 tokens over 31 to 20,280 keys: 140 us without it, 141 with it). Where the matrix cores are busy, half as many
+  // products again and the vector work beside them would take 232 us for 140 (three chunks over pages): there it is left out.
   const bf16x8 pb[2] = {to_bf16x8(s, 0), to_bf16x8(s, 8)};
   __builtin_amdgcn_s_setprio(kSoftmaxFirst<D> ? 0 : 1);
   const bool odd = MASK && (take_nonfinite(va[0]) | take_nonfinite(va[1]));
@@ -96,13 +99,19 @@ T2V_DEV void fwd_step(uint32_t kbase, uint32_t vbase0, uint32_t vbase1, int kb, 
 #pragma unroll
     for (int db = 0; db < DB; ++db) o[db] = mfma(va[hf][db], pb[hf], o[db]);
   if constexpr (!kSoftmaxFirst<D>) __builtin_amdgcn_s_setprio(0);
-  if constexpr (MASK) {
+  if constexpr (REST) {
+    if constexpr (!MASK) {  // infinities count with P, whose sign they keep, and not with the rest, which may be 0 or negative
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) take_nonfinite(va[hf]);
+    }
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
       const bf16x8 rest = rest_bf16x8(s, 8 * hf, pb[hf]);
 #pragma unroll
       for (int db = 0; db < DB; ++db) o[db] = mfma(va[hf][db], rest, o[db]);
     }
+  }
+  if constexpr (MASK) {
     if (odd)
       add_nonfinite(o, pb, G, [&](int half, int db) { return read_rows_opnd<D>(vbase0, vbase1, kb + half, db); },
                           [&](int kk, int) { return kk <= lim; });

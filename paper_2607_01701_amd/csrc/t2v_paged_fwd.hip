@@ -399,7 +399,7 @@ T2V_DEV void few_pieces(Walk& w, bf16* lds, float (&sM)[4][kFewRows], float (&sL
       };
       for (; n < nsteps && p.begin + n * 32 + 31 <= lim_lo; n += 4) {
         arrived();
-        fwd_step<D, false>(ko, vo0, vo1, 0, 0, scale, qop, o, m_run, l_run, lane, next);
+        fwd_step<D, false, true>(ko, vo0, vo1, 0, 0, scale, qop, o, m_run, l_run, lane, next);
       }
 #pragma unroll 1
       for (; n < nsteps; n += 4) {
