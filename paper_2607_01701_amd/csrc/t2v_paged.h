@@ -214,4 +214,8 @@ T2V_HD bool paged_piece(const PagedRule& r, const PagedSeq& s, const PagedTiles&
   return true;
 }
 
+// Workgroups that join a cut tile of `tile` rows, in a call of `rows` packed rows in all sequences: several, unless no tile can have more rows than one holds.
+// (What the call's sequences are is known on the GPU alone, and most of a cache's may have no queries: their number says nothing.)
+inline int paged_join_blocks(int64_t rows, int few, int several) { return rows <= few ? 1 : several; }
+
 }  // namespace t2v

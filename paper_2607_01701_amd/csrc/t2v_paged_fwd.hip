@@ -672,8 +672,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void paged_fwd_kernel(const P
 
 // ------------------------------------------------------------------ join
 
-// Workgroups of a cut tile of many rows, in calls whose sequences have more than 32 packed rows each in the mean; else one, as most
-// tiles have few: 32 tokens 6.3 us with four, 4.7 with one; the chunks above 29 with one, 11 with four, 10 with eight.
+// Workgroups of a cut tile, in calls that can have tiles of many rows; of a tile of few rows, all but one return at once. The chunks above: 20 us with one, 11
+// with four (10 with eight). 32 tokens take 5.1 us for the 4.8 with one; a chunk of 512 tokens, 24 heads over 8, 10.7 for 20.4.
 constexpr int kJoinBlocks = 4;
 constexpr int kJoinAhead = 4;  // pieces of a row in flight (a token over 100,000 keys: 5.6 us; one after the other, by 16 lanes, 24; eight: 5.2, mixtures 10 for 7)
 
@@ -828,7 +828,7 @@ hipError_t launch_paged_fwd(const PagedCall& c, int groups, void* ws, hipStream_
 
 hipError_t launch_paged_join(const PagedCall& c, int groups, void* ws, hipStream_t s) {
   const int d = c.cache.head_dim, group = c.heads / c.cache.kv_heads;
-  const int blocks = c.tokens * group <= static_cast<int64_t>(c.cache.nseq) * kFewRows ? 1 : kJoinBlocks;
+  const int blocks = paged_join_blocks(c.tokens * group, kFewRows, kJoinBlocks);
   const JoinArgs a{reinterpret_cast<const float*>(static_cast<char*>(ws) + desc_bytes(groups)), static_cast<const PagedDesc*>(ws), blocks,
                    c.heads, group, c.tokens, static_cast<bf16*>(c.out), c.lse};
   if (d == 128)

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2607_01701_amd import paged_attn_fwd
+from paper_2607_01701_amd import Pages, paged_attn_fwd
 
 from gpu_util import log
 from paged_util import Case
@@ -73,3 +73,20 @@ def test_infinities_that_a_token_sees(D):
     c.pages.v[p[7], r[7], 1, 3] = float("nan")
     out, _ = paged_attn_fwd(c.q, c.pages, c.cu, c.scale)
     assert out[0, 2:, 3].isnan().all() and int(out.isnan().sum()) == 2
+
+
+@pytest.mark.parametrize("H,Hk,D,queries,keys", [(24, 8, 128, [300], [2000]), (12, 4, 64, [200, 1, 40], [900, 1500, 40]), (8, 2, 128, [1, 1], [3000, 33])])
+def test_idle_sequences_change_nothing(H, Hk, D, queries, keys):
+    """A cache's other sequences, without queries, some with keys: the same bits as without them."""
+    log(f"case idle {H}/{Hk}x{D} {queries} over {keys}")
+    c = Case(H, Hk, D, 64, queries, keys)
+    ref = paged_attn_fwd(c.q, c.pages, c.cu, c.scale)
+    for n in (64, 256):
+        at = np.sort(np.random.default_rng(n).permutation(n)[:len(queries)])
+        table = torch.full((n, c.pages.table.shape[1]), -1, dtype=torch.int32, device="cuda")
+        lengths = torch.zeros(n, dtype=torch.int32, device="cuda")
+        lengths[::3] = 5
+        table[at], lengths[at] = c.pages.table, c.pages.lengths
+        cu = torch.from_numpy(np.concatenate([[0], np.cumsum(np.bincount(at, queries, n))]).astype(np.int32)).cuda()
+        got = paged_attn_fwd(c.q, Pages(c.pages.k, c.pages.v, table, lengths), cu, c.scale)
+        assert all(torch.equal(a, b) for a, b in zip(got, ref))
