@@ -292,7 +292,8 @@ int t2v_rotary(const void* q, const void* k, int64_t q_stride, int64_t k_stride,
 /* Norms of the heads of q and k, and rotary positions after them, in one pass:
  *   n = w x / sqrt(mean(x^2) + eps)   over the head_dim elements x of a token's head, w the weights of its tensor;
  *   the first 2 n_pairs dimensions of n are then turned and multiplied by mscale as in t2v_rotary, the others are n's.
- * All in 32 bits, rounded once: the sum of squares of a head whose elements pass 2^60 overflows, and gives zeros. */
+ * All in 32 bits, rounded once. Heads whose squares leave the range of 32 bits (elements of 2^60 and more, or below 2^-45 with an eps as small) are multiplied by a power
+ * of two before; only a head of zeros with eps 0 has no norm: 0 / 0, NaN. */
 typedef struct {
   const int32_t* positions;   /* the turn: as t2v_rotary's arguments; n_sections 0: none (the other five are not read) */
   const double* freqs;

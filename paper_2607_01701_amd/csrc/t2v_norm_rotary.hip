@@ -98,6 +98,28 @@ T2V_DEV float row_sum(float x) {
   return x;
 }
 
+// 1 / sqrt(mean x^2 + eps) of a row, f its elements' factor: 1, or, where the mean leaves the range in which 32 bits hold the squares of all that count, a power of
+// two by which u is multiplied first (a head of 2^70, or of 2^-80 with eps 0), and the reciprocal root is of the multiplied row.
+template <int D>
+T2V_DEV float row_root(float (&u)[kElems], float eps, float& f) {
+  constexpr int L = D / kElems;
+  auto mean = [&](float add) {
+    float s = 0.0f;
+#pragma unroll
+    for (int e = 0; e < kElems; ++e) s = fmaf(u[e], u[e], s);
+    return row_sum<L>(s) * (1.0f / D) + add;
+  };
+  float m = mean(eps);
+  f = 1.0f;
+  if (__builtin_expect(!(m >= 0x1p-90f && m <= 0x1p120f), 0)) {  // alike in a row's lanes
+    f = m < 1.0f ? 0x1p80f : 0x1p-70f;
+#pragma unroll
+    for (int e = 0; e < kElems; ++e) u[e] *= f;
+    m = mean(eps * f * f);
+  }
+  return rsqrtf(m);
+}
+
 // Places of a lane's two vectors within a row, and what of them turns.
 template <int D, bool INTERLEAVED, bool VIA_LDS>
 struct RowLane {
@@ -279,10 +301,8 @@ __global__ __launch_bounds__(kThreads) void norm_rotary_kernel(const NormArgs a,
         float u[kElems];
         unpack(u, x[i], y[i]);
         if (a.norm) {
-          float s = 0.0f;
-#pragma unroll
-          for (int e = 0; e < kElems; ++e) s = fmaf(u[e], u[e], s);
-          const float r = rsqrtf(row_sum<L>(s) * (1.0f / D) + a.eps);
+          float f;
+          const float r = row_root<D>(u, a.eps, f);
           const float* wr = wt[w.h >= hq];
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
@@ -359,10 +379,8 @@ __global__ __launch_bounds__(kThreads) void norm_rotary_bwd_kernel(const NormArg
             unpack(u, x[i][0], x[i][1]);
             unpack(v, g[i][0], g[i][1]);
             if (a.pairs > 0) turn_row(v, cs + w.t * (D / 2), a.pairs, sub, at, buf);
-            float s = 0.0f;
-#pragma unroll
-            for (int e = 0; e < kElems; ++e) s = fmaf(u[e], u[e], s);
-            const float r = rsqrtf(row_sum<L>(s) * (1.0f / D) + a.eps);
+            float f;
+            const float r = row_root<D>(u, a.eps, f);
             float c = 0.0f;
 #pragma unroll
             for (int e = 0; e < kElems; ++e) {
@@ -373,7 +391,7 @@ __global__ __launch_bounds__(kThreads) void norm_rotary_bwd_kernel(const NormArg
             }
             c = row_sum<L>(c) * (1.0f / D);
 #pragma unroll
-            for (int e = 0; e < kElems; ++e) v[e] = r * fmaf(-u[e], c, v[e]);
+            for (int e = 0; e < kElems; ++e) v[e] = r * fmaf(-u[e], c, v[e]) * f;
             gbf16* o = out + ((t0 + w.t) * heads + w.h) * D;
             store_vec(o + at.v0, packed(v, 0));
             store_vec(o + at.v1, packed(v, 8));
@@ -530,10 +548,8 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(const AppendArgs
           float u[kElems];
           unpack(u, z0, z1);
           if (a.norm) {
-            float s = 0.0f;
-#pragma unroll
-            for (int e = 0; e < kElems; ++e) s = fmaf(u[e], u[e], s);
-            const float r = rsqrtf(row_sum<L>(s) * (1.0f / D) + a.eps);
+            float f;
+            const float r = row_root<D>(u, a.eps, f);
             const float* wr = wt[not_q];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {

@@ -4,7 +4,8 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2607_01701_amd import Pages, paged_attn_fwd
+from oracle import norm_rotary as oracle
+from paper_2607_01701_amd import Pages, norm_rotary, norm_rotary_apply, norm_rotary_bwd, paged_append, paged_attn_fwd, rotary_frequencies
 
 from gpu_util import log
 from paged_util import Case
@@ -90,3 +91,56 @@ def test_idle_sequences_change_nothing(H, Hk, D, queries, keys):
         cu = torch.from_numpy(np.concatenate([[0], np.cumsum(np.bincount(at, queries, n))]).astype(np.int32)).cuda()
         got = paged_attn_fwd(c.q, Pages(c.pages.k, c.pages.v, table, lengths), cu, c.scale)
         assert all(torch.equal(a, b) for a, b in zip(got, ref))
+
+
+def within(got, ref, bound, what):
+    e = np.abs(np64(got) - ref)
+    worst = float((e / (bound + 1e-300)).max()) if e.size else 0.0
+    log(f"  {what}: {worst:.3f} of the bound")
+    assert worst <= 1.0, what
+
+
+@pytest.mark.parametrize("layout,pairs,D", [("half", 32, 64), ("interleaved", 40, 128), ("half", 21, 128)])
+@pytest.mark.parametrize("eps,powers", [(0.0, [0, -40, -50, -70, -74, -80, -100, -115]), (1e-6, [0, 40, 58, 62, 66, 100, 120]), (1e-30, [-60, -45, -75]),
+                                        (0.0, [63, 100]), (1e37, [0, 70])])
+def test_heads_of_any_size(eps, powers, layout, pairs, D):
+    """Heads whose squares pass the range of 32 bits either way are normalised like all others, and so are their gradients."""
+    log(f"case sizes {eps} {powers} {layout} {pairs} of {D}")
+    g = torch.Generator().manual_seed(len(powers) + D)
+    T = len(powers) * 3
+    size = torch.tensor(powers, dtype=torch.float64).repeat(3)[:, None, None]
+    q, k = ((torch.randn(T, h, D, generator=g, dtype=torch.float64).clamp(-4, 4) * 2.0 ** size).bfloat16().cuda() for h in (5, 2))
+    dq, dk = (torch.randn(T, h, D, generator=g).bfloat16().cuda() for h in (5, 2))
+    w = (1.0 + 0.25 * torch.randn(D, generator=g)).cuda()
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")
+    freqs, _ = rotary_frequencies(pairs)
+    turn = (pos.cpu().numpy(), freqs, layout, (pairs,), 1.0)
+    y = norm_rotary_apply(q, k, pos, freqs, w, w, eps, layout)
+    d = norm_rotary_bwd(q, k, dq, dk, pos, freqs, w, w, eps, layout)
+    n = torch.arange(T, dtype=torch.int64)
+    pages = Pages(*(torch.zeros(T, 16, 2, D, dtype=torch.bfloat16, device="cuda") for _ in range(2)),
+                  n[None].int().cuda(), torch.tensor([T], dtype=torch.int32, device="cuda"))
+    qa = paged_append(k, k, pages, torch.tensor([0, T], dtype=torch.int32, device="cuda"), q=q, positions=pos, freqs=freqs, layout=layout, q_weight=w,
+                      k_weight=w, eps=eps)
+    assert torch.equal(qa, y[0]) and torch.equal(pages.k[n // 16, n % 16], y[1])
+    # A result below the smallest normal number, 2^-126, is rounded by up to 2^-134 whatever its size.
+    for x, o, dy, dx, dw in ((q, y[0], dq, d[0], d[2]), (k, y[1], dk, d[1], d[3])):
+        ref, bound = oracle.forward(np64(x), np64(w), float(np.float32(eps)), *turn)
+        within(o, ref, bound + 2.0 ** -134, "normalised")
+        ref, ref_w, bound, bound_w = oracle.backward(np64(x), np64(dy), np64(w), float(np.float32(eps)), *turn, weight_step=2.0 ** -24)
+        within(dx, ref, bound + 2.0 ** -134, "gradient")
+        within(dw, ref_w, bound_w, "weight's gradient")
+
+
+def test_smallest_numbers_and_heads_of_one():
+    """Heads of the smallest numbers of the type, and heads with one element that is not zero; a head of zeros and no eps is 0 / 0."""
+    log("case smallest")
+    x = torch.zeros(4, 1, 128, dtype=torch.bfloat16, device="cuda")
+    x.view(torch.int16)[0] = 1  # 2^-133
+    x.view(torch.int16)[1, 0, 5] = 1
+    x[2, 0, 7] = -3.0e38
+    y, _ = norm_rotary_apply(x, None, None, None, eps=0.0)
+    assert (y[0] == 1.0).all()
+    root = torch.tensor(128.0 ** 0.5).bfloat16().item()
+    assert y[1, 0, 5] == root and int((y[1] != 0).sum()) == 1 and y[2, 0, 7] == -root and int((y[2] != 0).sum()) == 1
+    assert y[3].isnan().all()
