@@ -43,7 +43,7 @@ class Pages:
                                         table.data_ptr(), table.stride(0) if table.shape[0] > 1 else table.shape[1],
                                         table.shape[1], lengths.data_ptr(), table.shape[0], page_size, kv_heads, head_dim)
         self._ref = ctypes.byref(self._struct)
-        self._workspace = _lib._WORKSPACE  # what the last call needed
+        self._workspace = {}  # what calls needed, by the power of two that their packed rows reach
 
 
 def _check_cu(cu, pages):
@@ -76,7 +76,8 @@ def paged_attn_fwd(q, pages: Pages, cu_seqlens, scale: float, out=None, lse=None
     _check_cu(cu_seqlens, pages)
     device = pages.device
     _same_device(device, ("q", q), ("cu_seqlens", cu_seqlens))
-    size = pages._workspace
+    rows = (T * H // pages.kv_heads - 1).bit_length()
+    size = pages._workspace.get(rows, _lib._WORKSPACE)
     if out is None and lse is None and stream is None:
         out = torch.empty((T, H, D), dtype=torch.bfloat16, device=device)
         lse = torch.empty((H, T), dtype=torch.float32, device=device)
@@ -90,7 +91,7 @@ def paged_attn_fwd(q, pages: Pages, cu_seqlens, scale: float, out=None, lse=None
     args = (q.data_ptr(), step, H, cu_seqlens.data_ptr(), T, pages._ref, scale, out.data_ptr(), lse.data_ptr())
     st = _lib._call_on(device, stream, L.t2v_paged_fwd, *args, ws.data_ptr(), size, ctypes.byref(need))
     if st == _lib.T2V_ERR_WORKSPACE:
-        size = pages._workspace = need.value  # more than any call so far
+        size = pages._workspace[rows] = need.value  # more than any such call so far
         with _lib._on(stream):
             ws = torch.empty(size, dtype=torch.uint8, device=device)
         st = _lib._call_on(device, stream, L.t2v_paged_fwd, *args, ws.data_ptr(), size, ctypes.byref(need))

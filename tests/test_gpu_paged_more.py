@@ -144,3 +144,22 @@ def test_smallest_numbers_and_heads_of_one():
     root = torch.tensor(128.0 ** 0.5).bfloat16().item()
     assert y[1, 0, 5] == root and int((y[1] != 0).sum()) == 1 and y[2, 0, 7] == -root and int((y[2] != 0).sum()) == 1
     assert y[3].isnan().all()
+
+
+def test_a_chunk_leaves_tokens_their_workspace():
+    """A call takes the workspace of calls of its size, whatever larger ones the same pages had before."""
+    log("case workspace")
+    def took(c, q, cu):
+        torch.cuda.synchronize()
+        torch.cuda.reset_peak_memory_stats()
+        before = torch.cuda.memory_allocated()
+        paged_attn_fwd(q, c.pages, cu, c.scale)
+        return torch.cuda.max_memory_allocated() - before
+
+    c = Case(12, 4, 128, 64, [2000], [4000], width=1000)
+    one = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    token = [took(c, c.q[:1], one) for _ in range(2)]
+    chunk = [took(c, c.q, c.cu) for _ in range(2)]
+    again = [took(c, c.q[:1], one), took(c, c.q, c.cu), took(c, c.q[:10], torch.tensor([0, 10], dtype=torch.int32, device="cuda"))]
+    log(f"  {token} {chunk} {again}")
+    assert chunk[1] > 2 * token[1] and again[0] == token[1] and again[1] == chunk[1] and again[2] < chunk[1] / 2
