@@ -382,7 +382,8 @@ int t2v_paged_append(const void* k, const void* v, int64_t k_stride, int64_t v_s
  *   pages        of each buffer; page_bytes and page_stride (bytes) multiples of 16, page_bytes <= page_stride
  *   src, dst     HOST int32 [n], in 0 .. pages - 1; a page may be copied to several, but no page is written twice, nor both read and
  *                written: T2V_ERR_INVALID_ARG
- * Reads the HOST arrays before it returns. Buffers must not overlap, unless by pages that lie between each other's. */
+ * Reads the HOST arrays before it returns. Buffers whose pages share bytes are T2V_ERR_INVALID_ARG (pages may lie between each other's, and a buffer may
+ * be named twice). */
 int t2v_page_copy(void* const* buffers, int n_buffers, int64_t pages, int64_t page_stride, int64_t page_bytes,
                   const int32_t* src, const int32_t* dst, int n, void* stream);
 

@@ -50,6 +50,37 @@ __global__ __launch_bounds__(kThreads) void page_copy_kernel(const CopyArgs a) {
 
 int bad(const std::string& what) { return set_error(T2V_ERR_INVALID_ARG, what); }
 
+// Whether a page of the buffer at `low` shares bytes with one of the buffer at `high`, behind it.
+bool pages_meet(uintptr_t low, uintptr_t high, int64_t pages, int64_t stride, int64_t bytes) {
+  const auto far = static_cast<int64_t>(high - low), page = far / stride, in = far % stride;
+  return (page < pages && in < bytes) || (page + 1 < pages && stride - in < bytes);
+}
+
+// Whether pages of different buffers share bytes. (One buffer named twice is copied alike twice.) Buffers that lie apart are their neighbours' in the order of
+// addresses; of those that reach into each other, whose pages alternate, the places within a stride are neighbours.
+bool buffers_meet(void* const* buffers, int n, int64_t pages, int64_t stride, int64_t bytes) {
+  std::vector<uintptr_t> at(n);
+  for (int i = 0; i < n; ++i) at[i] = reinterpret_cast<uintptr_t>(buffers[i]);
+  std::sort(at.begin(), at.end());
+  at.erase(std::unique(at.begin(), at.end()), at.end());
+  const int count = static_cast<int>(at.size());
+  const double span = static_cast<double>(pages - 1) * stride + bytes;
+  std::vector<int64_t> in;
+  for (int i = 0, j; i < count; i = j) {
+    for (j = i + 1; j < count && static_cast<double>(at[j] - at[j - 1]) < span; ++j) {
+    }
+    in.clear();
+    for (int k = i; k < j; ++k) in.push_back(static_cast<int64_t>((at[k] - at[i]) % stride));
+    std::sort(in.begin(), in.end());
+    bool apart = in.back() + bytes <= stride;  // the first is at 0
+    for (size_t k = 1; k < in.size(); ++k) apart = apart && in[k] - in[k - 1] >= bytes;
+    for (int k = i; !apart && k < j; ++k)
+      for (int l = k + 1; l < j; ++l)
+        if (pages_meet(at[k], at[l], pages, stride, bytes)) return true;
+  }
+  return false;
+}
+
 int page_copy_impl(void* const* buffers, int n_buffers, int64_t pages, int64_t stride, int64_t bytes, const int32_t* src,
                    const int32_t* dst, int n, void* stream) {
   if (n_buffers < 0 || n < 0) return bad("n_buffers and n must be >= 0");
@@ -74,6 +105,7 @@ int page_copy_impl(void* const* buffers, int n_buffers, int64_t pages, int64_t s
   if (int st = validate_pointers(in, {})) return st;
   const int64_t parts = (bytes + kPart - 1) / kPart;
   if (parts * kThreads > UINT32_MAX) return bad("page_bytes is too large");
+  if (buffers_meet(buffers, n_buffers, pages, stride, bytes)) return bad("buffers overlap");
   CopyArgs a;
   a.stride = stride;
   a.bytes = bytes;

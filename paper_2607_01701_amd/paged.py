@@ -181,7 +181,8 @@ def _buffers(buffers):
 
 def page_copy(buffers, src, dst, stream=None):
     """Copies pages src[i] to pages dst[i] in every one of `buffers`: a tensor [pages, ...] on the GPU or a sequence of them, of one shape and
-    strides, each page's memory dense. src, dst: host int32 arrays; no page may be written twice, nor both read and written."""
+    strides, each page's memory dense and apart from the other buffers' pages. src, dst: host int32 arrays; no page may be written twice, nor both read
+    and written."""
     import torch
     buffers = (buffers,) if isinstance(buffers, torch.Tensor) else tuple(buffers)
     src, dst = _numbers(src), _numbers(dst)
