@@ -109,6 +109,18 @@ class PageTable:
         self.room[rows] -= more
         self.lengths[rows] += more.astype(np.int32)
 
+    def offsets(self, tokens):
+        """int32 offsets of a call in which sequence s has tokens[s] new tokens (a dict, or one count for each sequence)."""
+        counts = np.zeros(self.active.size, dtype=np.int64)
+        for s, n in tokens.items() if isinstance(tokens, dict) else enumerate(tokens):
+            if not (0 <= s < counts.size and 0 <= n < 2 ** 31) or s != int(s) or n != int(n):
+                raise ValueError(f"{n} tokens of sequence {s}, of {counts.size}")
+            counts[int(s)] = int(n)
+        cu = np.concatenate([[0], np.cumsum(counts)])
+        if cu[-1] >= 2 ** 31:
+            raise ValueError(f"{cu[-1]} tokens are too many for one call")
+        return cu.astype(np.int32)
+
     def fork(self, sequence: int) -> int:
         """A new sequence with the same tokens, whose pages both share."""
         (s,), _ = self._rows([sequence], 0)

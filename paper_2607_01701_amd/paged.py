@@ -240,15 +240,7 @@ class PagedCache:
 
     def offsets(self, tokens):
         """cu_seqlens on the GPU for a call in which sequence s has tokens[s] new tokens (a dict, or one count for each sequence)."""
-        counts = np.zeros(self._host().active.size, dtype=np.int64)
-        for s, n in tokens.items() if isinstance(tokens, dict) else enumerate(tokens):
-            if not 0 <= s < counts.size or n < 0:
-                raise ValueError(f"{n} tokens of sequence {s}, of {counts.size}")
-            counts[s] = n
-        cu = np.concatenate([[0], np.cumsum(counts)])
-        if cu[-1] >= 2 ** 31:
-            raise ValueError(f"{cu[-1]} tokens are too many for one call")
-        return self._to_device(cu.astype(np.int32))
+        return self._to_device(self._host().offsets(tokens))
 
     def _to_device(self, x, out=None):
         import torch
