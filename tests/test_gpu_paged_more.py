@@ -163,3 +163,71 @@ def test_a_chunk_leaves_tokens_their_workspace():
     again = [took(c, c.q[:1], one), took(c, c.q, c.cu), took(c, c.q[:10], torch.tensor([0, 10], dtype=torch.int32, device="cuda"))]
     log(f"  {token} {chunk} {again}")
     assert chunk[1] > 2 * token[1] and again[0] == token[1] and again[1] == chunk[1] and again[2] < chunk[1] / 2
+
+
+def many_tokens(T, H, Hk, D, pairs, layout, page, extra, seed):
+    """Queries, keys and values of T tokens and `extra` rows of padding in sequences of odd lengths, some empty, some of one token, beside pages in random order whose
+    other rows hold a canary; with the pages and rows that the tokens go to."""
+    r = np.random.default_rng(seed)
+    queries, left = [], T
+    while left:
+        n = min(left, int(r.choice([0, 1, 2, 7, int(r.integers(3, 60)), int(r.integers(60, max(61, T // 3)))])))
+        queries.append(n)
+        left -= n
+    keys = [n + int(r.choice([0, 1, 5, page, 3 * page + 2])) for n in queries]
+    counts = [-(-n // page) for n in keys]
+    order, width = r.permutation(sum(counts) + 5), max(counts) + 1
+    table = np.full((len(keys), width), -1, dtype=np.int32)
+    at, where = 0, []
+    for s, (n, m) in enumerate(zip(queries, keys)):
+        table[s, :counts[s]] = order[at:at + counts[s]]
+        at += counts[s]
+        j = np.arange(m - n, m)
+        where.append(np.stack([table[s, j // page], j % page]))
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    qkv = torch.randn(T + extra, H + 2 * Hk, D, generator=g, device="cuda").bfloat16()
+    pages = Pages(*(torch.full((order.size, page, Hk, D), 9.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)), torch.from_numpy(table).cuda(),
+                  torch.tensor(keys, dtype=torch.int32, device="cuda"))
+    cu = torch.from_numpy(np.concatenate([[0], np.cumsum(queries)]).astype(np.int32)).cuda()
+    pos = torch.randint(0, 100_000, (T + extra,), generator=g, device="cuda", dtype=torch.int32)
+    return qkv[:, :H], qkv[:, H:H + Hk], qkv[:, H + Hk:], pages, cu, pos, torch.from_numpy(np.concatenate(where, 1)).cuda().long()
+
+
+def check_append(T, H, Hk, D, pairs, layout, page, extra, with_q, sample, seed):
+    q, k, v, pages, cu, pos, (p, r) = many_tokens(T, H, Hk, D, pairs, layout, page, extra, seed)
+    freqs, _ = rotary_frequencies(pairs)
+    w = (1.0 + 0.25 * torch.randn(2, D, generator=torch.Generator().manual_seed(seed))).cuda()
+    q_out = torch.full((T + extra, H, D), 7.0, dtype=torch.bfloat16, device="cuda") if with_q else None
+    paged_append(k, v, pages, cu, q=q if with_q else None, positions=pos, freqs=freqs, layout=layout, q_weight=w[0] if with_q else None, k_weight=w[1], eps=1e-6,
+                 q_out=q_out)
+    assert torch.equal(pages.v[p, r], v[:T])
+    stored = torch.zeros(pages.k.shape[:2], dtype=torch.bool, device="cuda")
+    stored[p, r] = True
+    assert (pages.k[~stored] == 9.0).all() and (pages.v[~stored] == 9.0).all()
+    rows = torch.arange(T, device="cuda") if sample is None else torch.randperm(T, generator=torch.Generator().manual_seed(1))[:sample].cuda()
+    turn = (pos[rows].cpu().numpy(), freqs, layout, (pairs,), 1.0)
+    within(pages.k[p[rows], r[rows]], *oracle.forward(np64(k[rows]), np64(w[1]), 1e-6, *turn), "keys")
+    if with_q:
+        within(q_out[rows], *oracle.forward(np64(q[rows]), np64(w[0]), 1e-6, *turn), "queries")
+        assert (q_out[T:] == 7.0).all()
+        ref, _ = norm_rotary_apply(q, None, pos, freqs, w[0], eps=1e-6, layout=layout)
+        assert torch.equal(q_out[:T], ref[:T])  # every row, from the kernel that only normalises and turns
+
+
+@pytest.mark.parametrize("with_q", [True, False], ids=["q", "keys"])
+@pytest.mark.parametrize("T,H,Hk,D,pairs,layout,page,extra", [
+    (1537, 2, 1, 128, 64, "half", 64, 0), (1537, 2, 1, 128, 20, "interleaved", 16, 5), (16501, 2, 1, 128, 64, "interleaved", 64, 3), (16501, 1, 1, 64, 32, "half", 16, 1),
+    (16411, 1, 2, 64, 18, "half", 32, 700), (5003, 3, 1, 128, 21, "half", 256, 0), (4099, 30, 10, 64, 24, "half", 16, 9), (33003, 1, 1, 64, 7, "interleaved", 128, 0),
+    (2053, 24, 8, 128, 40, "half", 64, 2),
+])
+def test_append_with_several_tokens_to_a_workgroup(T, H, Hk, D, pairs, layout, page, extra, with_q):
+    """Sequences that begin, end and are empty within a workgroup's tokens, a last workgroup with fewer tokens, padding."""
+    log(f"case append {T} {H}/{Hk}x{D} {pairs} {layout} page {page} + {extra} {with_q}")
+    check_append(T, H, Hk, D, pairs, layout, page, extra, with_q, None, T + D)
+
+
+@pytest.mark.parametrize("T,layout,pairs", [(20_537, "half", 64), (20_537, "half", 21), (30_011, "interleaved", 64), (30_011, "half", 30)])
+def test_append_of_more_than_the_caches_hold(T, layout, pairs):
+    """210 MB read and written, and 307: inputs, and outputs too, that the caches need not keep."""
+    log(f"case append {T} {layout} {pairs}")
+    check_append(T, 24, 8, 128, pairs, layout, 64, 3, True, 400, T + pairs)
