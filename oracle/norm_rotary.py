@@ -11,7 +11,7 @@ Each result comes with how far a kernel may be off that computes in 32 bits and 
 to 32 bits is off by at most e = 2^-24 of the value, one to bf16 by 2^-8. The norm: at most 25 roundings in the mean of squares,
 whose error the root halves, 4 e of the reciprocal root, two products and r's own: under 32 e = 2^-19 of x^ and n. The turn: sine and
 cosine off by 2^-22, two products and a sum: 2^-21 mscale (|a| + |b|) of a pair (a, b). The backward pass's row sum has 25
-roundings as the norm's, its other steps three. dw's sums are at most 64 deep (a lane's rows, the lanes, the workgroups).
+roundings as the norm's, its other steps three. A term of dw's sums is rounded as often as weight_depth says.
 """
 from __future__ import annotations
 
@@ -50,6 +50,13 @@ def forward(x, w, eps, *turn):
     return y, e + 2.0 ** -8 * np.abs(y)
 
 
+def weight_depth(T, H, D):
+    """Sums that a term of dw goes through: those of a lane, which adds up its rows one after the other, of the 4096 / D groups of lanes of a workgroup, and of the
+    workgroups (two by a thread, eight steps of a tree). A workgroup has at most T / 256 tokens; its groups share the rows of eight or more of them at a time."""
+    groups, tokens = 4096 // D, -(-T // 256)
+    return -(-tokens * H // groups) + tokens // 8 + 2 + groups + 2 + 8
+
+
 def backward(x, dy, w, eps, *turn, weight_step=0.0):
     """dx, dw and their bounds; weight_step: the rounding of dw (2^-8 for bf16)."""
     x, dy = np.asarray(x, dtype=np.float64), np.asarray(dy, dtype=np.float64)
@@ -63,5 +70,5 @@ def backward(x, dy, w, eps, *turn, weight_step=0.0):
     dx = r * (g - xhat * c)
     e_dx = r * (e_g + np.abs(xhat) * e_c + 2 * NORM * (np.abs(g) + np.abs(xhat * c))) + 2.0 ** -8 * np.abs(dx)
     dw = (dn * xhat).sum((0, 1))
-    e_dw = (e_dn * np.abs(xhat) + (NORM + 64 * E) * np.abs(dn * xhat)).sum((0, 1)) + weight_step * np.abs(dw)
+    e_dw = (e_dn * np.abs(xhat) + (NORM + weight_depth(*x.shape) * E) * np.abs(dn * xhat)).sum((0, 1)) + weight_step * np.abs(dw)
     return dx, dw, e_dx, e_dw

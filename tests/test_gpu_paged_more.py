@@ -231,3 +231,35 @@ def test_append_of_more_than_the_caches_hold(T, layout, pairs):
     """210 MB read and written, and 307: inputs, and outputs too, that the caches need not keep."""
     log(f"case append {T} {layout} {pairs}")
     check_append(T, 24, 8, 128, pairs, layout, 64, 3, True, 400, T + pairs)
+
+
+@pytest.mark.parametrize("T,H,D,pairs,layout", [(200_003, 32, 128, 64, "interleaved"), (160_001, 30, 64, 18, "half"), (60_000, 100, 128, 32, "half")])
+@pytest.mark.parametrize("signs", ["one", "both"])
+def test_deep_sums_of_weight_gradients(T, H, D, pairs, layout, signs):
+    """Hundreds of rows to a lane, terms of one sign or of both: every dimension of dw within its sums' roundings."""
+    log(f"case deep sums {T} x {H}x{D} {signs}")
+    g = torch.Generator(device="cuda").manual_seed(T)
+    x = torch.randn(T, H, D, generator=g, device="cuda").bfloat16()
+    pos = torch.randint(0, 1000, (T,), generator=g, device="cuda", dtype=torch.int32)
+    freqs, _ = rotary_frequencies(pairs)
+    w = torch.ones(D, device="cuda")
+    # The gradient of |y|^2 / 2 is y: each of dw's terms is a square then.
+    dy = norm_rotary_apply(x, None, pos, freqs, w, layout=layout)[0] if signs == "one" else torch.randn(T, H, D, generator=g, device="cuda").bfloat16()
+    dw = norm_rotary_bwd(x, None, dy, None, pos, freqs, w, layout=layout)[2]
+    a, b = oracle._pairs(pairs, layout)
+    ref, size, turn = (torch.zeros(D, dtype=torch.float64, device="cuda") for _ in range(3))
+    angles = pos.double()[:, None, None] * torch.from_numpy(np.asarray(freqs, dtype=np.float64)).cuda()
+    for i in range(0, T, 8192):
+        xs, ds = x[i:i + 8192].double(), dy[i:i + 8192].double()
+        xhat = xs / torch.sqrt((xs * xs).mean(-1, keepdim=True) + 1e-6)
+        c, s = torch.cos(angles[i:i + 8192]), -torch.sin(angles[i:i + 8192])
+        dn, own = ds.clone(), torch.zeros_like(ds)
+        dn[..., a], dn[..., b] = ds[..., a] * c - ds[..., b] * s, ds[..., a] * s + ds[..., b] * c
+        own[..., a] = own[..., b] = ds[..., a].abs() + ds[..., b].abs()
+        ref += (dn * xhat).sum((0, 1))
+        size += (dn * xhat).abs().sum((0, 1))
+        turn += (own * xhat.abs()).sum((0, 1))
+    bound = (oracle.NORM + oracle.weight_depth(T, H, D) * oracle.E) * size + oracle.TURN * turn + 2.0 ** -24 * ref.abs()
+    worst = float(((dw.double() - ref).abs() / bound).max())
+    log(f"  {oracle.weight_depth(T, H, D)} deep: {worst:.4f} of the bound")
+    assert worst <= 1.0
