@@ -772,7 +772,7 @@ int norm_rotary_bwd_impl(const void* q, const void* k, int64_t q_stride, int64_t
   a.positions = turn->positions;
   a.tokens = tokens;
   if (int st = check_pointers(a, tokens > 0 ? axes : 0, in, out)) return st;
-  // As many workgroups as the GPU holds at once, if they get rows enough to have two in flight in every lane.
+  // At most 512 workgroups (measured: at the top), and fewer, 256 and more, for each to get rows enough to have two in flight in every lane.
   const int64_t rows = kRowsBack * (kThreads * kElems / head_dim), least = (rows + heads + kv_heads - 1) / (heads + kv_heads);
   const int64_t each = std::max<int64_t>((tokens + kMaxBackBlocks - 1) / kMaxBackBlocks, std::min<int64_t>(least, (tokens + 255) / 256));
   const int blocks = tokens == 0 ? 0 : static_cast<int>((tokens + each - 1) / each);

@@ -171,7 +171,7 @@ T2V_HD PagedShares paged_shares(const PagedRule& r, int64_t total, int n, int gr
   PagedShares s;
   s.dies = paged_by_die(groups) ? 8 : 1;
   s.each = n / s.dies;
-  const int64_t least = static_cast<int64_t>(r.share) * 256, keys = total / 256 / s.dies + 1;  // keys: of a die
+  const int64_t least = static_cast<int64_t>(r.share) * 256, keys = (total >> (s.dies == 8 ? 11 : 8)) + 1;  // keys: of a die
   if (keys < static_cast<int64_t>(s.each) * r.share) s.each = static_cast<int>((static_cast<unsigned>(keys) + r.share - 1) / static_cast<unsigned>(r.share));
   const int shares = s.dies * s.each;
 #if defined(__HIP_DEVICE_COMPILE__)
