@@ -53,7 +53,7 @@ struct PagesView {
 // The first piece of the tile that a workgroup cuts, for the join. Pieces 1, 2, .. are those of the line's next shares.
 struct PagedDesc {
   int64_t q0, first, next;  // first and second piece's place in the partial results, in floats
-  int lq, lk, row0, head, pieces, rows;
+  int lq, row0, head, pieces, rows;
 };
 
 struct PagedArgs {
@@ -219,7 +219,7 @@ T2V_DEV void for_pieces(Walk& w, F&& f) {
             begun = true;
             const int64_t place = slot_floats<D>(w, rule.tile), slot = static_cast<int64_t>(rule.tile) * (D + 2);
             if (threadIdx.x == 0)
-              arguments().desc[blockIdx.x] = {s.q0, place + slot, place + 2 * slot, s.lq, s.lk, tile * rule.tile, w.head, min(p.pieces, w.shares - w.share), rule.tile};
+              arguments().desc[blockIdx.x] = {s.q0, place + slot, place + 2 * slot, s.lq, tile * rule.tile, w.head, min(p.pieces, w.shares - w.share), rule.tile};
           }
           f(w.seq, s, t, w.head, p);
         }
@@ -688,7 +688,8 @@ struct JoinArgs {
 
 // Joins the pieces of the tile that a workgroup begins: with the largest reference m of a row, out = sum_p 2^(m_p - m) O_p / l,
 // l = sum_p 2^(m_p - m) l_p, in piece order. D / 8 lanes hold a row, eight columns each. Of a tile with fewer rows than a workgroup holds, several groups
-// of lanes take parts of the pieces, whose sums meet in LDS, in order.
+// of lanes take parts of the pieces, whose sums meet in LDS, in order. Every row sees keys: a tile is cut where its last row sees twice the shortest piece, 256
+// keys, or more, and has 128 queries at most.
 template <int D>
 __global__ __launch_bounds__(kThreads) void paged_join_kernel(const JoinArgs a) {
   constexpr int LPR = D / 8, RPB = kThreads / LPR;
@@ -752,7 +753,7 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(const JoinArgs a) 
     }
     if (!real || part > 0) continue;
     const PackedRow pr = packed_row(it.row0 + r, a.group);
-    const float inv = pr.query + (it.lk - it.lq) < 0 ? 0.0f : 1.0f / l;
+    const float inv = 1.0f / l;
     const int64_t token = it.q0 + pr.query;
     const int head = it.head * a.group + pr.head;
     bf16x8 o;

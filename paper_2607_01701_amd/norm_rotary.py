@@ -9,7 +9,7 @@ import numpy as np
 
 from . import _lib
 from .autograd import check_capture, note_leaves
-from .rotary import _SECTIONS, _arguments, _check_positions, _rows
+from .rotary import _arguments, _check_positions, _rows
 
 
 def _weights(q_weight, k_weight, q, k, eps):

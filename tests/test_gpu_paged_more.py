@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from oracle import norm_rotary as oracle
-from paper_2607_01701_amd import Pages, norm_rotary, norm_rotary_apply, norm_rotary_bwd, paged_append, paged_attn_fwd, rotary_frequencies
+from paper_2607_01701_amd import Pages, norm_rotary_apply, norm_rotary_bwd, paged_append, paged_attn_fwd, rotary_frequencies
 
 from gpu_util import log
 from paged_util import Case
