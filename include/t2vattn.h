@@ -319,7 +319,7 @@ int t2v_norm_rotary(const void* q, const void* k, int64_t q_stride, int64_t k_st
  *   dq, dk           device bf16, contiguous, written
  *   dq_weight, dk_weight   device [head_dim] of the weights' type, 16-byte aligned, written; NULL where not wanted or the weight is NULL
  *   ws, ws_bytes, need     as in t2v_causal_fwd; at most 1 MiB, 0 without gradients of weights
- * Outputs must not overlap each other or any input. Without tokens the gradients of weights are zeros. Deterministic: no atomics. */
+ * Outputs must not overlap each other or any input. Without tokens, or heads, the gradients of weights are zeros. Deterministic: no atomics. */
 int t2v_norm_rotary_bwd(const void* q, const void* k, int64_t q_stride, int64_t k_stride, const void* dq_out,
                         const void* dk_out, int64_t dq_out_stride, int64_t dk_out_stride, int64_t tokens, int heads,
                         int kv_heads, int head_dim, const t2v_turn* turn, void* dq, void* dk, void* dq_weight,

@@ -748,14 +748,13 @@ int norm_rotary_bwd_impl(const void* q, const void* k, int64_t q_stride, int64_t
   bool weights = false;
   for (int i = 0; i < 2; ++i) {
     a.heads[i] = t[i].heads;
-    if (t[i].heads == 0) continue;
     if (t[i].dweight != nullptr) {
-      if (a.weight[i] == nullptr) return bad(std::string(t[i].dweight_name) + " is given without its weight");
+      if ((i == 0 ? turn->q_weight : turn->k_weight) == nullptr) return bad(std::string(t[i].dweight_name) + " is given without its weight");
       a.dweight[i] = t[i].dweight;
       out.push_back({t[i].dweight, head_dim * (a.weights_f32 ? 4 : 2), t[i].dweight_name});
       weights = true;
     }
-    if (tokens == 0) continue;
+    if (tokens == 0 || t[i].heads == 0) continue;
     if (int st = check_stride(t[i].stride, t[i].heads, head_dim, t[i].stride_name)) return st;
     if (int st = check_stride(t[i].grad_stride, t[i].heads, head_dim, t[i].grad_stride_name)) return st;
     in.push_back({t[i].in, rows_bytes(tokens, t[i].stride, t[i].heads, head_dim), t[i].name});

@@ -263,3 +263,20 @@ def test_deep_sums_of_weight_gradients(T, H, D, pairs, layout, signs):
     worst = float(((dw.double() - ref).abs() / bound).max())
     log(f"  {oracle.weight_depth(T, H, D)} deep: {worst:.4f} of the bound")
     assert worst <= 1.0
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gradients_of_weights_that_no_head_takes(dtype):
+    """q without heads beside k: its weight's gradient is zeros."""
+    log(f"case no heads {dtype}")
+    g = torch.Generator().manual_seed(2)
+    k, dk = (torch.randn(50, 2, 64, generator=g).bfloat16().cuda() for _ in range(2))
+    w = torch.ones(64, dtype=dtype, device="cuda")
+    for _ in range(3):  # memory that an unwritten result would be made of
+        used = [torch.full((n,), 7.0, dtype=dtype, device="cuda") for n in (64, 64, 64)]
+        torch.cuda.synchronize()
+        del used
+        d = norm_rotary_bwd(k[:, :0], k, dk[:, :0], dk, None, None, w, w)
+        ref = norm_rotary_bwd(None, k, None, dk, None, None, None, w)
+        assert d[0].shape == (50, 0, 64) and (d[2] == 0).all()
+        assert torch.equal(d[1], ref[1]) and torch.equal(d[3], ref[3])
