@@ -369,7 +369,8 @@ int t2v_paged_fwd(const void* q, int64_t q_stride, int heads, const int32_t* cu_
  *   q, q_out     device bf16 [tokens, heads, D], q with a stride, q_out contiguous and written; heads 0: none
  *   cu_seqlens, cache   as in t2v_paged_fwd (the pages are written); K's and V's rows must not be the same memory
  *   turn         HOST struct or NULL: keys are stored as they are, and heads must be 0
- * A token without a place (a key below 0 or beyond the table's width, a page outside the cache) is not stored; padding behind the last
+ * A token without a place (a key below 0 or beyond the table's width, a page outside the cache) is not stored, nor is any of a sequence whose length passes
+ * the table's width; padding behind the last
  * sequence neither, and its q_out is left as it was. Other rows of the pages stay as they are. Pages that two sequences share must
  * not both get tokens in one row. */
 int t2v_paged_append(const void* k, const void* v, int64_t k_stride, int64_t v_stride, const void* q, int64_t q_stride,

@@ -70,7 +70,8 @@ def norm_rotary_apply(q, k, positions, freqs, q_weight=None, k_weight=None, eps=
                       mscale: float = 1.0, q_out=None, k_out=None, stream=None):
     """The heads of q [T, H, D] and k [T, Hk, D] divided by their root mean square (eps added to the mean square), times q_weight and
     k_weight ([D], both float32 or both bfloat16; None: ones), then turned as by rotary_apply, in one pass rounded once. bf16 on
-    the GPU, tokens any distance apart, either may be None; eps None: no norm; freqs (and positions) None: no turn. Returns contiguous (q, k)."""
+    the GPU, tokens any distance apart, either may be None; eps None: no norm; freqs (and positions) None: no turn. Returns contiguous (q, k),
+    without gradients or tangents, whatever the arguments have: norm_rotary is the call with autograd."""
     checked = _checked(q, k, positions, freqs, layout, sections, mscale, q_weight, k_weight, eps)
     return _forward(q, k, positions, checked, q_weight, k_weight, q_out, k_out, stream)
 
@@ -118,7 +119,7 @@ def _forward(q, k, positions, checked, q_weight, k_weight, q_out=None, k_out=Non
 def norm_rotary_bwd(q, k, dq_out, dk_out, positions, freqs, q_weight=None, k_weight=None, eps: float = 1e-6,
                     layout: str = "half", sections=None, mscale: float = 1.0, stream=None):
     """Backward of norm_rotary_apply: from its inputs and the gradients of its outputs (tokens any distance apart), those of q and k (bf16) and of
-    the weights (of their type, None without weights): (dq, dk, dq_weight, dk_weight)."""
+    the weights (of their type, None without weights): (dq, dk, dq_weight, dk_weight), which have no gradients themselves."""
     if eps is None:
         raise ValueError("the backward pass needs a norm; a turn alone is rotary_apply's inverse")
     checked = _checked(q, k, positions, freqs, layout, sections, mscale, q_weight, k_weight, eps)

@@ -65,7 +65,8 @@ def paged_attn_fwd(q, pages: Pages, cu_seqlens, scale: float, out=None, lse=None
     the GPU, tokens any distance apart) holds sequence s's queries in rows cu_seqlens[s] .. cu_seqlens[s + 1] - 1 (int32 on the GPU; rows behind
     the last are padding and left as they are in out and lse). Query i of Lq sees keys 0 .. i + lengths[s] - Lq of its sequence, whose
     keys and values are already stored. Returns (out [T, H, D]
-    bf16, lse [H, T] fp32). A page number outside the cache or a length beyond the table's width gives NaN."""
+    bf16, lse [H, T] fp32). A page number outside the cache or a length beyond the table's width gives NaN. No autograd: the results have no gradient or
+    tangent, whatever the arguments have."""
     import torch
     if q.dim() != 3:
         raise ValueError("q must be [tokens, heads, head_dim]")
@@ -105,7 +106,7 @@ def paged_append(k, v, pages: Pages, cu_seqlens, q=None, positions=None, freqs=N
     """Stores the keys and values k, v [T, Hk, D] of new tokens in their pages: of sequence s with Lq tokens (rows as in paged_attn_fwd), token i is key
     lengths[s] - Lq + i. With freqs and positions the keys are turned before, with eps normalised (times k_weight), and so are the
     queries q [T, H, D] of the same tokens, as by norm_rotary_apply, in the same pass; returns those (None without q). A token without a place in
-    the cache is not stored (attention over it gives NaN)."""
+    the cache is not stored, nor any of a sequence whose length passes the table's width (attention over them gives NaN). No autograd, as in paged_attn_fwd."""
     import torch
     if k.dim() != 3 or (q is not None and q.dim() != 3):
         raise ValueError("q and k must be [tokens, heads, head_dim]")
