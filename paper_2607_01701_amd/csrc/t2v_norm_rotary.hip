@@ -7,9 +7,9 @@
 // (VIA_LDS). Sines and cosines are worked out once a token and shared by its heads through LDS, after the first loads.
 //
 // Bound by memory, each element being read and written once (backward: two read, one written): 116,904 tokens of 24 + 24 heads of 128
-// forward 476 us, 6.0 TB/s, backward 819 us, 5.3 TB/s; 20,280 tokens of 24 + 8 heads 57 us, 5.8 TB/s; through LDS (14,750 tokens of 30 + 10
+// forward 476 us, 6.0 TB/s (in a training step, behind a backward pass, 489), backward 819 us, 5.3 TB/s; 20,280 tokens of 24 + 8 heads 57 us, 5.8 TB/s; through LDS (14,750 tokens of 30 + 10
 // heads of 64, 36 dimensions turned) 37 and 50 us. Forward, many short workgroups with one row a lane in flight are fastest: with two rows
-// 514 us of the 490 that it takes without the marks of set_once, with 2 tokens a workgroup in place of 1 525, with 8 555. Backward, 512
+// 514 us of the 492 that it takes without the marks of set_once, with 2 tokens a workgroup in place of 1 525, with 8 555. Backward, 512
 // workgroups, which leave few sums for the weights, lose nothing (512 to 32,768 of them with tokens of their own: 846 to 870 us), and marks gain
 // nothing (860 to 889).
 #include <algorithm>
@@ -672,7 +672,7 @@ int tokens_per_block(int64_t tokens, int heads, int head_dim) {
 // nothing (14,750 tokens, 75 MB: 36 us, 38 to 39 with either hint on reads). Where only the outputs fit: the inputs, so that the outputs wait there for the
 // attention (20,280 tokens, 24 + 8 heads, 166 MB: 57 us against 64; stored in pages, 210 MB: 77 against 90; with the outputs marked too
 // 84, or 81 for 90 where no call writes the memory of another). Else both
-// (116,904 tokens, 1.4 GB: 474 us against 490).
+// (116,904 tokens, 1.4 GB: 476 us against 492).
 void set_once(NormArgs* a, int64_t out_bytes) {
   constexpr int64_t kCache = 256 << 20;
   a->read_once = 2 * out_bytes > kCache;

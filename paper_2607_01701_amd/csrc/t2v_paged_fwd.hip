@@ -7,15 +7,17 @@
 //
 // A page number outside the cache is replaced by a row of NaN, so that it shows in the queries that see it and nothing is read.
 //
-// What bounds it. Few rows (single tokens): memory. 32 tokens over 31 to 20,280 keys, 40 heads over 8 of 128, 813 MB: 139 us, 5.8 TB/s; a
+// What bounds it. Few rows (single tokens): memory. 32 tokens over 31 to 20,280 keys, 40 heads over 8 of 128, 813 MB: 141 us, 5.75 TB/s; a
 // token over 100,000 keys, 24 heads over 8: 70 us; both and the join's 5. Copies to LDS reach 6.0 TB/s, and 6.6 marked as not to be kept (nt), which each
-// key is here: without the mark 17 and 10 us more. One token over 1,280 keys takes 9 us, a chain of dependent reads (offsets, page numbers, keys).
-// Many rows (chunks, prompts): the matrix cores. 768, 257 and 512 queries over 20,280, 4,097 and 9,999 keys, 12 heads over 4 of 128: 136 us, 970
-// TFLOP/s, and 11 for the join of 42 MB of partial sums; a prompt of 6,912 tokens, 24 heads over 8, 338 us in all, where the kernel of whole offsets on
+// key is here: without the mark 17 and 10 us more. One token over 1,280 keys takes 10 us, a chain of dependent reads (offsets, page numbers, keys).
+// Many rows (chunks, prompts): the matrix cores. 768, 257 and 512 queries over 20,280, 4,097 and 9,999 keys, 12 heads over 4 of 128: 140 to 143 us, 920 to
+// 940 TFLOP/s, and 11 for the join of 42 MB of partial sums; a prompt of 6,912 tokens, 24 heads over 8, 338 us in all, where the kernel of whole offsets on
 // the host (t2v_causal_fwd.hip), which deals tiles longest first and cuts fewer, takes 320; of 20,280 tokens 2,445 against 2,175, as
 // there the workgroups of a die read other parts of more keys than its L2 holds.
+// Every workgroup goes through the offsets and lengths of all sequences, 64 at a time: the chunks take 145 us among 64 sequences and 157 among 256, most of them
+// idle.
 // Mixtures run both at once, two workgroups a CU at head_dim 128 and three at 64, as many as registers and LDS let: 30 tokens beside chunks
-// of 512 and 300, 804 MB: 146 us (as two launches, one after the other, 202).
+// of 512 and 300, 804 MB: 148 us (as two launches, one after the other, 202).
 #include <algorithm>
 
 #include "t2v_causal_fwd_step.hpp"
