@@ -2,6 +2,8 @@
 shared by forks are copied when one of them goes on writing. No tensors here; PagedCache runs the copies."""
 from __future__ import annotations
 
+import math
+
 import numpy as np
 
 
@@ -112,11 +114,14 @@ class PageTable:
     def offsets(self, tokens):
         """int32 offsets of a call in which sequence s has tokens[s] new tokens (a dict, or one count for each sequence)."""
         counts = np.zeros(self.active.size, dtype=np.int64)
+        size = counts.size
         for s, n in tokens.items() if isinstance(tokens, dict) else enumerate(tokens):
-            if not (0 <= s < counts.size and 0 <= n < 2 ** 31) or s != int(s) or n != int(n):
-                raise ValueError(f"{n} tokens of sequence {s}, of {counts.size}")
-            counts[int(s)] = int(n)
+            if not 0 <= s < size or not 0 <= n < 2 ** 31 or s % 1:
+                raise ValueError(f"{n} tokens of sequence {s}, of {size}")
+            counts[s] = n
         cu = np.concatenate([[0], np.cumsum(counts)])
+        if math.fsum(tokens.values() if isinstance(tokens, dict) else tokens) != cu[-1]:  # what is stored of a fraction is less
+            raise ValueError(f"numbers of tokens must be whole, got {tokens}")
         if cu[-1] >= 2 ** 31:
             raise ValueError(f"{cu[-1]} tokens are too many for one call")
         return cu.astype(np.int32)
