@@ -29,13 +29,13 @@ def test_views_of_one_cache():
     assert copy([A, A + 40 * 4096], 60, 4096, 4096)
     assert copy([A + 40 * 4096, A], 60, 4096, 4096)
     assert copy([A, A + 1024], 10, 4096, 2048)
-    assert copy([A, A + 3072], 10, 4096, 2048)  # a page's end and the next page's begin
+    assert copy([A, A + 2560], 10, 4096, 2048)  # a page's end and the next page's begin
     assert copy([A, A + 2 ** 36, A + 2 ** 36 + 16], 10, 4096, 4096)
     assert not copy([A, A + 60 * 4096], 60, 4096, 4096)
     assert not copy([A, A + 2048], 60, 4096, 2048)
     assert not copy([A, A + 59 * 4096 + 2048], 60, 4096, 2048)
     assert not copy([A, A], 60, 4096, 4096)  # the same buffer twice
-    assert not copy([A, A + 4096 + 3072], 2, 4096, 2048)  # behind the last page's bytes
+    assert not copy([A, A + 4096 + 2560], 2, 4096, 2048)  # behind the last page's bytes
     assert not copy([A + 1000 * 16 * i for i in range(150)], 20, 1000 * 16 * 150, 1000 * 16)
     assert copy([A + 1000 * 16 * i for i in range(151)], 20, 1000 * 16 * 150, 1000 * 16)
 
